@@ -89,7 +89,10 @@ typedef enum {
     CIS_ERR_UNSUPPORTED = 2,   /* valid, but not supported here (layout, GPU)   */
     CIS_ERR_CUDA = 3,          /* a CUDA runtime call or launch failed          */
     CIS_ERR_DEVICE_TIMEOUT = 4,/* device status bit: a bounded wait ran out     */
-    CIS_ERR_BAD_TOKEN_ID = 8   /* device status bit: some valid y_t not in [0,V)*/
+    CIS_ERR_BAD_TOKEN_ID = 8,  /* device status bit: some valid y_t not in [0,V),
+                                * or a list with such an id, or one id twice    */
+    CIS_ERR_BAD_INPUT = 16     /* device status bit: a row's logits or settings
+                                * are not what the call documents               */
 } cis_status_t;
 
 typedef enum { CIS_F32 = 0, CIS_BF16 = 1 } cis_dtype_t;
@@ -428,6 +431,84 @@ CIS_API cis_status_t cis_mismatch_diagnostics(const void *logits_train, const vo
                                               float *logk_out, float *p_out, float *bias2_out,
                                               float *dvar_out, int32_t *dev_status,
                                               void *stream);
+
+/*
+ * Distillation from a teacher's lists: per row t the teacher's most likely
+ * tokens j_k and their log-probabilities a_k (cis_topk_logprobs writes such
+ * lists), against the student's p = softmax(z_t / temperature).  With S the
+ * listed tokens, q_k = e^{a_k}, and the rest r = {j not in S} as one outcome of
+ * probability p_r = sum_{j in r} p_j:
+ *   CIS_DISTILL_FORWARD  q_r = 1 - sum_k q_k, or 0 where that is below tail_min;
+ *       L = sum_k q_k (a_k - log p_k) + q_r (log q_r - log p_r);
+ *       dL/dz_j = (Q p_j - q_j) / temperature in S, Q = sum_k q_k + q_r,
+ *                 p_j (Q - q_r / p_r) / temperature outside.
+ *   CIS_DISTILL_REVERSE  q_r = max(1 - sum_k q_k, tail_min);
+ *       L = sum_k p_k (log p_k - a_k) + p_r (log p_r - log q_r);
+ *       dL/dz_j = p_j (l_j - L) / temperature, l_j = log p_j - a_j in S,
+ *                 log p_r - log q_r outside.
+ *   CIS_DISTILL_TOPK     q = softmax of the list (a_k may then be any scores, such
+ *       as the teacher's logits over the temperature), the rest left out of the
+ *       teacher: L = sum_k q_k (log q_k - log p_k), dL/dz_j = (p_j - q_j) / temperature.
+ * The lists are taken as made at this temperature.  The loss is
+ *   coef sum_t s_t g_t L_t,  s_t the normaliser of params->agg, g_t = token_weight[t].
+ */
+#define CIS_MAX_TOPK 256
+
+typedef enum {
+    CIS_DISTILL_FORWARD = 0,
+    CIS_DISTILL_REVERSE = 1,
+    CIS_DISTILL_TOPK = 2
+} cis_distill_kind_t;
+
+/* Defaults (cis_distill_default_params): forward, token mean, temperature 1,
+ * coef 1, tail_min 1e-6 (what fp32 log-probabilities leave of a full list's 1). */
+typedef struct {
+    int32_t kind;       /* cis_distill_kind_t                                    */
+    int32_t agg;        /* cis_agg_t                                             */
+    double temperature; /* in [1e-3, 1e3]                                        */
+    double coef;        /* finite: weight of the loss, e.g. temperature^2        */
+    double tail_min;    /* in (0, 0.5]: see the kinds above                      */
+    const int64_t *global_counts; /* as in cis_params_t                          */
+} cis_distill_params_t;
+
+CIS_API cis_status_t cis_distill_default_params(cis_distill_params_t *out);
+
+/* Bytes of device workspace cis_distill_fwd_bwd needs for T tokens.  Host only.
+ * CIS_ERR_INVALID_ARG if bytes is NULL or T < 0. */
+CIS_API cis_status_t cis_distill_workspace_size(int64_t T, size_t *bytes);
+
+/*
+ * The distillation loss and its gradient, in one pass over the logits.
+ *   logits       device, [T, ld] of `dtype`, any alignment of its rows.
+ *   top_ids      device int32 [T, ld_top], K of each row read, in any order.
+ *   top_lp       device float [T, ld_top].  A slot with id -1 or log-probability
+ *                -inf is empty.  Any other id outside [0, V), or an id twice in a
+ *                row: CIS_ERR_BAD_TOKEN_ID, kl NaN, dz 0.  A row of empty slots has
+ *                loss and gradient 0, under REVERSE too.
+ *   K            1 .. CIS_MAX_TOPK.
+ *   token_weight device float [T] or NULL (1).
+ *   mask, cu_seqlens, B: as for cis_loss_fwd_bwd (masked rows: kl 0, dz 0).
+ *   dlogits      device, [T, ld_out] of `dlogits_dtype`, written for every j < V;
+ *                NULL: the loss alone.  May not overlap the logits.
+ *   kl_out       device float [T] or NULL: L_t.
+ *   loss_out     device double [1] or NULL.
+ *   workspace    device, >= cis_distill_workspace_size(T) bytes, 256-byte aligned;
+ *                its first int32 is the device status word, zeroed by this call.
+ * A listed token at -inf makes L infinite under FORWARD and TOPK (its gradient
+ * stays finite) and counts 0 under REVERSE.  A row with NaN, +inf or no finite
+ * logit gives NaN.  Deterministic.  Errors: as cis_loss_fwd_bwd, plus
+ * CIS_ERR_INVALID_ARG for K or parameters out of range, ld_top < K or a pointer
+ * that is not aligned to its type, and CIS_ERR_UNSUPPORTED for V above 819200
+ * (bf16 logits) or 409600 (fp32).
+ */
+CIS_API cis_status_t cis_distill_fwd_bwd(const void *logits, int32_t dtype, int64_t T, int64_t V,
+                                         int64_t ld, const int32_t *top_ids, const float *top_lp,
+                                         int32_t K, int64_t ld_top, const float *token_weight,
+                                         const uint8_t *mask, const int32_t *cu_seqlens, int64_t B,
+                                         const cis_distill_params_t *params, void *dlogits,
+                                         int32_t dlogits_dtype, int64_t ld_out, float *kl_out,
+                                         double *loss_out, void *workspace,
+                                         size_t workspace_bytes, void *stream);
 
 /*
  * Confidence-binned counts and sums (Sec. 4.3, Fig. 5b: the sampled tokens

@@ -19,7 +19,7 @@ import torch
 from . import build as _build
 
 CIS_OK, CIS_ERR_INVALID_ARG, CIS_ERR_UNSUPPORTED, CIS_ERR_CUDA = 0, 1, 2, 3
-CIS_ERR_DEVICE_TIMEOUT, CIS_ERR_BAD_TOKEN_ID = 4, 8
+CIS_ERR_DEVICE_TIMEOUT, CIS_ERR_BAD_TOKEN_ID, CIS_ERR_BAD_INPUT = 4, 8, 16
 CIS_F32, CIS_BF16 = 0, 1
 CIS_MODE_CIS, CIS_MODE_TIS, CIS_MODE_EXACT, CIS_MODE_NONE = 0, 1, 2, 3
 CIS_AGG_TOKEN_MEAN, CIS_AGG_SEQ_MEAN_TOKEN_MEAN = 0, 1
@@ -29,6 +29,10 @@ MODES = {"cis": CIS_MODE_CIS, "tis": CIS_MODE_TIS, "exact": CIS_MODE_EXACT,
          "none": CIS_MODE_NONE, "band": CIS_MODE_BAND, "icepop": CIS_MODE_ICEPOP,
          "kpop": CIS_MODE_KPOP, "seq_tis": CIS_MODE_SEQ_TIS, "seq_mis": CIS_MODE_SEQ_MIS}
 SEQ_MODES = ("seq_tis", "seq_mis")
+CIS_DISTILL_FORWARD, CIS_DISTILL_REVERSE, CIS_DISTILL_TOPK = 0, 1, 2
+DISTILL_KINDS = {"forward": CIS_DISTILL_FORWARD, "reverse": CIS_DISTILL_REVERSE,
+                 "topk": CIS_DISTILL_TOPK}
+CIS_MAX_TOPK = 256
 
 
 class cis_params_t(ctypes.Structure):
@@ -61,6 +65,17 @@ class cis_stats_t(ctypes.Structure):
         ("max_abs_logk", ctypes.c_float),
         ("status", ctypes.c_int32),
         ("entropy_sum", ctypes.c_double),
+    ]
+
+
+class cis_distill_params_t(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int32),
+        ("agg", ctypes.c_int32),
+        ("temperature", ctypes.c_double),
+        ("coef", ctypes.c_double),
+        ("tail_min", ctypes.c_double),
+        ("global_counts", ctypes.c_void_p),  # as in cis_params_t
     ]
 
 
@@ -138,6 +153,14 @@ def _load():
                                   ctypes.POINTER(ctypes.c_void_p), i32, P, P, P, ctypes.c_size_t,
                                   P]
     L.cis_binned_sums.restype = ctypes.c_int
+    L.cis_distill_default_params.argtypes = [ctypes.POINTER(cis_distill_params_t)]
+    L.cis_distill_default_params.restype = ctypes.c_int
+    L.cis_distill_workspace_size.argtypes = [i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.cis_distill_workspace_size.restype = ctypes.c_int
+    L.cis_distill_fwd_bwd.argtypes = [P, i32, i64, i64, i64, P, P, i32, i64, P, P, P, i64,
+                                      ctypes.POINTER(cis_distill_params_t), P, i32, i64, P, P, P,
+                                      ctypes.c_size_t, P]
+    L.cis_distill_fwd_bwd.restype = ctypes.c_int
     _load_native(path)
     return L
 
@@ -242,14 +265,14 @@ def cis_count_valid(T: int, mask=None, cu_seqlens=None, out=None) -> torch.Tenso
     return out
 
 
-def with_global_counts(params: cis_params_t, counts: torch.Tensor) -> cis_params_t:
-    """A copy of params whose normaliser uses the batch-wide {N, G} in
+def with_global_counts(params, counts: torch.Tensor):
+    """A copy of params (cis_params_t or cis_distill_params_t) whose normaliser uses the batch-wide {N, G} in
     `counts` (device int64 [2], kept alive by the caller until the call's
     kernels have run)."""
     _need_cuda(counts)
     if counts.dtype != torch.int64 or counts.numel() != 2 or not counts.is_contiguous():
         raise ValueError("counts must be a contiguous device int64 tensor of 2 elements")
-    q = cis_params_t.from_buffer_copy(params)
+    q = type(params).from_buffer_copy(params)
     q.global_counts = counts.data_ptr()
     return q
 
@@ -520,6 +543,90 @@ def cis_mismatch_diagnostics(logits_train: torch.Tensor, logits_infer: torch.Ten
         _ptr(out["p"]), _ptr(out["bias2"]), _ptr(out["dvar"]), _ptr(dev_status), _stream())
     _check(rc, "cis_mismatch_diagnostics")
     return out
+
+
+def cis_distill_default_params(kind="forward", **kw) -> cis_distill_params_t:
+    """Parameters of the distillation loss: `kind` "forward", "reverse" or "topk", with
+    keyword overrides (agg, temperature, coef, tail_min)."""
+    p = cis_distill_params_t()
+    _check(lib().cis_distill_default_params(ctypes.byref(p)), "cis_distill_default_params")
+    p.kind = DISTILL_KINDS[kind] if isinstance(kind, str) else int(kind)
+    for k, v in kw.items():
+        if k not in ("agg", "temperature", "coef", "tail_min"):
+            raise TypeError(f"cis_distill_default_params has no parameter {k!r}")
+        setattr(p, k, v)
+    return p
+
+
+def cis_distill_workspace_size(T: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().cis_distill_workspace_size(T, ctypes.byref(n)), "cis_distill_workspace_size")
+    return n.value
+
+
+def _on(dev, **named):
+    """Every given tensor is on `dev`: the call runs on that device's current stream."""
+    for name, x in named.items():
+        if x is not None and x.device != dev:
+            raise ValueError(f"{name} is on {x.device}, the logits on {dev}")
+
+
+def _list(x, dtype, T, name):
+    if x.dtype != dtype or x.dim() != 2 or x.shape[0] != T or (x.shape[1] > 1 and
+                                                               x.stride(1) != 1):
+        raise ValueError(f"{name} must be a [{T}, K] {dtype} tensor with contiguous rows")
+    return x.stride(0) if T > 1 else x.shape[1]
+
+
+def cis_distill_fwd_bwd(logits: torch.Tensor, top_ids: torch.Tensor, top_lp: torch.Tensor,
+                        params: cis_distill_params_t, token_weight=None, mask=None,
+                        cu_seqlens=None, dlogits=None, dlogits_dtype=None, V=None, want_grad=True,
+                        workspace=None):
+    """Distillation loss against a teacher's lists (`top_ids` int32 and `top_lp` float,
+    [T, K], as cis_topk_logprobs returns them) and its gradient.  Returns a dict with
+    dlogits (None without want_grad), kl (the rows' divergences), loss (device fp64 [1])
+    and the workspace (its first int32 is the device status word)."""
+    _need_cuda(logits, top_ids, top_lp, token_weight, mask, cu_seqlens, dlogits, workspace)
+    T, ld = _rows(logits)
+    V = logits.shape[1] if V is None else V
+    if V > logits.shape[1]:
+        raise ValueError("V is larger than the logits' rows")
+    dev = logits.device
+    ld_top = _list(top_ids, torch.int32, T, "top_ids")
+    if top_lp.shape != top_ids.shape or _list(top_lp, torch.float32, T, "top_lp") != ld_top:
+        raise ValueError("top_ids and top_lp must have the same shape and strides")
+    _vec(token_weight, torch.float32, T, "token_weight")
+    _vec(mask, torch.uint8, T, "mask")
+    B = 0
+    if cu_seqlens is not None:
+        if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or \
+                not cu_seqlens.is_contiguous():
+            raise ValueError("cu_seqlens must be int32 [B + 1]")
+        B = cu_seqlens.shape[0] - 1
+    if dlogits is None and want_grad:
+        dlogits = torch.empty((T, V), device=dev,
+                              dtype=logits.dtype if dlogits_dtype is None else dlogits_dtype)
+    ld_out, dt_out = V, _dtype_code(logits.dtype)
+    if dlogits is not None:
+        To, ld_out = _rows(dlogits)
+        dt_out = _dtype_code(dlogits.dtype)
+        if To != T or dlogits.shape[1] < V:
+            raise ValueError("dlogits must be [T, >= V]")
+    _on(dev, top_ids=top_ids, top_lp=top_lp, token_weight=token_weight, mask=mask,
+        cu_seqlens=cu_seqlens, dlogits=dlogits, workspace=workspace)
+    nws = cis_distill_workspace_size(T)
+    with torch.cuda.device(dev):
+        kl = torch.empty(T, dtype=torch.float32, device=dev)
+        loss = torch.empty(1, dtype=torch.float64, device=dev)
+        if workspace is None or workspace.numel() < nws:
+            workspace = torch.empty(nws, dtype=torch.uint8, device=dev)
+        rc = lib().cis_distill_fwd_bwd(
+            _ptr(logits), _dtype_code(logits.dtype), T, V, ld, _ptr(top_ids), _ptr(top_lp),
+            top_ids.shape[1], ld_top, _ptr(token_weight), _ptr(mask), _ptr(cu_seqlens), B,
+            ctypes.byref(params), _ptr(dlogits), dt_out, ld_out, _ptr(kl), _ptr(loss),
+            _ptr(workspace), workspace.numel(), _stream())
+    _check(rc, "cis_distill_fwd_bwd")
+    return {"dlogits": dlogits, "kl": kl, "loss": loss, "workspace": workspace}
 
 
 def cis_binned_sums(key: torch.Tensor, edges, values=(), mask=None):

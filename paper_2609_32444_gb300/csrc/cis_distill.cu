@@ -1,0 +1,654 @@
+// cis_distill.cu -- the distillation loss against a teacher's lists and its gradient
+// (cis_distill_fwd_bwd): one read of the logits, one write of dlogits.
+//
+// Per row, with p = softmax(z / tau), the listed tokens S = {j_k} and the teacher's
+// log-probabilities a_k of them (kinds: cis_distill_kind_t):
+//   topk     q = softmax(a):  L = sum_k q_k (log q_k - log p_k),  tau dL/dz_j = p_j - q_j
+//   forward  q_k = e^{a_k}, the rest r = all j not in S with q_r = 1 - sum q:
+//            L = sum_b q_b (log q_b - log p_b) over the listed tokens and r,
+//            tau dL/dz_j = Q p_j - q_j,  for j in r  p_j (Q - q_r / p_r),  Q = sum_b q_b
+//   reverse  L = sum_b p_b (log p_b - log q_b),
+//            tau dL/dz_j = p_j (l_b(j) - L),  l_b = log p_b - log q_b.
+// Outside the list every gradient is one multiple of e^{z_j / tau}: the second pass over
+// the row is that product, and the listed entries (at most 256) are written after it.
+//
+// The listed entries are put at -inf in shared memory before the first pass, so that the
+// sum over the rest is formed by itself: p_r = 1 - p_S would lose it where the list holds
+// nearly all.
+//
+// Precision of L: it is a difference of terms far larger than itself.  With
+// phi(d) = e^{-d} - 1 + d >= 0 and d_b = log q_b - log p_b,
+//   sum_b q_b d_b = sum_b q_b phi(d_b) + sum_b q_b - sum_b p_b,
+// whose last two sums are known (1, or p_S), so that every term is of L's own size, and a
+// common error of the log p_b (that of the row's sum) falls out to first order.
+#include <math.h>
+
+#include "cis_nvtx.h"
+#include "cis_slice.cuh"
+
+namespace cis {
+namespace {
+
+constexpr int kMaxList = CIS_MAX_TOPK;  // listed tokens of a row
+constexpr int kHash = 512;              // slots of the table that finds repeated ids
+constexpr unsigned kAll32 = 0xffffffffu;
+
+// e^{-d} - 1 + d: its series where the terms cancel (the first left out is below 2^-26 of
+// the sum), -d as it stands where e^{-d} is out of range.
+__device__ __forceinline__ float phi_small(float d)
+{
+    float s = 1.0f / 362880.0f;
+    s = fmaf(s, -d, 1.0f / 40320.0f);
+    s = fmaf(s, -d, 1.0f / 5040.0f);
+    s = fmaf(s, -d, 1.0f / 720.0f);
+    s = fmaf(s, -d, 1.0f / 120.0f);
+    s = fmaf(s, -d, 1.0f / 24.0f);
+    s = fmaf(s, -d, 1.0f / 6.0f);
+    s = fmaf(s, -d, 0.5f);
+    return s * d * d;
+}
+// q phi(d) with d = log q - log p, for a term q d: q phi = p + q (d - 1).
+__device__ __forceinline__ float bregman(float q, float p, float d)
+{
+    if (fabsf(d) <= 0.5f)
+        return q * phi_small(d);
+    return q == 0.0f ? p : p + q * (d - 1.0f);
+}
+
+struct ListShared {
+    alignas(8) uint64_t bar[kChunks];
+    alignas(8) uint64_t xbar;
+    alignas(16) float2 part[kMaxCluster];
+    MaxSum red[16];
+    int32_t table[kHash];
+    int32_t id[kMaxList];   // -1: empty
+    float z[kMaxList], a[kMaxList];
+    float4 row;             // the row's max, the rest's multiplier, the list's, S
+    float4 list;            // Q or log-sum, reference of G, its mean
+};
+
+// What warp 0 knows of the list before the row's sum: every lane has it.
+struct ListSums {
+    float ms, ss;      // (max, sum of e^{(z - ms) / tau}) over the listed
+    float qh, ql;      // sum of q (forward, reverse) as a pair
+    float am, lq;      // topk: max a and log of sum e^{a - am}
+    float c0;          // reverse: reference of G_k = (z_k - ms) / tau - a_k - c0
+    float A;           //          sum of e^{(z_k - ms) / tau} G_k
+    bool any;
+};
+
+__device__ __forceinline__ float warp_sum_f(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v += __shfl_xor_sync(kAll32, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max_f(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = max_nan(v, __shfl_xor_sync(kAll32, v, o));
+    return v;
+}
+
+// (z_k - ms) / tau - a_k - c0, rounded about once.
+__device__ __forceinline__ float list_gap(float z, float a, float ms, float c0, const Scale &sc)
+{
+    float l, e1, e2;
+    const float p = scaled_diff(z, ms, sc, l);
+    const float u = two_sum(p, -a, e1), v = two_sum(u, -c0, e2);
+    return v + (e1 + e2 + l);
+}
+
+__device__ ListSums list_sums(const ListShared &sh, int K, int kind, const Scale &sc)
+{
+    const int lane = threadIdx.x & 31;
+    ListSums r{-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f, false};
+    bool any = false;
+    for (int k = lane; k < K; k += 32)
+        if (sh.id[k] >= 0) {
+            any = true;
+            r.ms = max_nan(r.ms, sh.z[k]);
+            r.am = max_nan(r.am, sh.a[k]);
+        }
+    r.any = __any_sync(kAll32, any);
+    r.ms = warp_max_f(r.ms);
+    r.am = warp_max_f(r.am);
+    float ss = 0.0f, sa = 0.0f, qh = 0.0f, ql = 0.0f;
+    for (int k = lane; k < K; k += 32)
+        if (sh.id[k] >= 0) {
+            float l;
+            const float x = scaled_diff(sh.z[k], r.ms, sc, l);
+            if (r.ms != -INFINITY)
+                ss += expf(x + l);
+            if (kind == CIS_DISTILL_TOPK) {
+                sa += expf(sh.a[k] - r.am);
+            } else {
+                float e, lo;
+                const float hi = exp_pair(sh.a[k], 0.0f, lo);
+                qh = two_sum(qh, hi, e);
+                ql += e + lo;
+            }
+        }
+    r.ss = warp_sum_f(ss);
+    if (kind == CIS_DISTILL_TOPK) {
+        r.lq = logf(warp_sum_f(sa));
+        return r;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        float e;
+        const float h = __shfl_xor_sync(kAll32, qh, o), l = __shfl_xor_sync(kAll32, ql, o);
+        qh = two_sum(qh, h, e);
+        ql += l + e;
+    }
+    r.qh = qh;
+    r.ql = ql;
+    if (kind == CIS_DISTILL_REVERSE && r.ms != -INFINITY) {
+        // the reference: any listed token's own value, so that the G_k are of the size of
+        // their differences
+        float c0 = 0.0f;
+        bool have = false;
+        for (int k = lane; k < K; k += 32)
+            if (!have && sh.id[k] >= 0 && sh.z[k] != -INFINITY) {
+                c0 = list_gap(sh.z[k], sh.a[k], r.ms, 0.0f, sc);
+                have = true;
+            }
+        const unsigned who = __ballot_sync(kAll32, have);
+        r.c0 = who ? __shfl_sync(kAll32, c0, __ffs(who) - 1) : 0.0f;
+        float A = 0.0f;
+        for (int k = lane; k < K; k += 32)
+            if (sh.id[k] >= 0 && sh.z[k] != -INFINITY) {
+                float l;
+                const float x = scaled_diff(sh.z[k], r.ms, sc, l);
+                A = fmaf(expf(x + l), list_gap(sh.z[k], sh.a[k], r.ms, r.c0, sc), A);
+            }
+        r.A = warp_sum_f(A);
+    }
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v)
+{
+    return __float2bfloat16_rn(v);
+}
+
+// W results to global memory with a streaming store.
+template <typename OutT, int W>
+__device__ __forceinline__ void store_w(OutT *dst, const float (&v)[W])
+{
+    if constexpr (sizeof(OutT) == 4) {
+        static_assert(W == 4, "one 16-byte store");
+        __stcs(reinterpret_cast<float4 *>(dst), make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+        uint32_t w[W / 2];
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        if constexpr (W == 8)
+            __stcs(reinterpret_cast<uint4 *>(dst), make_uint4(w[0], w[1], w[2], w[3]));
+        else
+            __stcs(reinterpret_cast<uint2 *>(dst), make_uint2(w[0], w[1]));
+    }
+}
+// W entries of the slab.
+template <typename InT, int W>
+__device__ __forceinline__ void load_w(const uint8_t *slab, int g, float (&z)[W])
+{
+    if constexpr (W == 8) {
+        load8<InT>(slab, g, z);
+    } else if constexpr (sizeof(InT) == 4) {
+        const float4 q = reinterpret_cast<const float4 *>(slab)[g];
+        z[0] = q.x; z[1] = q.y; z[2] = q.z; z[3] = q.w;
+    } else {
+        const uint2 q = reinterpret_cast<const uint2 *>(slab)[g];
+        z[0] = bf16_lo(q.x); z[1] = bf16_hi(q.x);
+        z[2] = bf16_lo(q.y); z[3] = bf16_hi(q.y);
+    }
+}
+
+// Zero n entries at dst (any alignment).
+template <typename OutT, int NT> __device__ __forceinline__ void zero_entries(OutT *dst, int n)
+{
+    constexpr int EV = 16 / sizeof(OutT);
+    int head = (int)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / (int)sizeof(OutT);
+    head = head < n ? head : n;
+    const int nvec = (n - head) / EV, tail = head + nvec * EV;
+    for (int v = threadIdx.x; v < nvec; v += NT)
+        __stcs(reinterpret_cast<uint4 *>(dst + head) + v, make_uint4(0, 0, 0, 0));
+    if ((int)threadIdx.x < head)
+        dst[threadIdx.x] = from_float<OutT>(0.0f);
+    else if ((int)threadIdx.x - head < n - tail)
+        dst[tail + threadIdx.x - head] = from_float<OutT>(0.0f);
+}
+
+template <typename InT, typename OutT, int NT>
+__global__ void __launch_bounds__(NT)
+    cis_distill_kernel(const __grid_constant__ DistillArgs a, int64_t slice)
+{
+    extern __shared__ __align__(128) uint8_t dyn_smem[];
+    __shared__ ListShared sh;
+    uint8_t *slab = slab_start(dyn_smem);
+    const ClusterPlace cl = cluster_place();
+    const int64_t t = blockIdx.x / cl.size;
+    const int tid = threadIdx.x, K = a.K;
+    const int64_t v0 = (int64_t)cl.rank * slice;
+    const Slice<InT> sl(reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, v0, slice);
+    OutT *orow = reinterpret_cast<OutT *>(a.dz) + t * a.ld_out + v0;
+    const bool grad = a.dz != nullptr;
+
+    if (tid == 0)
+        allow_next_grid();
+    auto leave = [&](float kl) {  // a row without a gradient
+        if (grad)
+            zero_entries<OutT, NT>(orow, sl.n);
+        if (tid == 0) {
+            grid_wait();  // in every CTA, so that this grid ends after the one before
+            if (cl.rank == 0) {
+                if (a.kl_out)
+                    a.kl_out[t] = kl;
+                a.ws_terms[t] = (double)kl;
+            }
+        }
+    };
+    if (a.mask != nullptr && a.mask[t] == 0) {  // the same branch in the whole cluster
+        leave(0.0f);
+        return;
+    }
+    for (int i = tid; i < kHash; i += NT)
+        sh.table[i] = -1;
+    if (tid == 0) {
+        for (int c = 0; c < kChunks; ++c)
+            mbar_init_only(smem_u32(&sh.bar[c]), 1);
+        mbar_init_only(smem_u32(&sh.xbar), 1);
+        mbar_init_fence();
+        mbar_expect_tx(smem_u32(&sh.xbar), (uint32_t)(cl.size * sizeof(float2)));
+        sl.copy(slab, sh.bar);
+    }
+    if (tid >= 32 && tid < 64)
+        sl.ends(slab, tid - 32);
+    __syncthreads();
+    // The list, while the copy is in flight; a repeated id is found in the table.
+    bool bad = false;
+    for (int k = tid; k < K; k += NT) {
+        int id = a.ids[t * a.ld_list + k];
+        const float lp = a.lp[t * a.ld_list + k];
+        float z = 0.0f;
+        if (id == -1 || lp == -INFINITY) {
+            id = -1;
+        } else if (id < 0 || id >= a.V) {
+            bad = true;
+            id = -1;
+        } else {
+            z = to_f32(reinterpret_cast<const InT *>(a.logits)[t * a.ld + id]);
+            unsigned h = ((unsigned)id * 2654435761u) >> 23;
+            for (int i = 0; i < kHash; ++i, h = (h + 1) & (kHash - 1)) {
+                const int32_t was = atomicCAS(&sh.table[h], -1, id);
+                if (was == -1)
+                    break;
+                if (was == id) {
+                    bad = true;
+                    break;
+                }
+            }
+        }
+        sh.id[k] = id;
+        sh.z[k] = z;
+        sh.a[k] = lp;
+    }
+    bad = __syncthreads_or(bad) != 0;
+    for (int c = 0; c < kChunks && sl.chunk_begin(c) < sl.ng; ++c)
+        wait_or_flag(smem_u32(&sh.bar[c]), false, a.status);
+    if (bad) {  // as every CTA of the cluster finds
+        leave(NAN);
+        if (tid == 0 && cl.rank == 0)
+            set_status(a.status, kStatusBadId);
+        return;
+    }
+    cluster_arrive_relaxed();
+    for (int k = tid; k < K; k += NT) {
+        const int64_t e = (int64_t)sh.id[k] - v0;
+        if (sh.id[k] >= 0 && e >= 0 && e < sl.n)
+            poke_neg_inf<InT>(slab, sl.pad + (int)e);
+    }
+    ListSums ls;
+    if (tid < 32)
+        ls = list_sums(sh, K, a.kind, a.sc);
+    __syncthreads();
+
+    // Pass 1: this thread's maximum over the rest, then its sum.
+    const float kappa = a.sc.kappa;
+    MaxAcc<InT> macc;
+    macc.consume(slab, tid, sl.ng, NT);
+    const float m = macc.result();
+    float s = 0.0f;
+    if (m != -INFINITY) {
+#pragma unroll 2
+        for (int g = tid; g < sl.ng; g += NT) {
+            float z[8];
+            load8_any<InT>(slab, g, z);
+            s += sum8_scaled(z, m, kappa);
+        }
+    }
+    const MaxSum mine = block_scaled<NT>(MaxSum{m, s}, sh.red, kappa);
+    cluster_wait();
+    if (tid < (int)cl.size)
+        st_async_pair(map_rank(smem_u32(&sh.part[cl.rank]), tid), mine.m, mine.s,
+                      map_rank(smem_u32(&sh.xbar), tid));
+    wait_or_flag(smem_u32(&sh.xbar), true, a.status);
+    cluster_arrive_relaxed();  // waited for at the end: no CTA leaves before its peers' stores
+
+    // The row's numbers.  Warp 0 has the list's; its lanes form them all.
+    float M = 0.0f, S = 0.0f, er = 0.0f, es = 0.0f, qr = 0.0f, gr = 0.0f, sw = 0.0f;
+    MaxSum rest{0.0f, 0.0f};
+    if (tid < 32) {
+        rest = combine_scaled(sh.part, cl.size, kappa);
+        M = fmaxf(rest.m, ls.ms);
+        float l;
+        er = rest.m == -INFINITY ? rest.s : rest.s * expf(scaled_diff(rest.m, M, a.sc, l) + l);
+        es = ls.ms == -INFINITY ? ls.ss : ls.ss * expf(scaled_diff(ls.ms, M, a.sc, l) + l);
+        S = er + es;
+        if (M == -INFINITY || ls.ms != ls.ms)
+            S = NAN;  // no finite entry, or NaN among the listed
+        qr = (1.0f - ls.qh) - ls.ql;
+        float mult = 0.0f, Q = 1.0f, mean = 0.0f;
+        if (a.kind == CIS_DISTILL_TOPK) {
+            mult = ls.any ? 1.0f : 0.0f;
+        } else if (a.kind == CIS_DISTILL_FORWARD) {
+            if (qr < a.tail_min) {
+                qr = 0.0f;
+                Q = ls.qh + ls.ql;
+            }
+            mult = er > 0.0f ? fmaf(-qr, S / er, Q) : 0.0f;
+        } else {
+            qr = fmaxf(qr, a.tail_min);
+            if (ls.qh != ls.qh)
+                qr = NAN;
+            if (ls.ms != -INFINITY) {  // (else only the rest: its gradient is 0)
+                gr = rest.s > 0.0f ? (logf(rest.s) - logf(qr)) +
+                                         ((scaled_diff(rest.m, ls.ms, a.sc, l) + l) - ls.c0)
+                                   : 0.0f;
+                const float f = es / ls.ss;
+                mean = (ls.A * f + er * gr) / S;
+                mult = rest.s > 0.0f ? gr - mean : 0.0f;
+            }
+        }
+        if (tid == 0) {
+            grid_wait();  // the workspace is the kernel before's until it has ended
+            sw = a.scale[t] * a.coef;
+            if (a.token_weight)
+                sw *= a.token_weight[t];
+            const float c = sw * a.sc.hi;
+            sh.row = make_float4(M, er == 0.0f ? 0.0f : c * mult / S, c, S);
+            sh.list = make_float4(Q, mean, ls.c0, ls.ms);
+            if (a.kind == CIS_DISTILL_TOPK)
+                sh.list = make_float4(ls.any ? ls.lq : 0.0f, ls.am, 0.0f, ls.ms);
+            if (S != S)
+                sh.row.y = NAN;
+        }
+    }
+    __syncthreads();
+
+    // Pass 2: the rest's gradients; the listed entries are at -inf and get 0 here.
+    if (grad) {
+        const float4 row = sh.row;
+        constexpr int W = sizeof(InT) == 4 || sizeof(OutT) == 4 ? 4 : 8;
+        constexpr int EV = 16 / sizeof(OutT);
+        const int phase = (int)(reinterpret_cast<uintptr_t>(orow) / sizeof(OutT)) - sl.pad;
+        const bool whole = (phase & (EV - 1)) == 0;
+        const int g0 = whole ? (sl.pad + W - 1) / W : 0;
+        const int g1 = whole ? (sl.pad + sl.n) / W : 0;
+        auto value = [&](float z) { return row.y * ex2_ftz((z - row.x) * kappa); };
+#pragma unroll 2
+        for (int g = g0 + tid; g < g1; g += NT) {
+            float z[W], v[W];
+            load_w<InT, W>(slab, g, z);
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                v[i] = value(z[i]);
+            store_w<OutT, W>(orow + (W * g - sl.pad), v);
+        }
+        const int e0 = whole ? min(sl.n, g0 ? W * g0 - sl.pad : 0) : 0;
+        const int e1 = whole ? max(e0, W * g1 - sl.pad) : 0;
+        const InT *se = reinterpret_cast<const InT *>(slab);
+        for (int k = tid; k < e0 + (sl.n - e1); k += NT) {
+            const int e = k < e0 ? k : e1 + (k - e0);
+            orow[e] = from_float<OutT>(value(to_f32(se[sl.pad + e])));
+        }
+        __syncthreads();  // the listed entries' values come after the zeros
+        const float4 li = sh.list;
+        for (int k = tid; k < K; k += NT) {
+            const int64_t e = (int64_t)sh.id[k] - v0;
+            if (sh.id[k] < 0 || e < 0 || e >= sl.n)
+                continue;
+            float l;
+            const float x = scaled_diff(sh.z[k], row.x, a.sc, l);
+            const float p = expf(x + l) / row.w;
+            float d;
+            if (a.kind == CIS_DISTILL_TOPK)
+                d = p - expf((sh.a[k] - li.y) - li.x);
+            else if (a.kind == CIS_DISTILL_FORWARD)
+                d = fmaf(li.x, p, -expf(sh.a[k]));
+            else
+                d = p == 0.0f ? 0.0f : p * (list_gap(sh.z[k], sh.a[k], li.w, li.z, a.sc) - li.y);
+            orow[e] = from_float<OutT>(row.z * d);
+        }
+    }
+    // The loss, by the row's first CTA.
+    if (cl.rank == 0 && tid < 32) {
+        const float ls0 = logf(S);
+        // log p_k = (z_k - M) / tau - log S
+        float sum = 0.0f;
+        const float logS = ls0, logSl = log_residual(S, ls0);
+        for (int k = tid; k < K; k += 32) {
+            if (sh.id[k] < 0)
+                continue;
+            float l, e1, e2;
+            const float x = scaled_diff(sh.z[k], M, a.sc, l);
+            const float u = two_sum(x, -logS, e1);  // log p = u + e1 + l - logSl
+            const float p = expf(u + (e1 + l - logSl));
+            float q, lq = sh.a[k], lql = 0.0f;
+            if (a.kind == CIS_DISTILL_TOPK) {
+                float e3;
+                lq = two_sum(sh.a[k], -ls.am, e3);
+                lq = two_sum(lq, -ls.lq, lql);
+                lql += e3;
+                q = expf(lq + lql);
+            } else {
+                q = expf(lq);
+            }
+            const float d0 = two_sum(lq, -u, e2);
+            const float d = sh.z[k] == -INFINITY ? INFINITY : d0 + (e2 + lql - (e1 + l - logSl));
+            if (a.kind == CIS_DISTILL_REVERSE)
+                sum += p == 0.0f ? q : bregman(p, q, -d);
+            else
+                sum += bregman(q, p, d);
+        }
+        sum = warp_sum_f(sum);
+        if (tid == 0) {
+            const float pr = er / S;
+            float kl;
+            if (a.kind == CIS_DISTILL_TOPK) {
+                kl = ls.any ? sum + pr : 0.0f;  // sum q - sum_S p = p_r
+                if (S != S)
+                    kl = NAN;
+            } else {
+                // d_r = log(q_r / p_r)
+                const float ratio = qr * (S / er);
+                const float dr =
+                    fabsf(ratio - 1.0f) < 0.25f ? log1pf(fmaf(qr, S / er, -1.0f)) : logf(ratio);
+                if (a.kind == CIS_DISTILL_FORWARD)
+                    kl = qr > 0.0f ? sum + bregman(qr, pr, dr)
+                                   : sum + (((ls.qh - 1.0f) + ls.ql) + pr);
+                else
+                    kl = sum + (pr == 0.0f ? qr : bregman(pr, qr, -dr)) +
+                         (((1.0f - ls.qh) - ls.ql) - qr);
+            }
+            if (a.kl_out)
+                a.kl_out[t] = kl;
+            a.ws_terms[t] = (double)sw * (double)kl;
+        }
+    }
+    cluster_wait();
+}
+
+template <typename InT, typename OutT, int NT>
+cudaError_t launch_nt(const DistillArgs &a, const RowPlan &p, cudaStream_t s)
+{
+    auto kern = cis_distill_kernel<InT, OutT, NT>;
+    const size_t smem = slab_bytes(p.slice, sizeof(InT));
+    const cudaError_t e = cudaFuncSetAttribute(
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.T * p.cs), 1, 1);
+    cfg.blockDim = dim3(NT, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.cs;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, a, p.slice);
+}
+
+template <typename InT, typename OutT>
+cudaError_t launch_distill_t(const DistillArgs &a, cudaStream_t s)
+{
+    const RowPlan p = row_plan(a.V, (int)sizeof(InT));
+    return p.nt == 128 ? launch_nt<InT, OutT, 128>(a, p, s) : launch_nt<InT, OutT, 256>(a, p, s);
+}
+
+bool distill_params_ok(const cis_distill_params_t *p)
+{
+    return p != nullptr && p->kind >= CIS_DISTILL_FORWARD && p->kind <= CIS_DISTILL_TOPK &&
+           (p->agg == CIS_AGG_TOKEN_MEAN || p->agg == CIS_AGG_SEQ_MEAN_TOKEN_MEAN) &&
+           temperature_ok(p->temperature) && isfinite(p->coef) && p->tail_min > 0.0 &&
+           p->tail_min <= 0.5;
+}
+
+}  // namespace
+}  // namespace cis
+
+using namespace cis;
+
+extern "C" {
+
+CIS_API cis_status_t cis_distill_default_params(cis_distill_params_t *out)
+{
+    if (out == nullptr)
+        return CIS_ERR_INVALID_ARG;
+    out->kind = CIS_DISTILL_FORWARD;
+    out->agg = CIS_AGG_TOKEN_MEAN;
+    out->temperature = 1.0;
+    out->coef = 1.0;
+    out->tail_min = 1e-6;
+    out->global_counts = nullptr;
+    return CIS_OK;
+}
+
+CIS_API cis_status_t cis_distill_workspace_size(int64_t T, size_t *bytes)
+{
+    if (bytes == nullptr || T < 0)
+        return CIS_ERR_INVALID_ARG;
+    *bytes = ws_layout(T).total;
+    return CIS_OK;
+}
+
+CIS_API cis_status_t cis_distill_fwd_bwd(const void *logits, int32_t dtype, int64_t T, int64_t V,
+                                         int64_t ld, const int32_t *top_ids, const float *top_lp,
+                                         int32_t K, int64_t ld_top, const float *token_weight,
+                                         const uint8_t *mask, const int32_t *cu_seqlens, int64_t B,
+                                         const cis_distill_params_t *params, void *dlogits,
+                                         int32_t dlogits_dtype, int64_t ld_out, float *kl_out,
+                                         double *loss_out, void *workspace,
+                                         size_t workspace_bytes, void *stream)
+{
+    NvtxRange nvtx_range("cis_distill_fwd_bwd");
+    if (!row_args_ok(logits, dtype, T, V, ld) || K < 1 || K > CIS_MAX_TOPK || ld_top < K ||
+        !distill_params_ok(params))
+        return CIS_ERR_INVALID_ARG;
+    const bool grad = dlogits != nullptr;
+    if (grad && !row_args_ok(dlogits, dlogits_dtype, T, V, ld_out))
+        return CIS_ERR_INVALID_ARG;
+    if (params->agg == CIS_AGG_SEQ_MEAN_TOKEN_MEAN && (cu_seqlens == nullptr || B < 0))
+        return CIS_ERR_INVALID_ARG;
+    const WsLayout L = ws_layout(T);
+    if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
+        workspace_bytes < L.total)
+        return CIS_ERR_INVALID_ARG;
+    if (T > 0 && (logits == nullptr || top_ids == nullptr || top_lp == nullptr))
+        return CIS_ERR_INVALID_ARG;
+    const int ib = dtype == CIS_BF16 ? 2 : 4;
+    if (T > 0 && grad) {
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits);
+        const uintptr_t a1 = a0 + (uintptr_t)((T - 1) * ld + V) * ib;
+        const uintptr_t b0 = reinterpret_cast<uintptr_t>(dlogits);
+        const uintptr_t b1 =
+            b0 + (uintptr_t)((T - 1) * ld_out + V) * (dlogits_dtype == CIS_BF16 ? 2 : 4);
+        if (a0 < b1 && b0 < a1)
+            return CIS_ERR_INVALID_ARG;
+    }
+    if (row_plan(V, ib).cs == 0 || T * kMaxCluster > 0x7fffffffLL)
+        return CIS_ERR_UNSUPPORTED;
+    cudaStream_t s = (cudaStream_t)stream;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    DistillArgs a = {};
+    a.logits = logits;
+    a.T = T;
+    a.V = V;
+    a.ld = ld;
+    a.ids = top_ids;
+    a.lp = top_lp;
+    a.K = K;
+    a.ld_list = ld_top;
+    a.token_weight = token_weight;
+    a.mask = mask;
+    a.scale = reinterpret_cast<float *>(ws + L.scale);
+    a.dz = dlogits;
+    a.ld_out = ld_out;
+    a.kl_out = kl_out;
+    a.ws_terms = reinterpret_cast<double *>(ws + L.terms);
+    a.status = reinterpret_cast<int32_t *>(ws + L.status);
+    a.kind = params->kind;
+    a.sc = make_scale(params->temperature);
+    a.tail_min = (float)params->tail_min;
+    a.coef = (float)params->coef;
+    PassArgs r = {};  // what the reduction needs
+    r.T = T;
+    r.mask = mask;
+    r.ws_terms = a.ws_terms;
+    r.status = a.status;
+    r.red_parts = ws + L.parts;
+    r.red_ticket = reinterpret_cast<uint32_t *>(ws + L.ticket);
+    r.overlap = true;
+    cudaError_t e = launch_scales(mask, T, cu_seqlens, B, params->agg,
+                                  reinterpret_cast<float *>(ws + L.scale), a.status, r.red_ticket,
+                                  s, params->global_counts);
+    if (e == cudaSuccess && T > 0) {
+        if (dtype == CIS_BF16)
+            e = grad && dlogits_dtype == CIS_F32
+                    ? launch_distill_t<__nv_bfloat16, float>(a, s)
+                    : launch_distill_t<__nv_bfloat16, __nv_bfloat16>(a, s);
+        else
+            e = grad && dlogits_dtype == CIS_BF16 ? launch_distill_t<float, __nv_bfloat16>(a, s)
+                                                  : launch_distill_t<float, float>(a, s);
+    }
+    if (e == cudaSuccess)
+        e = launch_reduce(r, nullptr, loss_out, s);
+    return e == cudaSuccess ? CIS_OK
+                            : (e == cudaErrorNotSupported ? CIS_ERR_UNSUPPORTED : CIS_ERR_CUDA);
+}
+
+}  // extern "C"

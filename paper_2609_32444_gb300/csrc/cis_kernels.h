@@ -45,6 +45,51 @@ struct PassArgs {
     bool overlap;
 };
 
+// 1 / temperature as an fp32 pair, and log2e / temperature.
+struct Scale {
+    float hi, lo, kappa;
+};
+inline Scale make_scale(double temperature)
+{
+    const double v = 1.0 / temperature;
+    Scale s;
+    s.hi = (float)v;
+    s.lo = (float)(v - (double)s.hi);
+    s.kappa = (float)(1.4426950408889634074 * v);
+    return s;
+}
+inline bool temperature_ok(double t) { return t >= 1e-3 && t <= 1e3; }
+
+// Logits (or dlogits) of a call: shape, row stride, type, and a base of the type's
+// alignment.
+inline bool row_args_ok(const void *p, int32_t dtype, int64_t T, int64_t V, int64_t ld)
+{
+    return T >= 0 && T <= 0x7fffffffLL && V > 0 && V <= 0x7fffffffLL && ld >= V &&
+           (dtype == CIS_F32 || dtype == CIS_BF16) &&
+           (reinterpret_cast<uintptr_t>(p) & (dtype == CIS_BF16 ? 1 : 3)) == 0;
+}
+
+// One launch of the distillation loss (cis_distill.cu).
+struct DistillArgs {
+    const void *logits;
+    int64_t T, V, ld;
+    const int32_t *ids;  // [T, ld_list], K of a row listed
+    const float *lp;
+    int K;
+    int64_t ld_list;
+    const float *token_weight;  // may be null
+    const uint8_t *mask;        // null: every token valid
+    const float *scale;         // s_t [T]
+    void *dz;                   // null: the loss alone
+    int64_t ld_out;
+    float *kl_out;              // may be null
+    double *ws_terms;
+    int32_t *status;
+    int32_t kind;
+    Scale sc;
+    float tail_min, coef;
+};
+
 // Host-side parameter checks and the kernels' copy of the parameters.
 bool params_ok(const cis_params_t *p);
 DevParams make_dev_params(const cis_params_t &p);

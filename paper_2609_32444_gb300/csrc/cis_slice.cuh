@@ -1,0 +1,213 @@
+// cis_slice.cuh -- one CTA's slice of a row in shared memory, for rows of any
+// alignment and length: the kernels that read a row several times (the distillation
+// loss, the teacher's lists, the sampler) split it over the CTAs of a cluster and hold
+// every slice on chip.
+//
+// The slab starts at the 8-entry boundary of global memory at or before the slice:
+// `pad` entries before the slice, and those after it up to a whole group of 8, are
+// -inf.  Bulk copies bring the 16-byte blocks that lie inside the slice, plain loads
+// the few entries at its two ends; nothing outside the slice is read.
+//
+// Exponents are formed as (z - m) kappa, kappa = log2e / temperature: one more packed
+// subtraction for two entries than z kappa - m kappa, and in return no rounding of an
+// offset to take out and no other form for maxima of any size (masked entries at
+// -1e9 or the type's lowest value).
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "cis_dsmem.cuh"
+#include "cis_kernels.h"
+
+namespace cis {
+namespace {
+
+struct ClusterPlace {
+    unsigned rank, size;
+};
+__device__ __forceinline__ ClusterPlace cluster_place()
+{
+    const cooperative_groups::cluster_group c = cooperative_groups::this_cluster();
+    return {c.block_rank(), c.num_blocks()};
+}
+
+template <typename InT> struct Slice {
+    const InT *src;  // the slice's first entry
+    int n;           // entries
+    int pad;         // entries of the slab before it
+    int ng;          // groups of 8 in the slab
+    int qg;          // groups per copy chunk
+
+    __device__ __forceinline__ Slice(const InT *row, int64_t V, int64_t v0, int64_t slice)
+    {
+        const int64_t left = V - v0;
+        n = (int)(left <= 0 ? 0 : (left < slice ? left : slice));
+        src = row + v0;
+        pad = (int)(reinterpret_cast<uintptr_t>(src) / sizeof(InT) & 7);
+        ng = n > 0 ? (pad + n + 7) / 8 : 0;
+        qg = (ng + kChunks - 1) / kChunks;
+    }
+    __device__ __forceinline__ int chunk_begin(int c) const { return c * qg; }
+    __device__ __forceinline__ int chunk_end(int c) const { return min(ng, (c + 1) * qg); }
+    // The 16-byte blocks inside the slice, as addresses.
+    __device__ __forceinline__ void blocks(uintptr_t &a0, uintptr_t &a1) const
+    {
+        const uintptr_t b0 = reinterpret_cast<uintptr_t>(src);
+        const uintptr_t b1 = b0 + (uintptr_t)n * sizeof(InT);
+        a1 = b1 & ~(uintptr_t)15;
+        a0 = (b0 + 15) & ~(uintptr_t)15;
+        a0 = a0 < a1 ? a0 : a1;
+    }
+    // One thread, the barriers initialised with one arrival each.
+    __device__ __forceinline__ void copy(uint8_t *slab, uint64_t *bar) const
+    {
+        constexpr int kGroup = 8 * (int)sizeof(InT);
+        uintptr_t a0, a1;
+        blocks(a0, a1);
+        const uintptr_t base = reinterpret_cast<uintptr_t>(src) - (uintptr_t)pad * sizeof(InT);
+        for (int c = 0; c < kChunks && chunk_begin(c) < ng; ++c) {
+            uintptr_t lo = base + (uintptr_t)chunk_begin(c) * kGroup;
+            uintptr_t hi = base + (uintptr_t)chunk_end(c) * kGroup;
+            lo = lo < a0 ? a0 : lo;
+            hi = hi > a1 ? a1 : hi;
+            const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) : 0u;
+            const uint32_t b = smem_u32(&bar[c]);
+            mbar_expect_tx(b, bytes);
+            if (bytes)
+                bulk_g2s(smem_u32(slab) + (uint32_t)(lo - base),
+                         reinterpret_cast<const void *>(lo), bytes, b);
+        }
+    }
+    // The ends, by the 32 lanes of one warp: the entries outside the blocks, at most 7
+    // on each side, and the padding.
+    __device__ __forceinline__ void ends(uint8_t *slab, int lane) const
+    {
+        if (n == 0)
+            return;
+        uintptr_t a0, a1;
+        blocks(a0, a1);
+        const uintptr_t b0 = reinterpret_cast<uintptr_t>(src);
+        const int he = (int)((a0 > b0 ? a0 - b0 : 0) / sizeof(InT));
+        const int te = (int)((a1 > b0 ? a1 - b0 : 0) / sizeof(InT));
+        InT *sl = reinterpret_cast<InT *>(slab);
+        // lanes 0..15 the head, 16..31 the tail (without a block: all of it is tail)
+        const int e = lane < 16 ? lane : te + (lane - 16);
+        if (lane < 16 ? e < he : e < n)
+            sl[pad + e] = src[e];
+        if (lane < pad)
+            poke_neg_inf<InT>(slab, lane);
+        if (lane < 8 * ng - pad - n)
+            poke_neg_inf<InT>(slab, pad + n + lane);
+    }
+};
+
+// CTAs per row, the entries of each (a multiple of 8) and their width: the smallest
+// cluster whose slices are within 80 KB, then up to 200 KB each; cs = 0 where 8 CTAs cannot
+// hold the row (over 819,200 bf16 or 409,600 fp32 entries).  The rule and the widths are
+// those of the fused pass, which reads and writes the same bytes.
+struct RowPlan {
+    int cs;
+    int64_t slice;
+    int nt;
+};
+inline RowPlan row_plan(int64_t V, int in_bytes)
+{
+    for (int cs = 1; cs <= kMaxCluster; ++cs) {
+        int64_t slice = ((V + cs - 1) / cs + 7) / 8 * 8;
+        if (slice * in_bytes <= 80 * 1024 || cs == kMaxCluster) {
+            if (slice * in_bytes > 200 * 1024)
+                return {0, 0, 0};
+            if (cs == 1 && slice * in_bytes > 40 * 1024) {
+                slice = ((V + 1) / 2 + 7) / 8 * 8;
+                return {2, slice, 128};
+            }
+            return {cs, slice, in_bytes == 4 || (cs == 1 && slice <= 16384) ? 128 : 256};
+        }
+    }
+    return {0, 0, 0};
+}
+
+// Bytes of a slab of `slice` entries, whatever its alignment, and room to start it on
+// a 128-byte boundary.
+constexpr size_t slab_bytes(int64_t slice, int in_bytes)
+{
+    return (size_t)(slice + 16) * in_bytes + 128;
+}
+__device__ __forceinline__ uint8_t *slab_start(uint8_t *dyn)
+{
+    return dyn + ((128 - (smem_u32(dyn) & 127)) & 127);
+}
+
+// Sum of 2^{(z_i - m) kappa} over 8 values, added pairwise.
+__device__ __forceinline__ float sum8_scaled(const float (&z)[8], float m, float kappa)
+{
+    const float2 nm = make_float2(-m, -m), k2 = make_float2(kappa, kappa);
+    float2 e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x =
+            __fmul2_rn(__fadd2_rn(make_float2(z[2 * i], z[2 * i + 1]), nm), k2);
+        e[i] = make_float2(ex2_ftz(x.x), ex2_ftz(x.y));
+    }
+    const float2 s = __fadd2_rn(__fadd2_rn(e[0], e[1]), __fadd2_rn(e[2], e[3]));
+    return s.x + s.y;
+}
+
+// (max, sum of 2^{(z - max) kappa}) of two sets; empty: (-inf, 0).
+__device__ __forceinline__ MaxSum scaled_combine(MaxSum a, MaxSum b, float kappa)
+{
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY)
+        return {m, a.s + b.s};
+    const float sa = a.m == -INFINITY ? a.s * 0.0f : a.s * ex2_ftz((a.m - m) * kappa);
+    const float sb = b.m == -INFINITY ? b.s * 0.0f : b.s * ex2_ftz((b.m - m) * kappa);
+    return {m, sa + sb};
+}
+
+// The CTA's (max, sum); every thread gets it.  sh: NT / 32 slots, used once.
+template <int NT>
+__device__ __forceinline__ MaxSum block_scaled(MaxSum v, MaxSum *sh, float kappa)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v = scaled_combine(v, {__shfl_xor_sync(0xffffffffu, v.m, o),
+                               __shfl_xor_sync(0xffffffffu, v.s, o)}, kappa);
+    if ((threadIdx.x & 31) == 0)
+        sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float M = sh[0].m;
+#pragma unroll
+    for (int i = 1; i < NT / 32; ++i)
+        M = fmaxf(M, sh[i].m);
+    float S = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) {
+        const MaxSum q = sh[i];
+        S += M == -INFINITY ? q.s : q.s * ex2_ftz((q.m - M) * kappa);
+    }
+    return {M, S};
+}
+
+// The pairs of a cluster's n CTAs, in rank order.
+__device__ __forceinline__ MaxSum combine_scaled(const float2 *part, unsigned n, float kappa)
+{
+    float M = part[0].x;
+    for (unsigned r = 1; r < n; ++r)
+        M = fmaxf(M, part[r].x);
+    float S = 0.0f;
+    for (unsigned r = 0; r < n; ++r)
+        S += M == -INFINITY ? part[r].y : part[r].y * ex2_ftz((part[r].x - M) * kappa);
+    return {M, S};
+}
+
+// (z - m) / temperature as an unevaluated pair.
+__device__ __forceinline__ float scaled_diff(float z, float m, const Scale &s, float &lo)
+{
+    float dl;
+    const float d = two_sum(z, -m, dl), p = d * s.hi;
+    lo = isfinite(p) ? fmaf(d, s.hi, -p) + fmaf(d, s.lo, dl * s.hi) : 0.0f;
+    return p;
+}
+
+}  // namespace
+}  // namespace cis

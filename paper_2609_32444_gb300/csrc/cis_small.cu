@@ -317,9 +317,9 @@ __global__ void __launch_bounds__(kRedTokens)
         p.loss = terms[t];
         if (is_valid(mask, t)) {
             p.nvalid = 1;
-            const float lk = logk[t];
+            const float lk = logk ? logk[t] : 0.0f;
             p.maxlk = fabsf(lk);
-            if (trunc[t]) {
+            if (trunc && trunc[t]) {
                 p.ntrunc = 1;
                 p.excess = exp((double)lk) - (double)w[t];
             }
