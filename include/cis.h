@@ -432,6 +432,73 @@ CIS_API cis_status_t cis_mismatch_diagnostics(const void *logits_train, const vo
                                               float *dvar_out, int32_t *dev_status,
                                               void *stream);
 
+/* Longest list of a row that cis_topk_logprobs writes and cis_distill_fwd_bwd reads. */
+#define CIS_MAX_TOPK 256
+
+/*
+ * Samples a token from each row of logits, from given uniform numbers.  With s =
+ * z / temperature and a row's order (z descending, then index ascending), the
+ * kept entries are a prefix of that order:
+ *   top_k  its first top_k entries (<= 0: all);
+ *   top_p  of those, the smallest prefix whose mass, the sum of e^s, is at least
+ *          top_p of theirs;
+ *   min_p  of those, the entries with e^s >= min_p e^{s_max}.
+ * The sample is the first entry, by index, whose running kept mass is above u
+ * times the kept mass.  temperature 0 takes the first entry of the order.
+ *   logits         device, [T, ld] of `dtype`, any alignment of its rows.
+ *   u              device float [T], each in [0, 1).
+ *   temperature    device float [T], each 0 or in [1e-3, 1e3]; NULL: 1.
+ *   top_k          device int32 [T] or NULL (off).
+ *   top_p          device float [T], each in (0, 1], or NULL (1).
+ *   min_p          device float [T], each in [0, 1], or NULL (0).
+ *   mask           device uint8 [T] or NULL; masked rows are not read and get id
+ *                  -1 and 0 for the log-probabilities.
+ *   ids_out        device int32 [T].
+ *   lp_out         device float [T] or NULL: the sampled token's log-probability
+ *                  at temperature 1 with nothing left out, the raw value that
+ *                  cis_loss_fwd_bwd takes as lp_infer.
+ *   lp_sampled_out device float [T] or NULL: its log-probability in the
+ *                  distribution it was drawn from (0 at temperature 0).
+ *   dev_status     device int32 [1] or NULL: device status bits are OR-ed in.
+ * A row with NaN, +inf or no finite logit, or a setting outside its range:
+ * CIS_ERR_BAD_INPUT, id -1 and NaN.  Entries at -inf are never sampled.  The
+ * decisions are taken on masses that are right to 2^-42 of each and 2^-44 of the
+ * row's largest.  Deterministic.  Errors: CIS_ERR_INVALID_ARG for NULL required
+ * pointers, T < 0, V <= 0, ld < V, an unknown dtype or logits not aligned to
+ * their type; CIS_ERR_UNSUPPORTED for V above 2^20.
+ */
+CIS_API cis_status_t cis_sample_tokens(const void *logits, int32_t dtype, int64_t T, int64_t V,
+                                       int64_t ld, const float *u, const float *temperature,
+                                       const int32_t *top_k, const float *top_p,
+                                       const float *min_p, const uint8_t *mask, int32_t *ids_out,
+                                       float *lp_out, float *lp_sampled_out, int32_t *dev_status,
+                                       void *stream);
+
+/*
+ * The K most likely tokens of each row with their log-probabilities: the lists
+ * that a teacher hands to cis_distill_fwd_bwd.
+ *   logits      device, [T, ld] of `dtype`, any alignment of its rows.
+ *   K           1 .. CIS_MAX_TOPK.
+ *   temperature in [1e-3, 1e3]: the log-probabilities are those of
+ *               softmax(z / temperature).
+ *   mask        device uint8 [T] or NULL; masked rows are not read: empty slots,
+ *               lse 0.
+ *   ids_out     device int32 [T, K]: in the order of the logits, the lower index
+ *               first among equal ones.  Entries at -inf are not listed; slots
+ *               without a token have id -1 and log-probability -inf.
+ *   lp_out      device float [T, K].
+ *   lse_out     device float [T] or NULL: logsumexp of z / temperature.
+ *   dev_status  device int32 [1] or NULL: device status bits are OR-ed in.
+ * A row with NaN, +inf or no finite logit: CIS_ERR_BAD_INPUT, ids -1 and NaN.
+ * Deterministic.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, T < 0,
+ * V <= 0, ld < V, an unknown dtype, logits not aligned to their type, K or the
+ * temperature out of range; CIS_ERR_UNSUPPORTED for V above 2^20.
+ */
+CIS_API cis_status_t cis_topk_logprobs(const void *logits, int32_t dtype, int64_t T, int64_t V,
+                                       int64_t ld, int32_t K, double temperature,
+                                       const uint8_t *mask, int32_t *ids_out, float *lp_out,
+                                       float *lse_out, int32_t *dev_status, void *stream);
+
 /*
  * Distillation from a teacher's lists: per row t the teacher's most likely
  * tokens j_k and their log-probabilities a_k (cis_topk_logprobs writes such
@@ -452,8 +519,6 @@ CIS_API cis_status_t cis_mismatch_diagnostics(const void *logits_train, const vo
  * The lists are taken as made at this temperature.  The loss is
  *   coef sum_t s_t g_t L_t,  s_t the normaliser of params->agg, g_t = token_weight[t].
  */
-#define CIS_MAX_TOPK 256
-
 typedef enum {
     CIS_DISTILL_FORWARD = 0,
     CIS_DISTILL_REVERSE = 1,

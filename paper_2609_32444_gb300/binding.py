@@ -161,6 +161,10 @@ def _load():
                                       ctypes.POINTER(cis_distill_params_t), P, i32, i64, P, P, P,
                                       ctypes.c_size_t, P]
     L.cis_distill_fwd_bwd.restype = ctypes.c_int
+    L.cis_sample_tokens.argtypes = [P, i32, i64, i64, i64, P, P, P, P, P, P, P, P, P, P, P]
+    L.cis_sample_tokens.restype = ctypes.c_int
+    L.cis_topk_logprobs.argtypes = [P, i32, i64, i64, i64, i32, ctypes.c_double, P, P, P, P, P, P]
+    L.cis_topk_logprobs.restype = ctypes.c_int
     _load_native(path)
     return L
 
@@ -543,6 +547,64 @@ def cis_mismatch_diagnostics(logits_train: torch.Tensor, logits_infer: torch.Ten
         _ptr(out["p"]), _ptr(out["bias2"]), _ptr(out["dvar"]), _ptr(dev_status), _stream())
     _check(rc, "cis_mismatch_diagnostics")
     return out
+
+
+def cis_sample_tokens(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=None,
+                      top_p=None, min_p=None, mask=None, V=None, want_lp=True,
+                      want_lp_sampled=False, dev_status=None):
+    """A token of each row from the uniform numbers `u` (float [T]); temperature, top_p and
+    min_p are float [T], top_k int32 [T], each optional.  Returns (ids int32, lp or None,
+    lp_sampled or None): lp is the raw log-probability that the token pass takes as
+    lp_infer, lp_sampled the one in the distribution that was drawn from."""
+    _need_cuda(logits, u, temperature, top_k, top_p, min_p, mask, dev_status)
+    T, ld = _rows(logits)
+    V = logits.shape[1] if V is None else V
+    if V > logits.shape[1]:
+        raise ValueError("V is larger than the logits' rows")
+    dev = logits.device
+    for x, dt, nm in ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"),
+                      (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+                      (min_p, torch.float32, "min_p"), (mask, torch.uint8, "mask")):
+        _vec(x, dt, T, nm)
+    _on(dev, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, mask=mask,
+        dev_status=dev_status)
+    with torch.cuda.device(dev):
+        ids = torch.empty(T, dtype=torch.int32, device=dev)
+        lp = torch.empty(T, dtype=torch.float32, device=dev) if want_lp else None
+        lps = torch.empty(T, dtype=torch.float32, device=dev) if want_lp_sampled else None
+        rc = lib().cis_sample_tokens(
+            _ptr(logits), _dtype_code(logits.dtype), T, V, ld, _ptr(u), _ptr(temperature),
+            _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(mask), _ptr(ids), _ptr(lp), _ptr(lps),
+            _ptr(dev_status), _stream())
+    _check(rc, "cis_sample_tokens")
+    return ids, lp, lps
+
+
+def cis_topk_logprobs(logits: torch.Tensor, K: int, temperature=1.0, mask=None, V=None,
+                      want_lse=False, dev_status=None):
+    """The K most likely tokens of each row, most likely first, and their
+    log-probabilities under softmax(logits / temperature): (ids int32 [T, K], lp float
+    [T, K], lse or None)."""
+    _need_cuda(logits, mask, dev_status)
+    T, ld = _rows(logits)
+    V = logits.shape[1] if V is None else V
+    if V > logits.shape[1]:
+        raise ValueError("V is larger than the logits' rows")
+    dev = logits.device
+    K = int(K)
+    if not 1 <= K <= CIS_MAX_TOPK:
+        raise ValueError(f"K must be between 1 and {CIS_MAX_TOPK}")
+    _vec(mask, torch.uint8, T, "mask")
+    _on(dev, mask=mask, dev_status=dev_status)
+    with torch.cuda.device(dev):
+        ids = torch.empty((T, K), dtype=torch.int32, device=dev)
+        lp = torch.empty((T, K), dtype=torch.float32, device=dev)
+        lse = torch.empty(T, dtype=torch.float32, device=dev) if want_lse else None
+        rc = lib().cis_topk_logprobs(
+            _ptr(logits), _dtype_code(logits.dtype), T, V, ld, K, float(temperature), _ptr(mask),
+            _ptr(ids), _ptr(lp), _ptr(lse), _ptr(dev_status), _stream())
+    _check(rc, "cis_topk_logprobs")
+    return ids, lp, lse
 
 
 def cis_distill_default_params(kind="forward", **kw) -> cis_distill_params_t:

@@ -61,6 +61,7 @@ __host__ __device__ __forceinline__ bool is_seq_mode(int32_t mode)
 // Device status bits (cis_status_t values that can only be seen on the GPU).
 constexpr int32_t kStatusTimeout = CIS_ERR_DEVICE_TIMEOUT;
 constexpr int32_t kStatusBadId = CIS_ERR_BAD_TOKEN_ID;
+constexpr int32_t kStatusBadInput = CIS_ERR_BAD_INPUT;
 
 // Bounded waits: each mbarrier poll suspends for at most kPollSuspendNs, and a
 // wait gives up after kMaxPolls polls (about 2 s) and reports a timeout.

@@ -90,6 +90,37 @@ struct DistillArgs {
     float tail_min, coef;
 };
 
+// The longest row whose masses (2^43 for the largest entry) add up within 63 bits.
+constexpr int64_t kMaxRowEntries = 1 << 20;
+
+// One launch of the sampler (cis_sample.cu).
+struct SampleArgs {
+    const void *logits;
+    int64_t T, V, ld;
+    const float *u;
+    const float *temperature;  // null: 1
+    const int32_t *top_k;      // null, or <= 0: off
+    const float *top_p;        // null: 1
+    const float *min_p;        // null: 0
+    const uint8_t *mask;
+    int32_t *ids_out;
+    float *lp_out, *lps_out;   // may be null
+    int32_t *status;
+};
+
+// One launch of the teacher's lists (cis_topk.cu).
+struct TopkArgs {
+    const void *logits;
+    int64_t T, V, ld;
+    int K;
+    Scale sc;
+    const uint8_t *mask;
+    int32_t *ids_out;  // [T, K]
+    float *lp_out;     // [T, K]
+    float *lse_out;    // may be null
+    int32_t *status;
+};
+
 // Host-side parameter checks and the kernels' copy of the parameters.
 bool params_ok(const cis_params_t *p);
 DevParams make_dev_params(const cis_params_t &p);

@@ -1,0 +1,389 @@
+// cis_select.cuh -- exact selection in a row's order (value descending, index ascending)
+// by a cluster of CTAs: the k largest, the smallest prefix of a given mass, the entry at
+// which a running mass passes a number.
+//
+// Values are compared as 32-bit keys in the order of the numbers (-0 as +0).  Masses are
+// whole numbers, e^{(z - M) / tau} in units of 2^-43 from an exponential that is right to
+// 2^-42: their sums do not depend on the order they are formed in, so that every CTA, every
+// split and every call come to the same entry, and 2^63 holds a row of 2^20 maxima.
+#pragma once
+
+#include "cis_slice.cuh"
+
+namespace cis {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kMassBits = 43;
+typedef unsigned long long mass_t;
+
+__device__ __forceinline__ uint32_t order_key(float z)
+{
+    const uint32_t b = __float_as_uint(z + 0.0f);  // -0 + 0 = +0
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k)
+{
+    return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
+// An entry in the order: larger is earlier.
+__device__ __forceinline__ mass_t order_pair(uint32_t key, uint32_t index)
+{
+    return ((mass_t)key << 32) | (0xffffffffu - index);
+}
+
+// 1 / tau of a row's own temperature.
+__device__ __forceinline__ Scale device_scale(float tau)
+{
+    const double v = 1.0 / (double)tau;
+    Scale s;
+    s.hi = (float)v;
+    s.lo = (float)(v - (double)s.hi);
+    s.kappa = (float)(1.4426950408889634074 * v);
+    return s;
+}
+
+// 2^{i/32} as fp32 pairs.
+__device__ const float2 kExp2Table[32] = {
+    {1.0f, 0.0f}, {0x1.059b0ep0f, -0x1.9d4f52p-25f},
+    {0x1.0b5586p0f, 0x1.9f3122p-25f}, {0x1.11301ep0f, -0x1.fdb496p-25f},
+    {0x1.172b84p0f, -0x1.c15742p-27f}, {0x1.1d4874p0f, -0x1.d2e8cap-25f},
+    {0x1.2387a6p0f, 0x1.ceac48p-25f}, {0x1.29e9ep0f, -0x1.5c0424p-25f},
+    {0x1.306fep0f, 0x1.4636e2p-25f}, {0x1.371a74p0f, -0x1.18aac6p-25f},
+    {0x1.3dea64p0f, 0x1.824684p-25f}, {0x1.44e086p0f, 0x1.8624b4p-30f},
+    {0x1.4bfdaep0f, -0x1.593abcp-25f}, {0x1.5342b6p0f, -0x1.2c561p-25f},
+    {0x1.5ab07ep0f, -0x1.5bd5ecp-27f}, {0x1.6247ecp0f, -0x1.f8b55p-25f},
+    {0x1.6a09e6p0f, 0x1.9fcef4p-26f}, {0x1.71f75ep0f, 0x1.1d8beep-25f},
+    {0x1.7a1148p0f, -0x1.829fdp-25f}, {0x1.82589ap0f, -0x1.accc7cp-26f},
+    {0x1.8ace54p0f, 0x1.15506ep-27f}, {0x1.93737cp0f, -0x1.e64744p-25f},
+    {0x1.9c4918p0f, 0x1.51f848p-27f}, {0x1.a5503cp0f, -0x1.b83b54p-25f},
+    {0x1.ae89fap0f, -0x1.a94b14p-26f}, {0x1.b7f77p0f, -0x1.a09438p-25f},
+    {0x1.c199bep0f, -0x1.3d56b2p-27f}, {0x1.cb720ep0f, -0x1.8837ccp-27f},
+    {0x1.d5818ep0f, -0x1.822dbcp-27f}, {0x1.dfc974p0f, -0x1.908c94p-25f},
+    {0x1.ea4afap0f, 0x1.52486cp-27f}, {0x1.f50766p0f, -0x1.246ebp-26f}};
+
+// e^{x + x_lo} in units of 2^-43 for -80 < x <= 0, right to 2^-42 and half a unit: x is
+// reduced to n ln2/32 + r, |r| <= 0.011, with ln2/32 in three parts (n has 12 bits and the
+// first part 12, so that the first product is exact), e^r is its Taylor series with the
+// terms up to r^2/2 kept as a pair, and 2^{n/32} comes from the table.
+__device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
+{
+    const float n = rintf(x * (32.0f * kLog2e));
+    const float t0 = fmaf(n, -0x1.62ep-6f, x);
+    float e1, e2, e3;
+    const float p1 = n * -0x1.0bfbe8p-20f, p1e = fmaf(n, -0x1.0bfbe8p-20f, -p1);
+    const float r = two_sum(t0, p1, e1);
+    const float rl = e1 + (p1e + fmaf(n, -0x1.cf79acp-45f, x_lo));
+    float q = fmaf(1.0f / 120.0f, r, 1.0f / 24.0f);
+    q = fmaf(q, r, 1.0f / 6.0f);
+    const float h = 0.5f * r, s2 = h * r, s2e = fmaf(h, r, -s2);
+    const float w = two_sum(r, s2, e2);  // e^{r + rl} - 1 = w + wl
+    const float wl = e2 + (s2e + fmaf(q * r, r * r, rl * (1.0f + w)));
+    const int ni = (int)n;
+    const float2 T = __ldg(&kExp2Table[ni & 31]);
+    const float p = T.x * w, pe = fmaf(T.x, w, -p);
+    const float s = two_sum(T.x, p, e3);
+    const float lo = e3 + (pe + (T.y + fmaf(T.x, wl, T.y * w)));
+    // (43 - 116 at the least: a normal number)
+    const float unit = __int_as_float((127 + kMassBits + (ni >> 5)) << 23);
+    return __float2ull_rz(s * unit) +
+           (unsigned long long)__float2ll_rn((s * unit - truncf(s * unit)) + lo * unit);
+}
+// e^{(z - M) / tau} in units of 2^-43, z <= M; 0 at -inf and below 2^-115.
+__device__ __forceinline__ mass_t fixed_mass(float z, float M, const Scale &sc)
+{
+    float l;
+    const float x = scaled_diff(z, M, sc, l);
+    return x > -80.0f ? fixed_exp(x, l) : 0;
+}
+__device__ __forceinline__ double mass_value(mass_t m)
+{
+    return (double)m / (double)(1ull << kMassBits);
+}
+
+// A row's settings (cis_sample_tokens), checked.
+struct RowSettings {
+    Scale sc;
+    float tau, u, top_p, min_p;
+    int top_k;  // 0: off
+    bool greedy, ok;
+};
+
+// The kept entries: those above `key`, and the first `ties` of those at it, by index.
+struct Kept {
+    uint32_t key;
+    mass_t ties;
+};
+
+// The lowest key that min_p keeps: entries with (z - M) / tau >= log(min_p).
+__device__ inline uint32_t min_p_key(float M, float tau, float min_p)
+{
+    const double lim = log((double)min_p), t = (double)tau;
+    auto in = [&](float z) { return ((double)z - (double)M) / t >= lim; };
+    float z = (float)((double)M + t * lim);
+    z = z > M ? M : z;
+    for (int i = 0; i < 4 && !in(z); ++i)
+        z = nextafterf(z, INFINITY);
+    for (int i = 0; i < 4 && in(nextafterf(z, -INFINITY)); ++i)
+        z = nextafterf(z, -INFINITY);
+    return order_key(z > M ? M : z);
+}
+
+// ------------------------------------------------------------------ clusters
+template <int NT> struct SelectShared {
+    mass_t part[2][2];      // this CTA's share of the running sums
+    mass_t red[2][NT / 32];
+    mass_t hist[256];
+    mass_t tot[256];
+    uint32_t digit;
+    mass_t above, equal;
+    mass_t got;             // the entry that was found (order_pair)
+    mass_t list[512];       // candidates to sort
+    int n;
+    int rows;               // rows of this CTA's share that are left to do
+    int row[NT];
+    float sum;
+};
+
+// One cluster's work on one row; CTA `rank` has the entries [j0, j1).
+template <typename InT, int NT> struct RowSelect {
+    SelectShared<NT> &sh;
+    cg::cluster_group cl;
+    unsigned rank, size;
+    const InT *row;
+    int64_t V, j0, j1;
+    int &buf;  // the exchanges' buffer in turn, across rows
+
+    __device__ RowSelect(SelectShared<NT> &s, const InT *r, int64_t V_, int &turn)
+        : sh(s), cl(cg::this_cluster()), row(r), V(V_), buf(turn)
+    {
+        rank = cl.block_rank();
+        size = cl.num_blocks();
+        j0 = V * rank / size;
+        j1 = V * (rank + 1) / size;
+    }
+    template <typename F> __device__ __forceinline__ void each(F f) const
+    {
+#pragma unroll 4
+        for (int64_t j = j0 + threadIdx.x; j < j1; j += NT)
+            f(j, to_f32(row[j]));
+    }
+    template <typename T> __device__ __forceinline__ const T *peer(T *p, unsigned r)
+    {
+        return cl.map_shared_rank(p, (int)r);
+    }
+    // Two sums over the CTA; in every thread.
+    __device__ void block_sum(mass_t &a, mass_t &b)
+    {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) {
+            sh.red[0][threadIdx.x >> 5] = a;
+            sh.red[1][threadIdx.x >> 5] = b;
+        }
+        __syncthreads();
+        a = b = 0;
+        for (int w = 0; w < NT / 32; ++w) {
+            a += sh.red[0][w];
+            b += sh.red[1][w];
+        }
+    }
+    // Two sums over the cluster, and their parts in the CTAs before this one.  The two
+    // buffers take turns: a CTA writes one again only after the next exchange's barrier,
+    // which its peers reach with their reads of this one done.
+    __device__ void cluster_sum(mass_t &a, mass_t &b, mass_t &a_before, mass_t &b_before)
+    {
+        block_sum(a, b);
+        if (threadIdx.x == 0) {
+            sh.part[buf][0] = a;
+            sh.part[buf][1] = b;
+        }
+        cl.sync();
+        a = b = a_before = b_before = 0;
+        for (unsigned r = 0; r < size; ++r) {
+            const mass_t *p = peer(&sh.part[buf][0], r);
+            const mass_t x = p[0], y = p[1];
+            a_before += r < rank ? x : 0;
+            b_before += r < rank ? y : 0;
+            a += x;
+            b += y;
+        }
+        buf ^= 1;
+    }
+    // The row's largest key; bad: NaN, +inf or no finite entry.
+    __device__ uint32_t max_key(bool &bad)
+    {
+        uint32_t k = 0;
+        mass_t nan = 0;
+        each([&](int64_t, float z) {
+            nan += z != z;
+            k = max(k, order_key(z));
+        });
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0)
+            sh.tot[threadIdx.x >> 5] = k;
+        mass_t any = nan;
+        mass_t none = 0;
+        block_sum(any, none);
+        mass_t m = 0;
+        for (int w = 0; w < NT / 32; ++w)
+            m = max(m, sh.tot[w]);
+        if (threadIdx.x == 0) {
+            sh.part[buf][0] = m;
+            sh.part[buf][1] = any;
+        }
+        cl.sync();
+        m = any = 0;
+        for (unsigned r = 0; r < size; ++r) {
+            const mass_t *p = peer(&sh.part[buf][0], r);
+            m = max(m, p[0]);
+            any += p[1];
+        }
+        buf ^= 1;
+        bad = any != 0 || m <= order_key(-INFINITY) || m >= order_key(INFINITY);
+        return (uint32_t)m;
+    }
+    // The key at which the weight of the entries from the largest on reaches `target`
+    // (1 .. the total): returns it, the weight strictly above it and that at it.
+    template <typename W>
+    __device__ uint32_t select(mass_t target, W weight, mass_t &above, mass_t &equal)
+    {
+        uint32_t prefix = 0;
+        mass_t over = 0;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = threadIdx.x; i < 256; i += NT)
+                sh.hist[i] = 0;
+            __syncthreads();
+            each([&](int64_t, float z) {
+                const uint32_t k = order_key(z);
+                if (shift == 24 || ((k ^ prefix) >> (shift + 8)) == 0) {
+                    const mass_t w = weight(z, k);
+                    if (w)
+                        atomicAdd(&sh.hist[(k >> shift) & 255], w);
+                }
+            });
+            cl.sync();
+            for (int i = threadIdx.x; i < 256; i += NT) {
+                mass_t s = 0;
+                for (unsigned r = 0; r < size; ++r)
+                    s += *peer(&sh.hist[i], r);
+                sh.tot[i] = s;
+            }
+            __syncthreads();
+            if (threadIdx.x < 32) {  // lane l: bins 255 - 8 l and the seven below it
+                const int lane = threadIdx.x;
+                mass_t s = 0;
+                for (int i = 0; i < 8; ++i)
+                    s += sh.tot[255 - 8 * lane - i];
+                mass_t incl = s;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const mass_t v = __shfl_up_sync(0xffffffffu, incl, o);
+                    incl += lane >= o ? v : 0;
+                }
+                mass_t run = over + incl - s;
+                if (run < target && (run + s >= target || lane == 31)) {
+                    int d = 255 - 8 * lane;
+                    for (int i = 0; i < 7 && run + sh.tot[d] < target; ++i)
+                        run += sh.tot[d--];
+                    sh.digit = (uint32_t)d;
+                    sh.above = run;
+                    sh.equal = sh.tot[d];
+                }
+            }
+            cl.sync();  // the peers' reads of the histogram are done as well
+            prefix |= sh.digit << shift;
+            over = sh.above;
+        }
+        above = over;
+        equal = sh.equal;
+        __syncthreads();
+        return prefix;
+    }
+    // Mass above `key` and the number of entries at it, with the parts before this CTA.
+    __device__ void kept_mass(uint32_t key, float M, const Scale &sc, mass_t &gt, mass_t &eq,
+                              mass_t &gt_before, mass_t &eq_before)
+    {
+        gt = eq = 0;
+        each([&](int64_t, float z) {
+            const uint32_t k = order_key(z);
+            if (k > key)
+                gt += fixed_mass(z, M, sc);
+            eq += k == key;
+        });
+        cluster_sum(gt, eq, gt_before, eq_before);
+    }
+    // The first entry, by index, whose running kept mass is above t (below the total): the
+    // CTA that has it returns true in all its threads, with the index.
+    __device__ bool locate(const Kept &kept, mass_t wkey, mass_t t, mass_t gt_before,
+                           mass_t eq_before, float M, const Scale &sc, int64_t &index)
+    {
+        mass_t run = gt_before + min(eq_before, kept.ties) * wkey, ties = eq_before;
+        if (run > t)
+            return false;  // an earlier CTA's
+        if (threadIdx.x == 0)
+            sh.got = 0;
+        for (int64_t b = j0; b < j1; b += NT) {
+            const int64_t j = b + threadIdx.x;
+            mass_t w = 0;
+            uint32_t k = 0;
+            if (j < j1) {
+                const float z = to_f32(row[j]);
+                k = order_key(z);
+                if (k > kept.key)
+                    w = fixed_mass(z, M, sc);
+            }
+            const bool tie = j < j1 && k == kept.key;
+            // this thread's place in the block's order: sums over the entries up to it
+            const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+            mass_t iw = w, it = tie;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const mass_t x = __shfl_up_sync(0xffffffffu, iw, o);
+                const mass_t y = __shfl_up_sync(0xffffffffu, it, o);
+                iw += lane >= o ? x : 0;
+                it += lane >= o ? y : 0;
+            }
+            __syncthreads();
+            if (lane == 31) {
+                sh.red[0][wid] = iw;
+                sh.red[1][wid] = it;
+            }
+            __syncthreads();
+            mass_t bw = 0, bt = 0, tw = 0, tt = 0;
+            for (int i = 0; i < NT / 32; ++i) {
+                const mass_t x = sh.red[0][i], y = sh.red[1][i];
+                bw += i < wid ? x : 0;
+                bt += i < wid ? y : 0;
+                tw += x;
+                tt += y;
+            }
+            // kept masses before the block, up to and before this entry
+            const mass_t before_ties = min(ties, kept.ties);
+            const mass_t upto = run + bw + iw + (min(ties + bt + it, kept.ties) - before_ties) * wkey;
+            const mass_t prev = run + bw + iw - w +
+                                (min(ties + bt + it - tie, kept.ties) - before_ties) * wkey;
+            if (upto > t && prev <= t)
+                sh.got = (mass_t)j + 1;
+            __syncthreads();
+            if (sh.got) {
+                index = (int64_t)sh.got - 1;
+                return true;
+            }
+            run += tw + (min(ties + tt, kept.ties) - before_ties) * wkey;
+            ties += tt;
+        }
+        return false;
+    }
+};
+
+}  // namespace
+}  // namespace cis
