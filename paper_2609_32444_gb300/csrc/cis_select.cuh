@@ -141,9 +141,44 @@ template <int NT> struct SelectShared {
     mass_t got;             // the entry that was found (order_pair)
     mass_t list[512];       // candidates to sort
     int n;
-    int rows;               // rows of this CTA's share that are left to do
-    int row[NT];
-    float sum;
+    unsigned left[NT / 32]; // rows left to do, a bit each
+};
+
+// The rows that one cluster of the exact kernel takes, in order: rows group, group + groups,
+// ... of which `left` says so, NT of them looked at together.  Every CTA of the cluster sees
+// the same: the marks are read before any CTA goes on to write over one.
+template <int NT> struct RowsLeft {
+    SelectShared<NT> &sh;
+    int64_t T, groups, base;
+    int word = NT / 32;
+    unsigned bits = 0;
+
+    __device__ RowsLeft(SelectShared<NT> &s, int64_t T_, int64_t groups_, int64_t group)
+        : sh(s), T(T_), groups(groups_), base(group - (int64_t)NT * groups_)
+    {
+    }
+    template <typename F> __device__ int64_t next(F left)
+    {
+        for (;;) {
+            while (bits == 0 && ++word < NT / 32)
+                bits = sh.left[word];
+            if (bits) {
+                const int b = __ffs(bits) - 1;
+                bits &= bits - 1;
+                return base + (int64_t)(32 * word + b) * groups;
+            }
+            base += (int64_t)NT * groups;
+            if (base >= T)
+                return -1;
+            const int64_t i = base + (int64_t)threadIdx.x * groups;
+            const unsigned b = __ballot_sync(0xffffffffu, i < T && left(i));
+            __syncthreads();
+            if ((threadIdx.x & 31) == 0)
+                sh.left[threadIdx.x >> 5] = b;
+            cg::this_cluster().sync();
+            word = -1;
+        }
+    }
 };
 
 // One cluster's work on one row; CTA `rank` has the entries [j0, j1).

@@ -49,6 +49,12 @@ template <typename InT> struct Slice {
     }
     __device__ __forceinline__ int chunk_begin(int c) const { return c * qg; }
     __device__ __forceinline__ int chunk_end(int c) const { return min(ng, (c + 1) * qg); }
+    // This thread's first group in chunk c, where group g is thread g % NT's.
+    template <int NT> __device__ __forceinline__ int first(int c) const
+    {
+        const int g0 = chunk_begin(c);
+        return g0 + (int)(threadIdx.x + NT - (unsigned)g0 % NT) % NT;
+    }
     // The 16-byte blocks inside the slice, as addresses.
     __device__ __forceinline__ void blocks(uintptr_t &a0, uintptr_t &a1) const
     {
