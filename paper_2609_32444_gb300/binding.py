@@ -191,7 +191,7 @@ def _load_native(path):
     spec = importlib.util.spec_from_file_location("_cis_native", so)
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
-    m.init(path, cis_params_t)
+    m.init(path, cis_params_t, cis_distill_params_t)
     _native = m
 
 
@@ -556,6 +556,13 @@ def cis_sample_tokens(logits: torch.Tensor, u: torch.Tensor, temperature=None, t
     min_p are float [T], top_k int32 [T], each optional.  Returns (ids int32, lp or None,
     lp_sampled or None): lp is the raw log-probability that the token pass takes as
     lp_infer, lp_sampled the one in the distribution that was drawn from."""
+    lib()
+    r = _native.sample_tokens(logits, u, temperature, top_k, top_p, min_p, mask, V, want_lp,
+                              want_lp_sampled, dev_status)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_sample_tokens")
+        return r
     _need_cuda(logits, u, temperature, top_k, top_p, min_p, mask, dev_status)
     T, ld = _rows(logits)
     V = logits.shape[1] if V is None else V
@@ -585,6 +592,12 @@ def cis_topk_logprobs(logits: torch.Tensor, K: int, temperature=1.0, mask=None, 
     """The K most likely tokens of each row, most likely first, and their
     log-probabilities under softmax(logits / temperature): (ids int32 [T, K], lp float
     [T, K], lse or None)."""
+    lib()
+    r = _native.topk_logprobs(logits, K, temperature, mask, V, want_lse, dev_status)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_topk_logprobs")
+        return r
     _need_cuda(logits, mask, dev_status)
     T, ld = _rows(logits)
     V = logits.shape[1] if V is None else V
@@ -648,6 +661,13 @@ def cis_distill_fwd_bwd(logits: torch.Tensor, top_ids: torch.Tensor, top_lp: tor
     [T, K], as cis_topk_logprobs returns them) and its gradient.  Returns a dict with
     dlogits (None without want_grad), kl (the rows' divergences), loss (device fp64 [1])
     and the workspace (its first int32 is the device status word)."""
+    lib()
+    r = _native.distill_fwd_bwd(logits, top_ids, top_lp, params, token_weight, mask, cu_seqlens,
+                                dlogits, dlogits_dtype, V, want_grad, workspace)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_distill_fwd_bwd")
+        return r
     _need_cuda(logits, top_ids, top_lp, token_weight, mask, cu_seqlens, dlogits, workspace)
     T, ld = _rows(logits)
     V = logits.shape[1] if V is None else V

@@ -29,19 +29,32 @@ __device__ __forceinline__ float exp2_accurate(float x)
 
 // Running (m, S[, U]) of one thread in the exponent form above; U = sum e x with
 // x = z log2e - c.  With |m| >= kHugeLogit x = (z - m) log2e and c is not used.
-template <bool kEnt> struct ExpAcc {
+// kScaled: a temperature, kappa = log2e / tau in the place of log2e (without kEnt).
+template <bool kScaled> struct ExpScale {
+    __device__ __forceinline__ static constexpr float kappa() { return kLog2e; }
+    __device__ __forceinline__ static constexpr float huge() { return kHugeLogit; }
+};
+template <> struct ExpScale<true> {
+    float k, h;
+    __device__ __forceinline__ float kappa() const { return k; }
+    __device__ __forceinline__ float huge() const { return h; }
+};
+template <bool kEnt, bool kScaled = false> struct ExpAcc : ExpScale<kScaled> {
+    static_assert(!(kEnt && kScaled), "the entropy's sum is in units of log2e");
+    using ExpScale<kScaled>::kappa;
+    using ExpScale<kScaled>::huge;
     float m = -INFINITY, c = -INFINITY, S = 0.0f, U = 0.0f;
 
-    __device__ __forceinline__ bool fast() const { return fabsf(m) < kHugeLogit; }
+    __device__ __forceinline__ bool fast() const { return fabsf(m) < huge(); }
     // Raise the offset to a larger (or NaN) maximum, in whichever of the two forms
     // each of the maxima has.
     __device__ __forceinline__ void raise(float mx)
     {
         if (mx > m || mx != mx) {
-            const float c1 = ceilf(mx * kLog2e);
-            const bool now = fast(), then = fabsf(mx) < kHugeLogit;
-            const float d = now ? (then ? c - c1 : fmaf(-mx, kLog2e, c))
-                                : (then ? fmaf(m, kLog2e, -c1) : (m - mx) * kLog2e);
+            const float c1 = ceilf(mx * kappa());
+            const bool now = fast(), then = fabsf(mx) < huge();
+            const float d = now ? (then ? c - c1 : fmaf(-mx, kappa(), c))
+                                : (then ? fmaf(m, kappa(), -c1) : (m - mx) * kappa());
             const float f = ex2_ftz(d);
             if (kEnt)
                 U = f == 0.0f ? 0.0f : fmaf(d, S, U) * f;
@@ -54,7 +67,7 @@ template <bool kEnt> struct ExpAcc {
     // offset covers them.
     __device__ __forceinline__ float2 sum8(const float2 (&z)[4], float2 &u) const
     {
-        const float2 l2 = make_float2(kLog2e, kLog2e), nc = make_float2(-c, -c);
+        const float2 l2 = make_float2(kappa(), kappa()), nc = make_float2(-c, -c);
         float2 e[4];
         u = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -87,7 +100,7 @@ template <bool kEnt> struct ExpAcc {
     // One entry, covered by the offset, in either form.
     __device__ __forceinline__ void add_entry(float z)
     {
-        const float x = fast() ? fmaf(z, kLog2e, -c) : (z - m) * kLog2e, e = ex2_ftz(x);
+        const float x = fast() ? fmaf(z, kappa(), -c) : (z - m) * kappa(), e = ex2_ftz(x);
         S += e;
         if (kEnt)
             U = fmaf(e, fmaxf(x, -1024.0f), U);
@@ -99,7 +112,7 @@ template <bool kEnt> struct ExpAcc {
     {
         if (m == -INFINITY)
             return {m, 0.0f, 0.0f};
-        const float err = fast() ? fmaf(m, kLog2e, -c) : 0.0f;
+        const float err = fast() ? fmaf(m, kappa(), -c) : 0.0f;
         const float f = fast() ? exp2_accurate(-err) : 1.0f;
         return {m, S * f, kEnt ? f * kLn2 * fmaf(-err, S, U) : 0.0f};
     }
@@ -107,8 +120,8 @@ template <bool kEnt> struct ExpAcc {
 
 // The CTA's threads' sums together, as sums of e^{z - m}; every thread gets them.
 // red: NT / 32 slots.
-template <int NT, bool kEnt>
-__device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt> &acc, MaxSumU *red)
+template <int NT, bool kEnt, bool kScaled>
+__device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt, kScaled> &acc, MaxSumU *red)
 {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     float M = acc.m;  // (a NaN is kept by its thread's sum)
@@ -122,9 +135,9 @@ __device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt> &acc, MaxSumU *r
 #pragma unroll
     for (int w = 1; w < NT / 32; ++w)
         M = fmaxf(M, red[w].m);
-    ExpAcc<kEnt> all;
+    ExpAcc<kEnt, kScaled> all = acc;
     all.m = M;
-    all.c = ceilf(M * kLog2e);
+    all.c = ceilf(M * acc.kappa());
     if (M == -INFINITY)
         all.c = 0.0f;  // no entry: every sum is 0, or NaN
     // This thread's sums at the common offset: an exact power of two where both are
@@ -132,11 +145,11 @@ __device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt> &acc, MaxSumU *r
     MaxSumU t = acc.result();
     float d, f;
     if (all.fast()) {
-        d = acc.fast() ? acc.c - all.c : fmaf(acc.m, kLog2e, -all.c);
+        d = acc.fast() ? acc.c - all.c : fmaf(acc.m, acc.kappa(), -all.c);
         t.s = acc.S;
         t.u = acc.U;
     } else {
-        d = acc.m == -INFINITY ? -INFINITY : (acc.m - M) * kLog2e;
+        d = acc.m == -INFINITY ? -INFINITY : (acc.m - M) * acc.kappa();
         t.u *= kLog2e;
     }
     f = ex2_ftz(d);
@@ -237,8 +250,8 @@ template <int N> __device__ __forceinline__ float vec_max(const Vec<float> (&v)[
     return m;
 }
 
-template <bool kEnt, int N>
-__device__ __forceinline__ void add_vecs(ExpAcc<kEnt> &acc, const Vec<__nv_bfloat16> (&v)[N])
+template <bool kEnt, int N, bool kScaled>
+__device__ __forceinline__ void add_vecs(ExpAcc<kEnt, kScaled> &acc, const Vec<__nv_bfloat16> (&v)[N])
 {
     float2 s[N], u[N];
 #pragma unroll
@@ -252,8 +265,8 @@ __device__ __forceinline__ void add_vecs(ExpAcc<kEnt> &acc, const Vec<__nv_bfloa
     }
     acc.grow(s, u);
 }
-template <bool kEnt, int N>
-__device__ __forceinline__ void add_vecs(ExpAcc<kEnt> &acc, const Vec<float> (&v)[N])
+template <bool kEnt, int N, bool kScaled>
+__device__ __forceinline__ void add_vecs(ExpAcc<kEnt, kScaled> &acc, const Vec<float> (&v)[N])
 {
     const float2 none = make_float2(-INFINITY, -INFINITY);
     float2 s[(N + 1) / 2], u[(N + 1) / 2];
@@ -271,10 +284,11 @@ __device__ __forceinline__ void add_vecs(ExpAcc<kEnt> &acc, const Vec<float> (&v
     acc.grow(s, u);
 }
 
-template <bool kEnt, int N, typename InT>
-__device__ __forceinline__ void take(ExpAcc<kEnt> &acc, const Vec<InT> (&v)[N])
+template <bool kEnt, int N, typename InT, bool kScaled>
+__device__ __forceinline__ void take(ExpAcc<kEnt, kScaled> &acc, const Vec<InT> (&v)[N],
+                                     float mx)
 {
-    acc.raise(vec_max<N>(v));
+    acc.raise(mx);
     if (acc.fast()) {
         add_vecs<kEnt, N>(acc, v);
     } else if (acc.m != -INFINITY) {
@@ -284,6 +298,12 @@ __device__ __forceinline__ void take(ExpAcc<kEnt> &acc, const Vec<InT> (&v)[N])
             for (int i = 0; i < Vec<InT>::kN; ++i)
                 acc.add_entry(v[k].entry(i));
     }
+}
+
+template <bool kEnt, int N, typename InT>
+__device__ __forceinline__ void take(ExpAcc<kEnt> &acc, const Vec<InT> (&v)[N])
+{
+    take<kEnt, N>(acc, v, vec_max<N>(v));
 }
 
 // Where row's 16-byte vectors lie: the entries before the first whole one, and

@@ -45,9 +45,10 @@ struct PassArgs {
     bool overlap;
 };
 
-// 1 / temperature as an fp32 pair, and log2e / temperature.
+// 1 / temperature as an fp32 pair, log2e / temperature, and the largest maximum whose
+// exponents are formed as z kappa - c (kHugeLogit at temperature 1).
 struct Scale {
-    float hi, lo, kappa;
+    float hi, lo, kappa, huge;
 };
 inline Scale make_scale(double temperature)
 {
@@ -56,6 +57,7 @@ inline Scale make_scale(double temperature)
     s.hi = (float)v;
     s.lo = (float)(v - (double)s.hi);
     s.kappa = (float)(1.4426950408889634074 * v);
+    s.huge = kHugeLogit * (float)temperature;
     return s;
 }
 inline bool temperature_ok(double t) { return t >= 1e-3 && t <= 1e3; }

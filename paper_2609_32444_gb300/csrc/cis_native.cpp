@@ -45,6 +45,10 @@ struct Library {
     decltype(&cis_binned_sums_workspace_size) bins_ws = nullptr;
     decltype(&cis_binned_sums) bins = nullptr;
     decltype(&cis_mismatch_diagnostics) diagnostics = nullptr;
+    decltype(&cis_sample_tokens) sample = nullptr;
+    decltype(&cis_topk_logprobs) topk = nullptr;
+    decltype(&cis_distill_workspace_size) distill_ws = nullptr;
+    decltype(&cis_distill_fwd_bwd) distill = nullptr;
 } lib;
 
 // A tensor argument: None, or a plain tensor (no subclass) with strides.
@@ -95,11 +99,11 @@ bool flag(PyObject *o, bool &v)
     return PyBool_Check(o);
 }
 // The parameter struct behind a ctypes object of the binding's own type, copied.
-PyObject *params_type = nullptr;
-bool params(PyObject *o, cis_params_t &p)
+PyObject *params_type = nullptr, *distill_type = nullptr;
+template <typename P> bool params_of(PyObject *o, const PyObject *type, P &p)
 {
     Py_buffer b;
-    if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != params_type || !PyObject_CheckBuffer(o) ||
+    if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != type || !PyObject_CheckBuffer(o) ||
         PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
         PyErr_Clear();
         return false;
@@ -109,6 +113,24 @@ bool params(PyObject *o, cis_params_t &p)
         memcpy(&p, b.buf, sizeof(p));
     PyBuffer_Release(&b);
     return ok;
+}
+bool params(PyObject *o, cis_params_t &p) { return params_of(o, params_type, p); }
+// Every given tensor is on the device of x, and that is the current one.
+bool together(const Tensor &x, std::initializer_list<const Tensor *> ts)
+{
+    for (const Tensor *t : ts)
+        if (t && t->device() != x.device())
+            return false;
+    return x.is_cuda() && x.device().index() == c10::cuda::current_device();
+}
+// None: the rows' length; else at most that.
+bool vocabulary(PyObject *o, const Tensor &z, int64_t &V)
+{
+    if (o == Py_None) {
+        V = z.size(1);
+        return true;
+    }
+    return integer(o, V) && V <= z.size(1);
 }
 
 template <typename T = void> T *ptr(const Tensor *t)
@@ -395,12 +417,155 @@ PyObject *mismatch_diagnostics(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// init(path, params type): the library's entry points, and the type of `params`.
+// (logits, u, temperature, top_k, top_p, min_p, mask, V, want_lp, want_lp_sampled, dev_status)
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *z, *u, *tau, *k, *p, *m, *mask, *st;
+    bool want_lp, want_lps;
+    if (n != 11 || !take(a[0], z) || !take(a[1], u) || !take(a[2], tau) || !take(a[3], k) ||
+        !take(a[4], p) || !take(a[5], m) || !take(a[6], mask) || !flag(a[8], want_lp) ||
+        !flag(a[9], want_lps) || !take(a[10], st))
+        return none();
+    int64_t T, ld, V;
+    int32_t code;
+    if (!z || !u || !together(*z, {u, tau, k, p, m, mask, st}) || !rows(*z, T, ld) ||
+        !dtype_code(z->scalar_type(), code) || !vocabulary(a[7], *z, V) ||
+        !vec(u, at::kFloat, T) || !vec(tau, at::kFloat, T) || !vec(k, at::kInt, T) ||
+        !vec(p, at::kFloat, T) || !vec(m, at::kFloat, T) || !vec(mask, at::kByte, T))
+        return none();
+    const at::Device dev = z->device();
+    const Tensor ids = fresh({T}, at::kInt, dev), lp = fresh_if(want_lp, T, at::kFloat, dev);
+    const Tensor lps = fresh_if(want_lps, T, at::kFloat, dev);
+    const void *pz = ptr(z);
+    const float *pu = ptr<float>(u), *ptau = ptr<float>(tau), *pp = ptr<float>(p);
+    const float *pm = ptr<float>(m);
+    const int32_t *pk = ptr<int32_t>(k);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    int32_t *pids = ptr<int32_t>(ids), *pst = ptr<int32_t>(st);
+    float *plp = ptr<float>(lp), *plps = ptr<float>(lps);
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.sample(pz, code, T, V, ld, pu, ptau, pk, pp, pm, pmask, pids, plp, plps, pst, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return Py_BuildValue("NNN", wrap(ids), wrap(lp), wrap(lps));
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, K, temperature, mask, V, want_lse, dev_status)
+PyObject *topk_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *z, *mask, *st;
+    bool want_lse;
+    int64_t T, ld, V, K;
+    int32_t code;
+    if (n != 7 || !take(a[0], z) || !integer(a[1], K) || !PyFloat_CheckExact(a[2]) ||
+        !take(a[3], mask) || !flag(a[5], want_lse) || !take(a[6], st))
+        return none();
+    if (!z || !together(*z, {mask, st}) || !rows(*z, T, ld) ||
+        !dtype_code(z->scalar_type(), code) || !vocabulary(a[4], *z, V) ||
+        !vec(mask, at::kByte, T) || K < 1 || K > CIS_MAX_TOPK)
+        return none();
+    const double tau = PyFloat_AS_DOUBLE(a[2]);
+    const at::Device dev = z->device();
+    const Tensor ids = fresh({T, K}, at::kInt, dev), lp = fresh({T, K}, at::kFloat, dev);
+    const Tensor lse = fresh_if(want_lse, T, at::kFloat, dev);
+    const void *pz = ptr(z);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    int32_t *pids = ptr<int32_t>(ids), *pst = ptr<int32_t>(st);
+    float *plp = ptr<float>(lp), *plse = ptr<float>(lse);
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.topk(pz, code, T, V, ld, (int32_t)K, tau, pmask, pids, plp, plse, pst, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return Py_BuildValue("NNN", wrap(ids), wrap(lp), wrap(lse));
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, top_ids, top_lp, params, token_weight, mask, cu_seqlens, dlogits, dlogits_dtype, V,
+//  want_grad, workspace)
+PyObject *distill_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *z, *ids, *lp, *w, *mask, *cu, *dz_in, *ws_in;
+    cis_distill_params_t P;
+    bool grad;
+    if (n != 12 || !take(a[0], z) || !take(a[1], ids) || !take(a[2], lp) ||
+        !params_of(a[3], distill_type, P) || !take(a[4], w) || !take(a[5], mask) ||
+        !take(a[6], cu) || !take(a[7], dz_in) || !flag(a[10], grad) || !take(a[11], ws_in))
+        return none();
+    int64_t T, ld, V, To, ldo, Tl, ldl, Tp, ldp;
+    int32_t code, code_out;
+    if (!z || !ids || !lp || !together(*z, {ids, lp, w, mask, cu, dz_in, ws_in}) ||
+        !rows(*z, T, ld) || !dtype_code(z->scalar_type(), code) || !vocabulary(a[9], *z, V) ||
+        V < 0 || !rows(*ids, Tl, ldl) || !rows(*lp, Tp, ldp) || Tl != T || Tp != T ||
+        ldl != ldp || ids->size(1) != lp->size(1) || ids->scalar_type() != at::kInt ||
+        lp->scalar_type() != at::kFloat || !vec(w, at::kFloat, T) || !vec(mask, at::kByte, T))
+        return none();
+    if (cu && (cu->scalar_type() != at::kInt || cu->dim() != 1 || !cu->is_contiguous()))
+        return none();
+    at::ScalarType dt = z->scalar_type();
+    if (a[8] != Py_None) {
+        if (!THPDtype_Check(a[8]))
+            return none();
+        dt = reinterpret_cast<THPDtype *>(a[8])->scalar_type;
+    }
+    if (dz_in)
+        dt = dz_in->scalar_type();
+    if (!dtype_code(dt, code_out) || ids->size(1) > CIS_MAX_TOPK ||
+        (dz_in && (!rows(*dz_in, To, ldo) || To != T || dz_in->size(1) < V)))
+        return none();
+    size_t need = 0;
+    if (lib.distill_ws(T, &need) != CIS_OK)
+        return none();
+    const at::Device dev = z->device();
+    Tensor dz;
+    ldo = V;
+    if (dz_in)
+        dz = *dz_in;
+    else if (grad)
+        dz = fresh({T, V}, dt, dev);
+    if (dz.defined())
+        rows(dz, To, ldo);
+    const Tensor kl = fresh({T}, at::kFloat, dev), loss = fresh({1}, at::kDouble, dev);
+    const Tensor ws = ws_in && ws_in->numel() >= (int64_t)need ? *ws_in
+                                                               : fresh({(int64_t)need}, at::kByte, dev);
+    const void *pz = ptr(z);
+    const int32_t *pids = ptr<int32_t>(ids), *pcu = ptr<int32_t>(cu);
+    const float *plp = ptr<float>(lp), *pw = ptr<float>(w);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    const int32_t K = (int32_t)ids->size(1);
+    const int64_t nseq = cu ? cu->size(0) - 1 : 0;
+    void *pdz = ptr(dz), *pws = ptr(ws);
+    float *pkl = ptr<float>(kl);
+    double *ploss = ptr<double>(loss);
+    const size_t nws = (size_t)ws.numel();
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.distill(pz, code, T, V, ld, pids, plp, K, ldl, pw, pmask, pcu, nseq, &P, pdz,
+                     code_out, ldo, pkl, ploss, pws, nws, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return dict({{"dlogits", dz}, {"kl", kl}, {"loss", loss}, {"workspace", ws}});
+    END_HANDLE_TH_ERRORS
+}
+
+// init(path, params type, distillation's params type): the library's entry points, and the
+// types of `params`.
 PyObject *init(PyObject *, PyObject *args)
 {
     const char *path;
-    PyObject *type;
-    if (!PyArg_ParseTuple(args, "sO", &path, &type))
+    PyObject *type, *distill;
+    if (!PyArg_ParseTuple(args, "sOO", &path, &type, &distill))
         return nullptr;
     void *h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
     if (h == nullptr)
@@ -417,10 +582,16 @@ PyObject *init(PyObject *, PyObject *args)
     get(lib.bins_ws, "cis_binned_sums_workspace_size");
     get(lib.bins, "cis_binned_sums");
     get(lib.diagnostics, "cis_mismatch_diagnostics");
+    get(lib.sample, "cis_sample_tokens");
+    get(lib.topk, "cis_topk_logprobs");
+    get(lib.distill_ws, "cis_distill_workspace_size");
+    get(lib.distill, "cis_distill_fwd_bwd");
     if (!ok)
         return PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path);
     Py_INCREF(type);
     Py_XSETREF(params_type, type);
+    Py_INCREF(distill);
+    Py_XSETREF(distill_type, distill);
     return none();
 }
 
@@ -435,6 +606,9 @@ PyMethodDef methods[] = {
     {"weights", fast(weights), METH_FASTCALL, nullptr},
     {"binned_sums", fast(binned_sums), METH_FASTCALL, nullptr},
     {"mismatch_diagnostics", fast(mismatch_diagnostics), METH_FASTCALL, nullptr},
+    {"sample_tokens", fast(sample_tokens), METH_FASTCALL, nullptr},
+    {"topk_logprobs", fast(topk_logprobs), METH_FASTCALL, nullptr},
+    {"distill_fwd_bwd", fast(distill_fwd_bwd), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cis_native", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kSelThreads) cis_sample_exact_kernel(const Sam
             rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, M, sc, j);
         // the row's own log-probability: its mass at temperature 1
         mass_t raw = 0, none = 0, x, y;
-        const Scale one{1.0f, 0.0f, kLog2e};
+        const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
         rs.each([&](int64_t, float z) { raw += fixed_mass(z, M, one); });
         rs.cluster_sum(raw, none, x, y);
         if (have && threadIdx.x == 0) {

@@ -41,6 +41,7 @@ __device__ __forceinline__ Scale device_scale(float tau)
     s.hi = (float)v;
     s.lo = (float)(v - (double)s.hi);
     s.kappa = (float)(1.4426950408889634074 * v);
+    s.huge = kHugeLogit * tau;
     return s;
 }
 

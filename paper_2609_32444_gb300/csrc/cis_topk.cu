@@ -3,15 +3,21 @@
 //
 // A row's order is (z descending, index ascending); lp_k = z_k / tau - log sum e^{z / tau}.
 //
-// A cluster of CTAs holds the row in shared memory.  Its first pass keeps, besides the sum of
-// exponentials, four maxima a thread, over disjoint quarters of the thread's entries.  With W
-// warps in the cluster and r = ceil(K / W), at least K entries are not below the least of the
-// warps' r-th largest maxima: that bound leaves some 2 K candidates of a row of any length
-// (measured: 100 to 330 for K = 64, V = 151936), which the second pass finds and the first
-// CTA puts in order by counting, for each, those before it.  A row with more candidates than
-// fit (long runs of equal entries) is left to the exact kernel, which follows.
+// The row is read once, straight into registers (cis_expacc.cuh), as by the forward kernel;
+// besides the sum of exponentials every thread keeps the maximum of each batch of vectors, in
+// shared memory, and four maxima over a quarter of its batches each.  With C CTAs on the row
+// and r = ceil(K / C), at least r entries of a CTA are not below the r-th largest of its
+// maxima, and the least of those over the CTAs bounds the row's K largest from below.  For
+// r <= 16 the CTA's is taken among its warps' four largest; above, it is the least of its 8
+// warps' own ceil(r / 8)-th largest, which needs no exchange of more than one number.  The batches that reach that bound are read again (from L2), their entries
+// that reach it are the candidates, and the first CTA sorts them.  A row with more candidates
+// than fit (long runs of equal entries) is left to the exact kernel, which follows.
+//
+// Before (slices of the row in the shared memory of four CTAs, read three times): T=8192,
+// V=151936, K=64 took 1336 us, at 16 warps an SM and 4900 issue slots a slice.
 #include <math.h>
 
+#include "cis_expacc.cuh"
 #include "cis_nvtx.h"
 #include "cis_select.cuh"
 
@@ -55,34 +61,15 @@ __device__ __forceinline__ void fill_row(const TopkArgs &a, int64_t t, float lp,
         a.lse_out[t] = lse;
 }
 
-constexpr int kCand = 1024;     // candidates of a row
-constexpr int kCandCta = 512;   // of one CTA
-constexpr int32_t kTodo = -2;   // in a row's first id: left to the exact kernel
+constexpr int32_t kTodo = -2;    // in a row's first id: left to the exact kernel
 
-struct TopkShared {
-    alignas(8) uint64_t bar[kChunks];
-    alignas(8) uint64_t xbar;
-    alignas(16) float4 part[kMaxCluster];  // max, sum, bound
-    MaxSum red[16];
-    float bound[16];
-    int n;
+template <int NT> struct TopkShared {
+    float part[kMaxCluster][3];  // each CTA's max, sum and bound
+    MaxSumU red[NT / 32];
+    float bound[NT / 32 * 4];
+    int items, n;
     int count[kMaxCluster];
-    alignas(16) mass_t list[kCandCta];
 };
-
-// The four maxima of a thread.
-__device__ __forceinline__ void max_parts(const MaxAcc<__nv_bfloat16> &a, float (&m)[4])
-{
-    m[0] = __low2float(a.a0);
-    m[1] = __high2float(a.a0);
-    m[2] = __low2float(a.a1);
-    m[3] = __high2float(a.a1);
-}
-__device__ __forceinline__ void max_parts(const MaxAcc<float> &a, float (&m)[4])
-{
-    for (int i = 0; i < 4; ++i)
-        m[i] = a.m[i];
-}
 
 // A value that at least r (1 .. 128) of the warp's 128 maxima are not below: the r-th
 // largest, rounded down to 16 bits.  Bit by bit from the first in which the warp's keys
@@ -109,157 +96,275 @@ __device__ __forceinline__ float warp_bound(const float (&m)[4], int r)
     return v <= (order_key(-INFINITY) >> 16) ? -INFINITY : key_value(v << 16);
 }
 
-template <typename InT, int NT>
-__global__ void __launch_bounds__(NT)
-    cis_topk_kernel(const __grid_constant__ TopkArgs a, int64_t slice, int r)
+// The warp's kTop largest maxima, rounded down to 16 bits, into `out`.
+constexpr int kTop = 4;
+__device__ __forceinline__ void warp_top(const float (&m)[4], float *out)
 {
-    extern __shared__ __align__(128) uint8_t dyn_smem[];
-    __shared__ TopkShared sh;
-    uint8_t *slab = slab_start(dyn_smem);
-    const ClusterPlace cl = cluster_place();
-    const int64_t t = blockIdx.x / cl.size;
+    uint32_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)  // made different by the lane and place: one goes at a time
+        k[i] = (order_key(m[i]) & 0xffff0000u) | ((threadIdx.x & 31) << 2) | i;
+#pragma unroll
+    for (int n = 0; n < kTop; ++n) {
+        const uint32_t best = __reduce_max_sync(0xffffffffu, max(max(k[0], k[1]), max(k[2], k[3])));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            k[i] = k[i] == best ? 0u : k[i];
+        const uint32_t v = best >> 16;
+        if ((threadIdx.x & 31) == 0)
+            out[n] = v <= (order_key(-INFINITY) >> 16) ? -INFINITY : key_value(v << 16);
+    }
+}
+// The r-th largest (1 .. n) of n <= 32 values; every lane gets it.
+__device__ __forceinline__ float nth_of(const float *v, int n, int r)
+{
+    const int lane = threadIdx.x & 31;
+    const float x = lane < n ? v[lane] : -INFINITY;
+    int before = 0;  // values ahead of this one
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const float y = __shfl_sync(0xffffffffu, x, i);
+        before += y > x || (y == x && i < lane);
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, before == r - 1);
+    return __shfl_sync(0xffffffffu, x, who ? __ffs(who) - 1 : 0);
+}
+
+// The maxima of a vector's four quarters.
+__device__ __forceinline__ void quarters(const Vec<__nv_bfloat16> &x, float (&m)[4])
+{
+    const uint32_t w[4] = {x.q.x, x.q.y, x.q.z, x.q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = max_nan(bf16_lo(w[i]), bf16_hi(w[i]));
+}
+__device__ __forceinline__ void quarters(const Vec<float> &x, float (&m)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = x.entry(i);
+}
+
+// kB vectors a batch (1: short rows, and the four maxima are over the vectors' quarters); r:
+// see the top; cap: items and candidates that fit, a power of two.  Dynamic shared memory: cap candidates, cap items, the batches' maxima (and, in
+// their place, the candidates of all CTAs).
+template <typename InT, int NT, int kB>
+__global__ void __launch_bounds__(NT)
+    cis_topk_kernel(const __grid_constant__ TopkArgs a, unsigned cs, int r, int cap)
+{
+    constexpr int EV = Vec<InT>::kN;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
+    __shared__ TopkShared<NT> sh;
+    mass_t *list = reinterpret_cast<mass_t *>(dyn_smem);
+    int *items = reinterpret_cast<int *>(list + cap);
+    float *bmax = reinterpret_cast<float *>(items + cap);
+    const int64_t t = blockIdx.x / cs;
+    const unsigned rank = blockIdx.x - (unsigned)t * cs;
     const int tid = threadIdx.x;
     if (tid == 0)
         allow_next_grid();
-    if (a.mask != nullptr && a.mask[t] == 0) {  // the same branch in the whole cluster
-        if (cl.rank == 0)
+    if (a.mask != nullptr && a.mask[t] == 0) {  // the same branch in every CTA of the row
+        if (rank == 0)
             fill_row(a, t, -INFINITY, 0.0f);
         return;
     }
-    const int64_t v0 = (int64_t)cl.rank * slice;
-    const Slice<InT> sl(reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, v0, slice);
-    if (tid == 0) {
-        for (int c = 0; c < kChunks; ++c)
-            mbar_init_only(smem_u32(&sh.bar[c]), 1);
-        mbar_init_only(smem_u32(&sh.xbar), 1);
-        mbar_init_fence();
-        mbar_expect_tx(smem_u32(&sh.xbar), (uint32_t)(cl.size * sizeof(float4)));
-        sl.copy(slab, sh.bar);
-        sh.n = 0;
-    }
-    if (tid >= 32 && tid < 64)
-        sl.ends(slab, tid - 32);
-    cluster_arrive_relaxed();
-    __syncthreads();
+    if (tid == 0)
+        sh.items = sh.n = 0;
+    const InT *row = reinterpret_cast<const InT *>(a.logits) + t * a.ld;
+    const int V = (int)a.V;
+    const int head = row_head(row, V);
+    const int nvec = (V - head) / EV;
+    const int v0 = (int)((int64_t)nvec * rank / cs), v1 = (int)((int64_t)nvec * (rank + 1) / cs);
+    const uint4 *rv = reinterpret_cast<const uint4 *>(row + head);
 
-    MaxAcc<InT> macc;
-    for (int c = 0; c < kChunks && sl.chunk_begin(c) < sl.ng; ++c) {
-        wait_or_flag(smem_u32(&sh.bar[c]), false, a.status);
-        macc.consume(slab, sl.template first<NT>(c), sl.chunk_end(c), NT);
+    ExpAcc<false, true> acc;
+    acc.k = a.sc.kappa;
+    acc.h = a.sc.huge;
+    float q[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    float *mine = bmax + tid;
+    int nb = 0;
+    auto batch = [&](const Vec<InT> (&x)[kB]) {
+        const float mx = vec_max<kB>(x);
+        *mine = mx;
+        mine += NT;
+        ++nb;
+        if constexpr (kB == 1) {
+            float p[4];
+            quarters(x[0], p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                q[i] = max_nan(q[i], p[i]);
+        } else {
+            const float q0 = max_nan(q[0], mx);
+            q[0] = q[1];
+            q[1] = q[2];
+            q[2] = q[3];
+            q[3] = q0;
+        }
+        take<false, kB>(acc, x, mx);
+    };
+    int v = v0 + tid;
+    for (; v + (kB - 1) * NT < v1; v += kB * NT) {
+        Vec<InT> x[kB];
+#pragma unroll
+        for (int k = 0; k < kB; ++k)
+            x[k].q = __ldg(rv + v + k * NT);
+        batch(x);
     }
-    const float kappa = a.sc.kappa, m = macc.result();
-    float s = 0.0f;
-    if (m != -INFINITY) {
-#pragma unroll 2
-        for (int g = tid; g < sl.ng; g += NT) {
-            float z[8];
-            load8_any<InT>(slab, g, z);
-            s += sum8_scaled(z, m, kappa);
+    if (kB > 1 && v < v1) {  // the last, partial batch: absent vectors count as -inf
+        Vec<InT> x[kB];
+#pragma unroll
+        for (int k = 0; k < kB; ++k)
+            x[k].q = v + k * NT < v1 ? __ldg(rv + v + k * NT)
+                                     : make_uint4(Vec<InT>::kNone, Vec<InT>::kNone,
+                                                  Vec<InT>::kNone, Vec<InT>::kNone);
+        batch(x);
+    }
+    int end = -1;  // the ragged ends, fewer than 2 EV entries: one a thread of the first CTA
+    float zend = -INFINITY;
+    if (rank == 0) {
+        const int tail0 = head + nvec * EV;
+        if (tid < head)
+            end = tid;
+        else if (tid - head < V - tail0)
+            end = tail0 + tid - head;
+        if (end >= 0) {
+            zend = to_f32(row[end]);
+            acc.raise(zend);
+            if (acc.m != -INFINITY)
+                acc.add_entry(zend);
+            q[0] = max_nan(q[0], zend);
         }
     }
-    float parts[4];
-    max_parts(macc, parts);
-    const float wb = warp_bound(parts, r);
-    if ((tid & 31) == 0)
-        sh.bound[tid >> 5] = wb;
-    const MaxSum mine = block_scaled<NT>(MaxSum{m, s}, sh.red, kappa);
-    float bound = sh.bound[0];
-#pragma unroll
-    for (int w = 1; w < NT / 32; ++w)
-        bound = fminf(bound, sh.bound[w]);
-    cluster_wait();
-    if (tid < (int)cl.size)
-        st_async_quad(map_rank(smem_u32(&sh.part[cl.rank]), tid), mine.m, mine.s, bound,
-                      map_rank(smem_u32(&sh.xbar), tid));
-    wait_or_flag(smem_u32(&sh.xbar), true, a.status);
-    float M = sh.part[0].x;
-    for (unsigned q = 0; q < cl.size; ++q) {
-        M = fmaxf(M, sh.part[q].x);
-        bound = fminf(bound, sh.part[q].z);
+    constexpr int W = NT / 32;
+    const bool few = r <= 2 * W;
+    if (few) {
+        warp_top(q, sh.bound + kTop * (tid >> 5));
+    } else {
+        const float wb = warp_bound(q, (r + W - 1) / W);
+        if ((tid & 31) == 0)
+            sh.bound[tid >> 5] = wb;
     }
+    MaxSumU o = block_exp<NT>(acc, sh.red);  // (its barriers)
+    float bound = sh.bound[0];
+    if (few) {
+        bound = nth_of(sh.bound, kTop * W, r);
+    } else {
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+            bound = fminf(bound, sh.bound[w]);
+    }
+    if (cs > 1) {
+        cluster_sync_data();  // every CTA of the row has started
+        if (tid < (int)cs) {
+            float *to = cg::this_cluster().map_shared_rank(&sh.part[rank][0], tid);
+            to[0] = o.m;
+            to[1] = o.s;
+            to[2] = bound;
+        }
+        cluster_sync_data();
+        float M = sh.part[0][0], S = 0.0f;
+        for (unsigned c = 0; c < cs; ++c) {
+            M = fmaxf(M, sh.part[c][0]);
+            bound = fminf(bound, sh.part[c][2]);
+        }
+        for (unsigned c = 0; c < cs; ++c)  // in rank order
+            S += sh.part[c][1] * exp2f((sh.part[c][0] - M) * a.sc.kappa);
+        o.m = M;
+        o.s = S;
+    }
+    const bool bad = !(o.s > 0.0f && o.s < INFINITY) || !(fabsf(o.m) < INFINITY);
 
-    // Pass 2: the candidates.
-    auto keep = [&](float z, int e) {
+    // The batches that reach the bound, then their vectors, one a thread.
+    for (int b = 0; b < nb; ++b) {
+        const float x = bmax[b * NT + tid];
+        if (x >= bound && x != -INFINITY) {
+            const int at = atomicAdd(&sh.items, 1);
+            if (at < cap)
+                items[at] = v0 + b * kB * NT + tid;
+        }
+    }
+    auto offer = [&](float z, int j) {
         if (z >= bound && z != -INFINITY) {
             const int at = atomicAdd(&sh.n, 1);
-            if (at < kCandCta)
-                sh.list[at] = order_pair(order_key(z), (uint32_t)(v0 + (e - sl.pad)));
+            if (at < cap)
+                list[at] = order_pair(order_key(z), (uint32_t)j);
         }
     };
-    for (int g = tid; g < sl.ng; g += NT) {
-        float z[8];
-        load8<InT>(slab, g, z);
-        float top = z[0];
+    if (end >= 0)
+        offer(zend, end);
+    __syncthreads();
+    const int m = min(sh.items, cap);
+    for (int i = tid; i < m * kB; i += NT) {
+        const int w = items[i / kB] + (i % kB) * NT;
+        if (w >= v1)
+            continue;
+        Vec<InT> x;
+        x.q = __ldg(rv + w);
 #pragma unroll
-        for (int i = 1; i < 8; ++i)
-            top = fmaxf(top, z[i]);
-        if (top >= bound)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                keep(z[i], 8 * g + i);
+        for (int k = 0; k < EV; ++k)
+            offer(x.entry(k), head + w * EV + k);
     }
-    cluster_sync_data();
-    // The first CTA gathers the lists, in its slab.
-    mass_t *all = reinterpret_cast<mass_t *>(slab);
-    int n = 0;
-    bool fits = true;
-    if (cl.rank == 0) {
-        const cg::cluster_group cluster = cg::this_cluster();
-        if (tid < (int)cl.size)
-            sh.count[tid] = *cluster.map_shared_rank(&sh.n, tid);
-        __syncthreads();
-        for (unsigned q = 0; q < cl.size; ++q) {
-            const int c = sh.count[q];
-            fits = fits && c <= kCandCta && n + c <= kCand;
-            if (fits) {
-                const mass_t *from = cluster.map_shared_rank(&sh.list[0], (int)q);
-                for (int i = tid; i < c; i += NT)
-                    all[n + i] = from[i];
-                n += c;
+    __syncthreads();
+    int n = sh.items > cap ? cap + 1 : sh.n;
+    if (cs > 1) {  // the first CTA gathers the lists
+        if (tid == 0)
+            sh.n = n;
+        cluster_sync_data();
+        mass_t *all = reinterpret_cast<mass_t *>(bmax);
+        if (rank == 0) {
+            const cg::cluster_group cluster = cg::this_cluster();
+            if (tid < (int)cs)
+                sh.count[tid] = *cluster.map_shared_rank(&sh.n, tid);
+            __syncthreads();
+            n = 0;
+            for (unsigned c = 0; c < cs; ++c) {
+                const int k = sh.count[c];
+                if (n + k <= cap && k <= cap) {
+                    const mass_t *from = cluster.map_shared_rank(list, (int)c);
+                    for (int i = tid; i < k; i += NT)
+                        all[n + i] = from[i];
+                    n += k;
+                } else {
+                    n = cap + 1;
+                }
             }
         }
+        cluster_sync_data();  // no CTA leaves while its list is read
+        if (rank != 0)
+            return;
+        list = all;
     }
-    cluster_sync_data();  // no CTA leaves while its list is read; the list is whole
-    if (cl.rank != 0)
-        return;
-    float S = 0.0f;
-    for (unsigned q = 0; q < cl.size; ++q)
-        S += sh.part[q].y * ex2_ftz((sh.part[q].x - M) * kappa);
-    if (tid == 0)
-        grid_wait();
-    __syncthreads();
-    if (!(S > 0.0f && S < INFINITY) || M == INFINITY) {
+    if (bad) {
         fill_row(a, t, NAN, NAN);
         if (tid == 0)
             set_status(a.status, kStatusBadInput);
         return;
     }
-    if (!fits) {
+    if (n > cap) {
         if (tid == 0)
             a.ids_out[t * a.K] = kTodo;
         return;
     }
-    const float ls = logf(S), lsl = log_residual(S, ls);
-    for (int i = tid; i < n; i += NT) {
-        const mass_t p = all[i];
-        int before = 0;
-        for (int j = 0; j < n; ++j)
-            before += all[j] > p;
-        if (before < a.K) {
+    sort_list<NT>(list, n);
+    const float ls = logf(o.s), lsl = log_residual(o.s, ls);
+    for (int i = tid; i < a.K; i += NT) {
+        if (i < n) {
+            const mass_t p = list[i];
             float l, e;
-            const float x = scaled_diff(key_value((uint32_t)(p >> 32)), M, a.sc, l);
+            const float x = scaled_diff(key_value((uint32_t)(p >> 32)), o.m, a.sc, l);
             const float u = two_sum(x, -ls, e);
-            a.ids_out[t * a.K + before] = (int32_t)(0xffffffffu - (uint32_t)p);
-            a.lp_out[t * a.K + before] = u + (e + l - lsl);
+            a.ids_out[t * a.K + i] = (int32_t)(0xffffffffu - (uint32_t)p);
+            a.lp_out[t * a.K + i] = u + (e + l - lsl);
+        } else {
+            a.ids_out[t * a.K + i] = -1;
+            a.lp_out[t * a.K + i] = -INFINITY;
         }
-    }
-    for (int i = n + tid; i < a.K; i += NT) {
-        a.ids_out[t * a.K + i] = -1;
-        a.lp_out[t * a.K + i] = -INFINITY;
     }
     if (tid == 0 && a.lse_out) {
         float e;
-        const float p = M * a.sc.hi, pl = isfinite(p) ? fmaf(M, a.sc.hi, -p) + M * a.sc.lo : 0.0f;
+        const float p = o.m * a.sc.hi;
+        const float pl = isfinite(p) ? fmaf(o.m, a.sc.hi, -p) + o.m * a.sc.lo : 0.0f;
         const float u = two_sum(p, ls, e);
         a.lse_out[t] = u + (e + pl + lsl);
     }
@@ -360,31 +465,37 @@ __global__ void __launch_bounds__(kSelThreads)
     cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
 
-template <typename InT, int NT>
-cudaError_t launch_fast(const TopkArgs &a, const RowPlan &p, cudaStream_t s)
+template <typename InT, int NT, int kB>
+cudaError_t launch_fast(const TopkArgs &a, int cs, cudaStream_t s)
 {
-    auto kern = cis_topk_kernel<InT, NT>;
-    size_t smem = slab_bytes(p.slice, sizeof(InT));
-    if (smem < kCand * sizeof(mass_t) + 128)
-        smem = kCand * sizeof(mass_t) + 128;
+    auto kern = cis_topk_kernel<InT, NT, kB>;
+    const int64_t vecs = (a.V * (int64_t)sizeof(InT) / 16 + cs - 1) / cs;
+    const int64_t nb = (vecs + kB * NT - 1) / (kB * NT);
+    // short rows always fit, whatever their entries; a long one has some 2 K candidates
+    const int cap = a.V <= 1024 ? 1024 : a.V <= 2048 ? 2048 : a.K <= 64 ? 512 : 1024;
+    size_t maxima = (size_t)(nb * NT) * sizeof(float);
+    if (cs > 1 && maxima < cap * sizeof(mass_t))
+        maxima = cap * sizeof(mass_t);
+    const size_t smem = cap * (sizeof(mass_t) + sizeof(int)) + maxima;
+    if (smem > 200 * 1024)
+        return cudaErrorNotSupported;
     const cudaError_t e = cudaFuncSetAttribute(
         kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.T * p.cs), 1, 1);
+    cfg.gridDim = dim3((unsigned)(a.T * cs), 1, 1);
     cfg.blockDim = dim3(NT, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.cs;
+    attr[0].val.clusterDim.x = (unsigned)cs;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const int warps = p.cs * (NT / 32);
-    return cudaLaunchKernelEx(&cfg, kern, a, p.slice, (a.K + warps - 1) / warps);
+    cfg.numAttrs = cs > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, a, (unsigned)cs, (a.K + cs - 1) / cs, cap);
 }
 
 // The exact kernel: every row, or those that the fast one before it left.
@@ -410,11 +521,17 @@ cudaError_t launch_exact(const TopkArgs &a, bool every, cudaStream_t s)
 
 template <typename InT> cudaError_t launch_topk(const TopkArgs &a, cudaStream_t s)
 {
-    const RowPlan p = row_plan(a.V, (int)sizeof(InT));
-    if (p.cs == 0 || a.T * kMaxCluster > 0x7fffffffLL)
+    if (a.T * kMaxCluster > 0x7fffffffLL)
         return launch_exact<InT>(a, true, s);
-    const cudaError_t e = p.nt == 128 ? launch_fast<InT, 128>(a, p, s)
-                                      : launch_fast<InT, 256>(a, p, s);
+    const int64_t nvec = a.V * (int64_t)sizeof(InT) / 16;
+    int cs = 1;
+    while (cs < kMaxCluster && a.T * cs * 2 <= 608 && nvec / (2 * cs) >= 512)
+        cs *= 2;
+    while (cs < kMaxCluster && nvec / cs > 65536)  // the maxima fit shared memory
+        cs *= 2;
+    const cudaError_t e = nvec <= 512         ? launch_fast<InT, 64, 1>(a, cs, s)
+                          : nvec <= 4096 * cs ? launch_fast<InT, 256, 1>(a, cs, s)
+                                              : launch_fast<InT, 256, 4>(a, cs, s);
     return e != cudaSuccess ? e : launch_exact<InT>(a, false, s);
 }
 
