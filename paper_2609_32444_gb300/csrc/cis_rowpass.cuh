@@ -1,0 +1,268 @@
+// cis_rowpass.cuh -- one read of a row straight into registers, and the row's largest entries
+// (the teacher's lists, the sampler).
+//
+// The CTAs of a cluster, and the warps of a CTA, have consecutive stretches of the row; a
+// warp reads kB 16-byte vectors a lane at a time (a batch).  Besides what the caller forms of
+// them (sums of exponentials), every lane keeps the maximum of each of its batches, in shared
+// memory, and four maxima over a quarter of its entries each.  A CTA's r-th largest of those
+// maxima is a bound that at least r of its entries are not below, and the least of the CTAs'
+// bounds, with r = ceil(K / CTAs), is one that the row's K largest are not below.  The batches
+// that reach the bound are read again (from L2), and their entries that reach it are the
+// candidates: a complete head of the row's order, some 1.3 K long where the entries lie in no
+// particular order.
+#pragma once
+
+#include "cis_select.cuh"
+
+namespace cis {
+namespace {
+
+template <int NT> struct PassShared {
+    float part[kMaxCluster][4];  // each CTA's max, bound and two sums
+    MaxSumU red[NT / 32], red2[NT / 32];
+    float bound[NT / 32 * kTop];
+    int items, n;
+    int count[kMaxCluster];
+};
+
+// The maxima of a vector's four quarters.
+__device__ __forceinline__ void quarters(const Vec<__nv_bfloat16> &x, float (&m)[4])
+{
+    const uint32_t w[4] = {x.q.x, x.q.y, x.q.z, x.q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = max_nan(bf16_lo(w[i]), bf16_hi(w[i]));
+}
+__device__ __forceinline__ void quarters(const Vec<float> &x, float (&m)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        m[i] = x.entry(i);
+}
+
+template <typename InT, int NT, int kB> struct RowPass {
+    static constexpr int EV = Vec<InT>::kN, W = NT / 32;
+    const InT *row;
+    const uint4 *rv;
+    int V, head, nvec;
+    int v0, v1;    // this CTA's vectors
+    int s0, s1;    // this warp's
+    float *bmax;   // [batches][NT]
+    int nb;
+    int end;       // the entry outside the vectors that this thread has (-1: none)
+    float zend;
+    float q[4];
+
+    __device__ __forceinline__ RowPass(const InT *r, int64_t V_, unsigned rank, unsigned cs,
+                                       float *maxima)
+        : row(r), V((int)V_), bmax(maxima), nb(0), end(-1), zend(-INFINITY)
+    {
+        head = row_head(row, V);
+        nvec = (V - head) / EV;
+        rv = reinterpret_cast<const uint4 *>(row + head);
+        v0 = (int)((int64_t)nvec * rank / cs);
+        v1 = (int)((int64_t)nvec * (rank + 1) / cs);
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        s0 = seg(w);
+        s1 = seg(w + 1);
+        // the ragged ends, fewer than EV entries each: the first ones to the first warp of
+        // the row, the last ones to the last
+        const int tail0 = head + nvec * EV;
+        if (rank == 0 && w == 0 && lane < head)
+            end = lane;
+        if (rank == cs - 1 && w == W - 1 && lane >= 16 && lane - 16 < V - tail0)
+            end = tail0 + lane - 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            q[i] = -INFINITY;
+    }
+    __device__ __forceinline__ int seg(int w) const { return v0 + (v1 - v0) * w / W; }
+
+    // take(vectors, their maximum) for every batch, one(entry) for the ragged ends.  Absent
+    // vectors of the last batch count as -inf.
+    template <typename Take, typename One>
+    __device__ __forceinline__ void stream(bool maxima, Take take, One one)
+    {
+        float *mine = bmax + threadIdx.x;
+        auto batch = [&](const Vec<InT> (&x)[kB]) {
+            const float mx = vec_max<kB>(x);
+            if (maxima) {
+                *mine = mx;
+                mine += NT;
+                ++nb;
+                if constexpr (kB == 1) {
+                    float p[4];
+                    quarters(x[0], p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        q[i] = max_nan(q[i], p[i]);
+                } else {
+                    const float q0 = max_nan(q[0], mx);
+                    q[0] = q[1];
+                    q[1] = q[2];
+                    q[2] = q[3];
+                    q[3] = q0;
+                }
+            }
+            take(x, mx);
+        };
+        int v = s0 + (threadIdx.x & 31);
+        for (; v + (kB - 1) * 32 < s1; v += kB * 32) {
+            Vec<InT> x[kB];
+#pragma unroll
+            for (int k = 0; k < kB; ++k)
+                x[k].q = __ldg(rv + v + k * 32);
+            batch(x);
+        }
+        if (kB > 1 && v < s1) {
+            Vec<InT> x[kB];
+#pragma unroll
+            for (int k = 0; k < kB; ++k)
+                x[k].q = v + k * 32 < s1 ? __ldg(rv + v + k * 32)
+                                         : make_uint4(Vec<InT>::kNone, Vec<InT>::kNone,
+                                                      Vec<InT>::kNone, Vec<InT>::kNone);
+            batch(x);
+        }
+        if (end >= 0) {
+            zend = to_f32(row[end]);
+            q[0] = max_nan(q[0], zend);
+            one(zend);
+        }
+    }
+    // The CTA's bound for r of its entries: put() before a barrier, get() after it.
+    __device__ __forceinline__ static bool few(int r) { return r <= 2 * W; }
+    __device__ __forceinline__ void bound_put(PassShared<NT> &sh, int r) const
+    {
+        // r <= 2 W: the CTA's is taken among its warps' four largest; above, it is the least
+        // of the warps' own ceil(r / W)-th largest
+        if (few(r)) {
+            warp_top(q, sh.bound + kTop * (threadIdx.x >> 5));
+        } else {
+            const float b = warp_bound(q, (r + W - 1) / W);
+            if ((threadIdx.x & 31) == 0)
+                sh.bound[threadIdx.x >> 5] = b;
+        }
+    }
+    __device__ __forceinline__ static float bound_get(const PassShared<NT> &sh, int r)
+    {
+        if (few(r))
+            return nth_of(sh.bound, kTop * W, r);
+        float b = sh.bound[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+            b = fminf(b, sh.bound[w]);
+        return b;
+    }
+    // This CTA's candidates, in no order: all its entries at `bound` or above, but -inf.
+    // Returns their number, above cap if they do not fit (or the batches to read do not).
+    __device__ int collect(PassShared<NT> &sh, float bound, mass_t *list, int *items, int cap)
+    {
+        const int tid = threadIdx.x;
+        for (int b = 0; b < nb; ++b) {
+            const float x = bmax[b * NT + tid];
+            if (x >= bound && x != -INFINITY) {
+                const int at = atomicAdd(&sh.items, 1);
+                if (at < cap)
+                    items[at] = (tid >> 5) << 24 | (s0 + b * kB * 32 + (tid & 31));
+            }
+        }
+        auto offer = [&](float z, int j) {
+            if (z >= bound && z != -INFINITY) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < cap)
+                    list[at] = order_pair(order_key(z), (uint32_t)j);
+            }
+        };
+        if (end >= 0)
+            offer(zend, end);
+        __syncthreads();
+        // one vector of an item a thread: neighbouring lanes read an item's vectors, which lie
+        // 512 bytes apart
+        const int m = min(sh.items, cap);
+        for (int i = tid; i < m * kB; i += NT) {
+            const int it = items[i / kB], v = (it & 0xffffff) + (i % kB) * 32;
+            if (v >= seg((it >> 24) + 1))
+                continue;
+            Vec<InT> x;
+            x.q = __ldg(rv + v);
+#pragma unroll
+            for (int k = 0; k < EV; ++k)
+                offer(x.entry(k), head + v * EV + k);
+        }
+        __syncthreads();
+        return sh.items > cap ? cap + 1 : sh.n;
+    }
+};
+
+// The lists of a row's CTAs (the same `list` in each, n entries of it) together, into `all` of
+// the first CTA, which gets their number (above cap: they do not fit).  With barriers of the
+// cluster; no CTA goes on before its list is read.
+template <int NT>
+__device__ int gather_lists(PassShared<NT> &sh, unsigned rank, unsigned cs, mass_t *list, int n,
+                            mass_t *all, int cap)
+{
+    if (threadIdx.x == 0)
+        sh.n = n;
+    cluster_sync_data();
+    if (rank == 0) {
+        const cg::cluster_group cluster = cg::this_cluster();
+        if (threadIdx.x < cs)
+            sh.count[threadIdx.x] = *cluster.map_shared_rank(&sh.n, (int)threadIdx.x);
+        __syncthreads();
+        n = 0;
+        for (unsigned c = 0; c < cs; ++c) {
+            const int k = sh.count[c];
+            if (n + k <= cap && k <= cap) {
+                const mass_t *from = cluster.map_shared_rank(list, (int)c);
+                for (int i = threadIdx.x; i < k; i += NT)
+                    all[n + i] = from[i];
+                n += k;
+            } else {
+                n = cap + 1;
+            }
+        }
+    }
+    cluster_sync_data();
+    return n;
+}
+
+// This CTA's numbers to every CTA of the row.
+template <int NT>
+__device__ __forceinline__ void exchange(PassShared<NT> &sh, unsigned rank, unsigned cs, float m,
+                                         float bound, float s, float raw)
+{
+    cluster_sync_data();  // every CTA of the row has started
+    if (threadIdx.x < cs) {
+        float *to = cg::this_cluster().map_shared_rank(&sh.part[rank][0], (int)threadIdx.x);
+        to[0] = m;
+        to[1] = bound;
+        to[2] = s;
+        to[3] = raw;
+    }
+    cluster_sync_data();
+}
+
+// CTAs a row and the vectors that the plan's CTAs have at most.  As for the forward kernel, a
+// row is split only while the CTAs stay within 608 and keep 512 vectors each.
+struct PassPlan {
+    int cs, nt, kb;
+    size_t maxima;  // bytes of the batches' maxima
+};
+inline PassPlan pass_plan(int64_t T, int64_t V, int in_bytes)
+{
+    const int64_t nvec = V * in_bytes / 16;
+    PassPlan p{1, nvec <= 512 ? 64 : 256, 4, 0};
+    while (p.cs < kMaxCluster && T * p.cs * 2 <= 608 && nvec / (2 * p.cs) >= 512)
+        p.cs *= 2;
+    while (p.cs < kMaxCluster && nvec / p.cs > 65536)  // the maxima fit shared memory
+        p.cs *= 2;
+    if (nvec <= 4096 * p.cs)
+        p.kb = 1;
+    // a warp's share of a CTA's share, each rounded up
+    const int64_t cta = (nvec + p.cs - 1) / p.cs, warp = (cta + p.nt / 32 - 1) / (p.nt / 32);
+    p.maxima = (size_t)((warp + 32 * p.kb - 1) / (32 * p.kb)) * p.nt * sizeof(float);
+    return p;
+}
+
+}  // namespace
+}  // namespace cis

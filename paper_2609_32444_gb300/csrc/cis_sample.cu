@@ -7,11 +7,24 @@
 //   top_p   of those, the smallest prefix whose mass is at least top_p of theirs;
 //   min_p   of those, the entries with s_j >= s_max + log(min_p).
 // The sample is the first entry, by index, whose running kept mass is above u times the kept
-// mass.  Every decision is taken on masses in whole numbers (cis_select.cuh).
+// mass.
+//
+// The row is read once (cis_rowpass.cuh), for its maximum and the sums of its exponentials at
+// tau and at 1.  What follows depends on the row:
+//   nothing cut off   the CTA, the warp and then, with that warp's stretch read again by the
+//                     whole CTA, the thread in whose part the running mass passes u Z;
+//   else              the row's candidates, sorted by the first CTA, with masses in whole
+//                     numbers (cis_select.cuh).
+// Masses of fp32 exponentials decide only where their error cannot matter: each is off by
+// less than 2^-20 (the exponential 2^-22, the rounding of an exponent of up to 16 and of
+// kappa), and the sums' roundings together by less than 2^-19, so that a running mass within
+// 2^-18 Z of its goal is left open.  Rows left open, and those with more candidates than fit
+// or a kept set that reaches beyond them, are left to the exact kernel that follows, which
+// takes every decision on whole numbers.
 #include <math.h>
 
 #include "cis_nvtx.h"
-#include "cis_select.cuh"
+#include "cis_rowpass.cuh"
 
 namespace cis {
 namespace {
@@ -43,15 +56,465 @@ __device__ __forceinline__ void write_row(const SampleArgs &a, int64_t t, int32_
     if (a.lps_out) a.lps_out[t] = lps;
 }
 
+constexpr int32_t kTodo = -2;  // as a row's id: left to the exact kernel
+constexpr float kOpen = 0x1p-18f;
+constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
+constexpr int kAim = 256;      // candidates aimed at where top_k does not say
+
+// Inclusive sums over the CTA's threads, in `scan`; with barriers.
+template <int NT, typename T> __device__ void block_scan(T v, T *scan, T *warps)
+{
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T x = __shfl_up_sync(0xffffffffu, v, o);
+        v += lane >= o ? x : T(0);
+    }
+    if (lane == 31)
+        warps[w] = v;
+    __syncthreads();
+    T before = 0;
+    for (int i = 0; i < w; ++i)
+        before += warps[i];
+    scan[threadIdx.x] = before + v;
+    __syncthreads();
+}
+
+template <int NT> struct SampleShared {
+    PassShared<NT> pass;
+    float scan[NT];
+    float warps[NT / 32];
+    mass_t warps64[NT / 32];
+    uint32_t low;   // min_p's lowest key
+    int kept;
+    int found;      // place of the sampled candidate
+};
+
+// The log-probabilities of z: (z - M) / tau - log of the mass it is drawn from, and at 1.
+__device__ __forceinline__ float log_share(float z, float M, const Scale &sc, float mass)
+{
+    float l, e;
+    const float x = scaled_diff(z, M, sc, l), ls = logf(mass);
+    const float u = two_sum(x, -ls, e);
+    return u + (e + l - log_residual(mass, ls));
+}
+
+// A row with nothing cut off, in the CTA that has its goal g: the running mass before the CTA
+// is `base`, the warps' masses red[w].s * unit.  True and the index in the thread that has it.
+template <typename InT, int NT, int kB>
+__device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &ps, float base,
+                              float unit, float g, float M, float Z, const Scale &sc,
+                              unsigned rank, unsigned cs, int &index, float &zi)
+{
+    constexpr int W = NT / 32, EV = Vec<InT>::kN;
+    const int tid = threadIdx.x;
+    int w = 0;
+    float run = base;
+    for (; w < W - 1; ++w) {
+        const float next = run + sh.pass.red[w].s * unit;
+        if (next > g)
+            break;
+        run = next;
+    }
+    const int s0 = ps.seg(w), n = ps.seg(w + 1) - s0;
+    const int per = (n + NT - 1) / NT, a0 = s0 + min(n, tid * per), a1 = s0 + min(n, tid * per + per);
+    // entries [j0, j1), with the row's ragged ends at the first and the last thread
+    int j0 = ps.head + a0 * EV, j1 = ps.head + a1 * EV;
+    if (rank == 0 && w == 0 && tid == 0)
+        j0 = 0;
+    if (rank == cs - 1 && w == W - 1 && tid == NT - 1)
+        j1 = ps.V;
+    auto weight = [&](float z) { return ex2_ftz((z - M) * sc.kappa); };
+    float sum = 0.0f;
+    for (int j = j0; j < ps.head + a0 * EV; ++j)
+        sum += weight(to_f32(ps.row[j]));
+    for (int v = a0; v < a1; ++v) {
+        Vec<InT> x;
+        x.q = __ldg(ps.rv + v);
+        float p = 0.0f;
+#pragma unroll
+        for (int k = 0; k < EV; ++k)
+            p += weight(x.entry(k));
+        sum += p;
+    }
+    for (int j = ps.head + a1 * EV; j < j1; ++j)
+        sum += weight(to_f32(ps.row[j]));
+    block_scan<NT>(sum, sh.scan, sh.warps);
+    const float lo = run + (tid ? sh.scan[tid - 1] : 0.0f), hi = run + sh.scan[tid];
+    if (!(lo <= g && g < hi))
+        return false;
+    float part = 0.0f;
+    for (int j = j0; j < j1; ++j) {
+        const float z = to_f32(ps.row[j]), x = weight(z), next = part + x;
+        if (lo + next > g && x > 0.0f) {
+            const float open = kOpen * Z;
+            // before the row's first mass there is nothing to be off
+            const bool sure = (lo + next) - g > open &&
+                              (g - (lo + part) > open || (lo == 0.0f && part == 0.0f));
+            index = j;
+            zi = z;
+            return sure;
+        }
+        part = next;
+    }
+    return false;
+}
+
+// A row with something cut off, in its first CTA: n candidates in `list`, sorted.  whole: they
+// are all the row's finite entries.  above: they are all its entries from min_p's key on.
+// Returns the sampled candidate's place, -1 (left open), or -2 - m for m kept ones that are
+// yet to be put in order of their index; the kept mass; in `mass` the running masses.
+template <int NT>
+__device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t *list, int n,
+                             mass_t *mass, int V, float M, float Z, bool whole, bool above,
+                             mass_t &kept_mass)
+{
+    const int tid = threadIdx.x;
+    const Scale &sc = rs.sc;
+    if (tid == 0) {
+        sh.kept = n;
+        sh.found = -1;
+    }
+    // running masses of the order: each thread has a stretch
+    const int per = (n + NT - 1) / NT, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+    mass_t sum = 0;
+    for (int i = i0; i < i1; ++i) {
+        const mass_t m = fixed_mass(key_value((uint32_t)(list[i] >> 32)), M, sc);
+        mass[i] = m;
+        sum += m;
+    }
+    mass_t run = sum;
+    const int lane = tid & 31, w = tid >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const mass_t x = __shfl_up_sync(0xffffffffu, run, o);
+        run += lane >= o ? x : 0;
+    }
+    __syncthreads();
+    if (lane == 31)
+        sh.warps64[w] = run;
+    __syncthreads();
+    run -= sum;
+    for (int i = 0; i < w; ++i)
+        run += sh.warps64[i];
+    for (int i = i0; i < i1; ++i) {
+        run += mass[i];
+        mass[i] = run;  // inclusive
+    }
+    __syncthreads();
+    int m = n;
+    bool open = false, exact = whole;
+    if (rs.top_k > 0 && rs.top_k < V) {
+        // (a list that ends before top_k entries may yet do, if top_p or min_p ends sooner)
+        exact = exact || rs.top_k <= n;
+        m = min(n, rs.top_k);
+        open = !exact;
+    } else {
+        open = !whole;
+    }
+    const bool cut = !open;      // the prefix so far is m entries, known
+    if (rs.top_p < 1.0f) {
+        // the first place whose running mass reaches the goal
+        double goal, slack = 0.0;
+        if (cut) {
+            goal = ceil((double)rs.top_p * (double)mass[m - 1]);
+        } else if (rs.top_k > 0 && rs.top_k < V) {
+            return -1;  // their mass is not known
+        } else {
+            const double unit = (double)(1ull << kMassBits);
+            goal = (double)rs.top_p * (double)Z * unit;
+            slack = (double)kOpen * (double)Z * unit;
+        }
+        for (int i = tid; i < m; i += NT) {
+            const double c = (double)mass[i], b = i ? (double)mass[i - 1] : 0.0;
+            if (cut ? (mass[i] >= (mass_t)goal && (i == 0 || mass[i - 1] < (mass_t)goal))
+                    : (c >= goal && b < goal)) {
+                // not cut: certain only where both sides are away from the goal
+                const bool sure = cut || (c - goal > slack && (goal - b > slack || i == 0));
+                sh.kept = sure ? i + 1 : -1;
+            }
+        }
+        __syncthreads();
+        const int k = sh.kept;
+        if (k < 0)
+            return -1;
+        if (cut || k < n || (double)mass[n - 1] >= goal) {
+            m = k;
+            open = false;
+        } else if (!(goal - (double)mass[n - 1] > slack)) {
+            return -1;
+        }  // else the goal lies beyond the list
+        __syncthreads();
+    }
+    if (rs.min_p > 0.0f) {
+        for (int i = tid; i < m; i += NT) {
+            const bool in = (uint32_t)(list[i] >> 32) >= sh.low;
+            const bool next = i + 1 < m && (uint32_t)(list[i + 1] >> 32) >= sh.low;
+            if (in && !next)
+                sh.kept = i + 1;
+        }
+        __syncthreads();
+        const int k = sh.kept;
+        if (k < m || above) {  // the entries that min_p keeps are all here
+            m = min(m, k);
+            open = false;
+        }
+    }
+    if (open)
+        return -1;
+    kept_mass = mass[m - 1];
+    const mass_t t = min((mass_t)((double)rs.u * (double)kept_mass), kept_mass - 1);
+    if (m == 1)
+        return 0;
+    // running masses by index: for each kept entry those with a lower index
+    if (m <= 64) {
+        if (tid < m) {
+            const uint32_t me = (uint32_t)list[tid];  // larger: a lower index
+            mass_t c = 0, own = 0;
+            for (int i = 0; i < m; ++i) {
+                const mass_t x = mass[i] - (i ? mass[i - 1] : 0);
+                c += (uint32_t)list[i] > me ? x : 0;
+                own = i == tid ? x : own;
+            }
+            if (c <= t && c + own > t)
+                sh.found = tid;
+        }
+        __syncthreads();
+        return sh.found;
+    }
+    return -2 - m;
+}
+
+template <typename InT, int NT, int kB>
+__global__ void __launch_bounds__(NT)
+    cis_sample_kernel(const __grid_constant__ SampleArgs a, unsigned cs, int cap)
+{
+    constexpr int W = NT / 32;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
+    __shared__ SampleShared<NT> sh;
+    mass_t *list = reinterpret_cast<mass_t *>(dyn_smem);
+    mass_t *room = list + cap;  // the candidates of all CTAs
+    int *items = reinterpret_cast<int *>(room + cap);
+    float *bmax = reinterpret_cast<float *>(items + cap);
+    const int64_t t = blockIdx.x / cs;
+    const unsigned rank = blockIdx.x - (unsigned)t * cs;
+    const int tid = threadIdx.x;
+    if (tid == 0)
+        allow_next_grid();
+    if (a.mask && a.mask[t] == 0) {  // the same branch in every CTA of the row
+        if (rank == 0 && tid == 0)
+            write_row(a, t, -1, 0.0f, 0.0f);
+        return;
+    }
+    const RowSettings rs = row_settings(a, t);
+    if (!rs.ok) {
+        if (rank == 0 && tid == 0) {
+            write_row(a, t, -1, NAN, NAN);
+            set_status(a.status, kStatusBadInput);
+        }
+        return;
+    }
+    const bool by_k = rs.top_k > 0 && rs.top_k < a.V;
+    const bool cut = rs.greedy || by_k || rs.top_p < 1.0f || rs.min_p > 0.0f;
+    const bool two = a.lp_out != nullptr && rs.sc.hi != 1.0f;
+    if (tid == 0)
+        sh.pass.items = sh.pass.n = 0;
+    RowPass<InT, NT, kB> ps(reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, rank, cs,
+                            bmax);
+    ExpAcc<false, true> acc;
+    acc.k = rs.sc.kappa;
+    acc.h = rs.sc.huge;
+    ExpAcc<false> raw;
+    auto entry = [&](auto &e, float z) {
+        e.raise(z);
+        if (e.m != -INFINITY)
+            e.add_entry(z);
+    };
+    if (two)
+        ps.stream(
+            cut,
+            [&](const Vec<InT> (&x)[kB], float mx) {
+                take<false, kB>(acc, x, mx);
+                take<false, kB>(raw, x, mx);
+            },
+            [&](float z) {
+                entry(acc, z);
+                entry(raw, z);
+            });
+    else
+        ps.stream(
+            cut, [&](const Vec<InT> (&x)[kB], float mx) { take<false, kB>(acc, x, mx); },
+            [&](float z) { entry(acc, z); });
+    const int aim = rs.greedy ? 1 : by_k ? min(rs.top_k, kAim) : kAim;
+    const int r = (aim + (int)cs - 1) / (int)cs;
+    if (cut)
+        ps.bound_put(sh.pass, r);
+    MaxSumU o = block_exp<NT>(acc, sh.pass.red);  // (its barriers)
+    float S1 = two ? block_exp<NT>(raw, sh.pass.red2).s : o.s;
+    float bound = cut ? ps.bound_get(sh.pass, r) : -INFINITY;
+    float sum_w = 0.0f;  // the warps' sums, in their own unit
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+        sum_w += sh.pass.red[w].s;
+    float unit = o.s / sum_w, base = 0.0f;
+    float M = o.m, Z = o.s, goal = 0.0f;
+    unsigned has = 0;  // the CTA with the goal
+    if (cs > 1) {
+        exchange(sh.pass, rank, cs, o.m, bound, o.s, S1);
+        const auto &part = sh.pass.part;
+        for (unsigned c = 0; c < cs; ++c) {
+            M = fmaxf(M, part[c][0]);
+            bound = fminf(bound, part[c][1]);
+        }
+        Z = S1 = 0.0f;
+        for (unsigned c = 0; c < cs; ++c) {  // in rank order
+            const float d = part[c][0] - M;
+            Z += part[c][2] * exp2f(d * rs.sc.kappa);
+            S1 += part[c][3] * exp2f(d * kLog2e);
+        }
+        goal = rs.u * Z;
+        for (; has < cs - 1; ++has) {
+            const float next = base + part[has][2] * exp2f((part[has][0] - M) * rs.sc.kappa);
+            if (next > goal)
+                break;
+            base = next;
+        }
+        unit *= exp2f((o.m - M) * rs.sc.kappa);
+    }
+    goal = rs.u * Z;
+    if (!(Z > 0.0f && Z < INFINITY) || !(fabsf(M) < INFINITY)) {  // as every CTA finds
+        if (rank == 0 && tid == 0) {
+            write_row(a, t, -1, NAN, NAN);
+            set_status(a.status, kStatusBadInput);
+        }
+        return;
+    }
+    const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
+    if (!cut) {
+        if (rank != has)
+            return;
+        int j;
+        float z;
+        __shared__ int done;
+        if (tid == 0)
+            done = 0;
+        __syncthreads();
+        if (draw_by_index<InT, NT, kB>(sh, ps, base, unit, goal, M, Z, rs.sc, rank, cs, j, z)) {
+            write_row(a, t, j, log_share(z, M, one, S1), log_share(z, M, rs.sc, Z));
+            done = 1;
+        }
+        __syncthreads();
+        if (tid == 0 && !done)
+            a.ids_out[t] = kTodo;
+        return;
+    }
+
+    // The candidates; what min_p leaves out is none.
+    bool above = false;
+    if (rs.min_p > 0.0f && !rs.greedy) {
+        if (tid == 0)
+            sh.low = min_p_key(M, rs.tau, rs.min_p);
+        __syncthreads();
+        const float least = key_value(sh.low);
+        above = bound <= least;
+        if (rs.top_p >= 1.0f && (above || !by_k)) {
+            // (top_p needs the mass of those that min_p leaves out); with nothing but min_p
+            // the kept set is all of them, however many
+            bound = least;
+            above = true;
+        }
+    }
+    int n = ps.collect(sh.pass, bound, list, items, cap);
+    if (cs > 1) {
+        n = gather_lists<NT>(sh.pass, rank, cs, list, n, room, cap);
+        if (rank != 0)
+            return;
+        mass_t *swap = list;
+        list = room;
+        room = swap;
+    }
+    if (n > cap) {
+        if (tid == 0)
+            a.ids_out[t] = kTodo;
+        return;
+    }
+    sort_list<NT>(list, n);
+    int at = 0;
+    mass_t kept = (mass_t)1 << kMassBits;
+    if (!rs.greedy)
+        at = draw_by_order<NT>(sh, rs, list, n, room, (int)a.V, M, Z, bound == -INFINITY, above,
+                               kept);
+    mass_t pick = at >= 0 ? list[at] : 0;
+    if (at < -2) {
+        // more than 64 kept: put in order of the index, with their places
+        const int m = -2 - at;
+        const mass_t t0 = min((mass_t)((double)rs.u * (double)kept), kept - 1);
+        for (int i = tid; i < m; i += NT)
+            list[i] = (list[i] << 32) | (uint32_t)i;  // (the inverted index: larger is lower)
+        __syncthreads();
+        sort_list<NT>(list, m);
+        const int per = (m + NT - 1) / NT, i0 = min(m, tid * per), i1 = min(m, i0 + per);
+        auto own = [&](int i) {
+            const uint32_t p = (uint32_t)list[i];
+            return room[p] - (p ? room[p - 1] : 0);
+        };
+        mass_t sum = 0;
+        for (int i = i0; i < i1; ++i)
+            sum += own(i);
+        mass_t run = sum;
+        const int lane = tid & 31, w = tid >> 5;
+#pragma unroll
+        for (int o2 = 1; o2 < 32; o2 <<= 1) {
+            const mass_t x = __shfl_up_sync(0xffffffffu, run, o2);
+            run += lane >= o2 ? x : 0;
+        }
+        if (lane == 31)
+            sh.warps64[w] = run;
+        __syncthreads();
+        run -= sum;
+        for (int i = 0; i < w; ++i)
+            run += sh.warps64[i];
+        for (int i = i0; i < i1; ++i) {
+            const mass_t next = run + own(i);
+            if (run <= t0 && next > t0)
+                sh.found = i;
+            run = next;
+        }
+        __syncthreads();
+        at = sh.found;
+        if (at >= 0) {
+            const uint32_t inv = (uint32_t)(list[at] >> 32);
+            const int j = (int)(0xffffffffu - inv);
+            pick = order_pair(order_key(to_f32(ps.row[j])), (uint32_t)j);
+        }
+    }
+    if (tid == 0) {
+        if (at < 0) {
+            a.ids_out[t] = kTodo;
+        } else {
+            const float z = key_value((uint32_t)(pick >> 32));
+            write_row(a, t, (int32_t)(0xffffffffu - (uint32_t)pick), log_share(z, M, one, S1),
+                      rs.greedy ? 0.0f : log_share(z, M, rs.sc, (float)mass_value(kept)));
+        }
+    }
+}
+
 // Any row, exactly: a cluster per row reads it from memory (L2 after the first time) once
 // for each step.
 template <typename InT>
-__global__ void __launch_bounds__(kSelThreads) cis_sample_exact_kernel(const SampleArgs a)
+__global__ void __launch_bounds__(kSelThreads)
+    cis_sample_exact_kernel(const __grid_constant__ SampleArgs a, bool every)
 {
     __shared__ SelectShared<kSelThreads> sh;
-    const unsigned group = blockIdx.x / kSelCluster, groups = gridDim.x / kSelCluster;
     int turn = 0;
-    for (int64_t t = group; t < a.T; t += groups) {
+    if (threadIdx.x == 0)
+        allow_next_grid();
+    grid_wait();
+    RowsLeft<kSelThreads> rows(sh, a.T, gridDim.x / kSelCluster, blockIdx.x / kSelCluster);
+    for (;;) {
+        const int64_t t = rows.next([&](int64_t i) { return every || a.ids_out[i] == kTodo; });
+        if (t < 0)
+            break;
         RowSelect<InT, kSelThreads> rs(sh, reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V,
                                        turn);
         const bool first = rs.rank == 0 && threadIdx.x == 0;
@@ -133,21 +596,60 @@ __global__ void __launch_bounds__(kSelThreads) cis_sample_exact_kernel(const Sam
     cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
 
-template <typename InT> cudaError_t launch_exact(const SampleArgs &a, cudaStream_t s)
+template <typename InT, int NT, int kB>
+cudaError_t launch_fast(const SampleArgs &a, const PassPlan &p, cudaStream_t s)
+{
+    auto kern = cis_sample_kernel<InT, NT, kB>;
+    const size_t smem = kCap * (2 * sizeof(mass_t) + sizeof(int)) + p.maxima;
+    const cudaError_t e = cudaFuncSetAttribute(
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.T * p.cs), 1, 1);
+    cfg.blockDim = dim3(NT, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.cs;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.cs > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, a, (unsigned)p.cs, kCap);
+}
+
+// The exact kernel: every row, or those that the fast one before it left.
+template <typename InT>
+cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
 {
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 76 ? a.T : 76;
+    const int64_t groups = a.T < 38 ? a.T : 38;
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = kSelCluster;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, cis_sample_exact_kernel<InT>, a);
+    cfg.numAttrs = every ? 1 : 2;
+    return cudaLaunchKernelEx(&cfg, cis_sample_exact_kernel<InT>, a, every);
+}
+
+template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStream_t s)
+{
+    const PassPlan p = pass_plan(a.T, a.V, (int)sizeof(InT));
+    if (a.T * p.cs > 0x7fffffffLL)
+        return launch_exact<InT>(a, true, s);
+    const cudaError_t e = p.nt == 64  ? launch_fast<InT, 64, 1>(a, p, s)
+                          : p.kb == 1 ? launch_fast<InT, 256, 1>(a, p, s)
+                                      : launch_fast<InT, 256, 4>(a, p, s);
+    return e != cudaSuccess ? e : launch_exact<InT>(a, false, s);
 }
 
 }  // namespace
@@ -186,7 +688,7 @@ extern "C" CIS_API cis_status_t cis_sample_tokens(
     a.lps_out = lp_sampled_out;
     a.status = dev_status;
     const cudaError_t e = dtype == CIS_BF16
-                              ? launch_exact<__nv_bfloat16>(a, (cudaStream_t)stream)
-                              : launch_exact<float>(a, (cudaStream_t)stream);
+                              ? launch_sample<__nv_bfloat16>(a, (cudaStream_t)stream)
+                              : launch_sample<float>(a, (cudaStream_t)stream);
     return e == cudaSuccess ? CIS_OK : CIS_ERR_CUDA;
 }

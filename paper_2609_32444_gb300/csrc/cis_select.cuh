@@ -8,6 +8,7 @@
 // split and every call come to the same entry, and 2^63 holds a row of 2^20 maxima.
 #pragma once
 
+#include "cis_expacc.cuh"
 #include "cis_slice.cuh"
 
 namespace cis {
@@ -33,14 +34,14 @@ __device__ __forceinline__ mass_t order_pair(uint32_t key, uint32_t index)
     return ((mass_t)key << 32) | (0xffffffffu - index);
 }
 
-// 1 / tau of a row's own temperature.
+// 1 / tau of a row's own temperature, as a pair (its residual from an FMA), and log2e / tau.
 __device__ __forceinline__ Scale device_scale(float tau)
 {
-    const double v = 1.0 / (double)tau;
     Scale s;
-    s.hi = (float)v;
-    s.lo = (float)(v - (double)s.hi);
-    s.kappa = (float)(1.4426950408889634074 * v);
+    s.hi = 1.0f / tau;
+    s.lo = s.hi * fmaf(-s.hi, tau, 1.0f);
+    constexpr float log2e_lo = (float)(1.4426950408889634074 - (double)kLog2e);
+    s.kappa = fmaf(kLog2e, s.hi, fmaf(kLog2e, s.lo, log2e_lo * s.hi));
     s.huge = kHugeLogit * tau;
     return s;
 }
@@ -129,6 +130,90 @@ __device__ inline uint32_t min_p_key(float M, float tau, float min_p)
     for (int i = 0; i < 4 && in(nextafterf(z, -INFINITY)); ++i)
         z = nextafterf(z, -INFINITY);
     return order_key(z > M ? M : z);
+}
+
+// ------------------------------------------------------------------ candidates
+// Sort n pairs in descending order (bitonic, padded with 0 up to a power of two); all threads.
+template <int NT> __device__ void sort_list(mass_t *list, int n)
+{
+    int size = 2;
+    while (size < n)
+        size *= 2;
+    for (int i = threadIdx.x; i < size; i += NT)
+        if (i >= n)
+            list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int i = threadIdx.x; i < size / 2; i += NT) {
+                const int lo = 2 * j * (i / j) + i % j, hi = lo + j;
+                const mass_t x = list[lo], y = list[hi];
+                if ((x < y) == ((lo & k) == 0)) {
+                    list[lo] = y;
+                    list[hi] = x;
+                }
+            }
+            __syncthreads();
+        }
+}
+
+// A value that at least r (1 .. 128) of the warp's 128 maxima are not below: the r-th
+// largest, rounded down to 16 bits.  Bit by bit from the first in which the warp's keys
+// differ.
+__device__ __forceinline__ float warp_bound(const float (&m)[4], int r)
+{
+    uint32_t k[4], lo = 0xffffu, hi = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        k[i] = order_key(m[i]) >> 16;
+        lo = min(lo, k[i]);
+        hi = max(hi, k[i]);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    const int bits = 32 - __clz(lo ^ hi);
+    uint32_t v = (hi >> bits) << bits;
+    for (int b = bits - 1; b >= 0; --b) {
+        const uint32_t mid = v | (1u << b);
+        const uint32_t n = (k[0] >= mid) + (k[1] >= mid) + (k[2] >= mid) + (k[3] >= mid);
+        if (__reduce_add_sync(0xffffffffu, n) >= (uint32_t)r)
+            v = mid;
+    }
+    return v <= (order_key(-INFINITY) >> 16) ? -INFINITY : key_value(v << 16);
+}
+
+// The warp's kTop largest maxima, rounded down to 16 bits, into `out`.
+constexpr int kTop = 4;
+__device__ __forceinline__ void warp_top(const float (&m)[4], float *out)
+{
+    uint32_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)  // made different by the lane and place: one goes at a time
+        k[i] = (order_key(m[i]) & 0xffff0000u) | ((threadIdx.x & 31) << 2) | i;
+#pragma unroll
+    for (int n = 0; n < kTop; ++n) {
+        const uint32_t best = __reduce_max_sync(0xffffffffu, max(max(k[0], k[1]), max(k[2], k[3])));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            k[i] = k[i] == best ? 0u : k[i];
+        const uint32_t v = best >> 16;
+        if ((threadIdx.x & 31) == 0)
+            out[n] = v <= (order_key(-INFINITY) >> 16) ? -INFINITY : key_value(v << 16);
+    }
+}
+// The r-th largest (1 .. n) of n <= 32 values; every lane gets it.
+__device__ __forceinline__ float nth_of(const float *v, int n, int r)
+{
+    const int lane = threadIdx.x & 31;
+    const float x = lane < n ? v[lane] : -INFINITY;
+    int before = 0;  // values ahead of this one
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const float y = __shfl_sync(0xffffffffu, x, i);
+        before += y > x || (y == x && i < lane);
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, before == r - 1);
+    return __shfl_sync(0xffffffffu, x, who ? __ffs(who) - 1 : 0);
 }
 
 // ------------------------------------------------------------------ clusters
