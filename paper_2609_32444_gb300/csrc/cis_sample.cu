@@ -29,9 +29,6 @@
 namespace cis {
 namespace {
 
-constexpr int kSelThreads = 512;
-constexpr int kSelCluster = 8;
-
 __device__ inline RowSettings row_settings(const SampleArgs &a, int64_t t)
 {
     RowSettings r;
@@ -499,13 +496,13 @@ __global__ void __launch_bounds__(NT)
     }
 }
 
-// Any row, exactly: a cluster per row reads it from memory (L2 after the first time) once
-// for each step.
+// Any row, exactly: a cluster per row.
 template <typename InT>
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelThreads, 3)
     cis_sample_exact_kernel(const __grid_constant__ SampleArgs a, bool every)
 {
-    __shared__ SelectShared<kSelThreads> sh;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
+    SelectShared<kSelThreads> &sh = *reinterpret_cast<SelectShared<kSelThreads> *>(dyn_smem);
     int turn = 0;
     if (threadIdx.x == 0)
         allow_next_grid();
@@ -525,7 +522,8 @@ __global__ void __launch_bounds__(kSelThreads)
         }
         const RowSettings rset = row_settings(a, t);
         bool bad;
-        const uint32_t mk = rs.max_key(bad);
+        uint32_t least;
+        const uint32_t mk = rs.max_key(least, bad);
         if (bad || !rset.ok) {  // as every CTA of the cluster finds
             if (first) {
                 write_row(a, t, -1, NAN, NAN);
@@ -533,17 +531,32 @@ __global__ void __launch_bounds__(kSelThreads)
             }
             continue;
         }
-        const float M = key_value(mk);
+        const float M = key_value(mk), bottom = key_value(least);
         const Scale &sc = rset.sc;
+        const bool two = a.lp_out != nullptr && sc.hi != 1.0f;
         Kept kept{0, 0};
         mass_t above, equal;
         const int64_t k = rset.greedy ? 1 : rset.top_k;
         if (k > 0 && k < a.V) {
-            kept.key = rs.select((mass_t)k, [](float, uint32_t) { return (mass_t)1; }, above, equal);
+            kept.key = rs.select((mass_t)k, (float)k, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
+                                 [](float, uint32_t) { return 1.0f; },
+                                 [](float, uint32_t) { return (mass_t)1; }, above, equal);
             kept.ties = (mass_t)k - above;
         }
         mass_t gt, eq, gt0, eq0;
-        rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0);
+        float raw = 0.0f;
+        rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0, two ? &raw : nullptr);
+        // (the row's mass at temperature 1: fp32 exponentials, added up as whole numbers)
+        mass_t S1 = 0, none = 0, x, y;
+        if (two) {
+            S1 = (mass_t)((double)raw * (double)(1ull << kMassBits));
+            rs.cluster_sum(S1, none, x, y);
+        } else if (kept.key == 0) {
+            S1 = gt;
+        } else if (a.lp_out) {
+            rs.each([&](int64_t, float z) { S1 += fixed_mass(z, M, sc); });
+            rs.cluster_sum(S1, none, x, y);
+        }
         mass_t wkey = kept.ties ? fixed_mass(key_value(kept.key), M, sc) : 0;
         bool moved = false;
         if (rset.top_p < 1.0f && !rset.greedy) {
@@ -551,8 +564,12 @@ __global__ void __launch_bounds__(kSelThreads)
                 (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
             if (target <= gt) {
                 const uint32_t floor_key = kept.key;
+                const float low = M - 32.0f * rset.tau;
                 kept.key = rs.select(
-                    target,
+                    target, (float)mass_value(target), bottom > low ? bottom : low, M,
+                    [&](float z, uint32_t key) {
+                        return key > floor_key ? ex2_ftz((z - M) * sc.kappa) : 0.0f;
+                    },
                     [&](float z, uint32_t key) {
                         return key > floor_key ? fixed_mass(z, M, sc) : (mass_t)0;
                     },
@@ -573,23 +590,15 @@ __global__ void __launch_bounds__(kSelThreads)
             }
         }
         if (moved)
-            rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0);
+            rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0, nullptr);
         const mass_t Z = gt + min(eq, kept.ties) * wkey;
         const mass_t target = (mass_t)((double)rset.u * (double)Z);
         int64_t j = 0;
-        const bool have =
-            rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, M, sc, j);
-        // the row's own log-probability: its mass at temperature 1
-        mass_t raw = 0, none = 0, x, y;
-        const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
-        rs.each([&](int64_t, float z) { raw += fixed_mass(z, M, one); });
-        rs.cluster_sum(raw, none, x, y);
-        if (have && threadIdx.x == 0) {
+        if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, j, M, sc) && threadIdx.x == 0) {
             const float z = to_f32(rs.row[j]);
-            const double d = (double)z - (double)M;
-            write_row(a, t, (int32_t)j, (float)(d - log(mass_value(raw))),
-                      rset.greedy ? 0.0f
-                                  : (float)(d / (double)rset.tau - log(mass_value(Z))));
+            const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
+            write_row(a, t, (int32_t)j, log_share(z, M, one, (float)mass_value(S1)),
+                      rset.greedy ? 0.0f : log_share(z, M, sc, (float)mass_value(Z)));
         }
         __syncthreads();
     }
@@ -624,10 +633,16 @@ cudaError_t launch_fast(const SampleArgs &a, const PassPlan &p, cudaStream_t s)
 template <typename InT>
 cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
 {
+    constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
+    const cudaError_t e = cudaFuncSetAttribute(
+        cis_sample_exact_kernel<InT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess)
+        return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 38 ? a.T : 38;
+    const int64_t groups = a.T < 57 ? a.T : 57;  // three CTAs an SM
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

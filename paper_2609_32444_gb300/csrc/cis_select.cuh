@@ -217,15 +217,26 @@ __device__ __forceinline__ float nth_of(const float *v, int n, int r)
 }
 
 // ------------------------------------------------------------------ clusters
+constexpr int kSelThreads = 256;
+constexpr int kSelCluster = 8;
+constexpr int kBins = 32;
+constexpr int kListMax = 1024;  // entries that a selection may come down to
+
 template <int NT> struct SelectShared {
     mass_t part[2][2];      // this CTA's share of the running sums
     mass_t red[2][NT / 32];
+    mass_t stretch[2][NT / 32];  // the warps' kept mass and ties
     mass_t hist[256];
     mass_t tot[256];
-    uint32_t digit;
+    float bins[2][kBins];
+    uint32_t digit, low_key;
+    float bin_over;
+    int bin;
+    bool edges;
     mass_t above, equal;
-    mass_t got;             // the entry that was found (order_pair)
-    mass_t list[512];       // candidates to sort
+    mass_t got;             // the entry that was found, plus 1
+    mass_t list[kListMax];  // candidates
+    float cols[kBins * NT]; // a selection's bins, a column a thread; then the cluster's list
     int n;
     unsigned left[NT / 32]; // rows left to do, a bit each
 };
@@ -267,13 +278,17 @@ template <int NT> struct RowsLeft {
     }
 };
 
-// One cluster's work on one row; CTA `rank` has the entries [j0, j1).
+// One cluster's work on one row.  CTA `rank` has the entries [j0, j1), and each of its warps a
+// stretch of them; the row is read from memory (L2 after the first time) once for each step.
 template <typename InT, int NT> struct RowSelect {
+    static constexpr int EV = Vec<InT>::kN, W = NT / 32;
+    static_assert(NT == 256, "a histogram's bin a thread");
     SelectShared<NT> &sh;
     cg::cluster_group cl;
     unsigned rank, size;
     const InT *row;
     int64_t V, j0, j1;
+    int head, v0, v1;
     int &buf;  // the exchanges' buffer in turn, across rows
 
     __device__ RowSelect(SelectShared<NT> &s, const InT *r, int64_t V_, int &turn)
@@ -281,27 +296,66 @@ template <typename InT, int NT> struct RowSelect {
     {
         rank = cl.block_rank();
         size = cl.num_blocks();
-        j0 = V * rank / size;
-        j1 = V * (rank + 1) / size;
+        head = row_head(row, (int)V);
+        const int64_t nvec = (V - head) / EV;
+        v0 = (int)(nvec * rank / size);
+        v1 = (int)(nvec * (rank + 1) / size);
+        j0 = rank == 0 ? 0 : head + (int64_t)v0 * EV;
+        j1 = rank == size - 1 ? V : head + (int64_t)v1 * EV;
     }
+    __device__ __forceinline__ int seg(int w) const
+    {
+        return v0 + (int)((int64_t)(v1 - v0) * w / W);
+    }
+    // The entries of warp w's stretch: [first(w), first(w + 1)).
+    __device__ __forceinline__ int64_t first(int w) const
+    {
+        return w == 0 ? j0 : w == W ? j1 : head + (int64_t)seg(w) * EV;
+    }
+    // f(index, entry) for this CTA's entries, each by a lane of its stretch's warp.
     template <typename F> __device__ __forceinline__ void each(F f) const
     {
-#pragma unroll 4
-        for (int64_t j = j0 + threadIdx.x; j < j1; j += NT)
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const uint4 *rv = reinterpret_cast<const uint4 *>(row + head);
+        const int s1 = seg(w + 1);
+        int v = seg(w) + lane;
+        Vec<InT> x, y;
+        if (v < s1)
+            x.q = __ldg(rv + v);
+#pragma unroll 1
+        for (; v < s1; v += 32) {
+            if (v + 32 < s1)
+                y.q = __ldg(rv + v + 32);
+#pragma unroll
+            for (int k = 0; k < EV; ++k)
+                f(head + (int64_t)v * EV + k, x.entry(k));
+            x = y;
+        }
+        int64_t j = -1;  // the ragged ends
+        const int64_t tail = head + (V - head) / EV * EV;
+        if (rank == 0 && w == 0 && lane < head)
+            j = lane;
+        if (rank == size - 1 && w == W - 1 && lane >= 16 && tail + lane - 16 < V)
+            j = tail + lane - 16;
+        if (j >= 0)
             f(j, to_f32(row[j]));
     }
     template <typename T> __device__ __forceinline__ const T *peer(T *p, unsigned r)
     {
         return cl.map_shared_rank(p, (int)r);
     }
-    // Two sums over the CTA; in every thread.
-    __device__ void block_sum(mass_t &a, mass_t &b)
+    __device__ __forceinline__ static void warp_sums(mass_t &a, mass_t &b)
     {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, o);
             b += __shfl_xor_sync(0xffffffffu, b, o);
         }
+    }
+    // Two sums over the CTA; in every thread.
+    __device__ void block_sum(mass_t &a, mass_t &b)
+    {
+        warp_sums(a, b);
         __syncthreads();
         if ((threadIdx.x & 31) == 0) {
             sh.red[0][threadIdx.x >> 5] = a;
@@ -309,7 +363,7 @@ template <typename InT, int NT> struct RowSelect {
         }
         __syncthreads();
         a = b = 0;
-        for (int w = 0; w < NT / 32; ++w) {
+        for (int w = 0; w < W; ++w) {
             a += sh.red[0][w];
             b += sh.red[1][w];
         }
@@ -336,52 +390,228 @@ template <typename InT, int NT> struct RowSelect {
         }
         buf ^= 1;
     }
-    // The row's largest key; bad: NaN, +inf or no finite entry.
-    __device__ uint32_t max_key(bool &bad)
+    // The row's largest key, and its least but that of -inf; bad: NaN, +inf or no finite entry.
+    __device__ uint32_t max_key(uint32_t &least, bool &bad)
     {
-        uint32_t k = 0;
-        mass_t nan = 0;
+        const uint32_t none = order_key(-INFINITY);
+        uint32_t k = 0, l = 0xffffffffu;
         each([&](int64_t, float z) {
-            nan += z != z;
-            k = max(k, order_key(z));
+            // (NaN as the largest)
+            const uint32_t q = z != z ? 0xffffffffu : order_key(z);
+            k = max(k, q);
+            l = q > none ? min(l, q) : l;
         });
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        k = __reduce_max_sync(0xffffffffu, k);
+        l = __reduce_min_sync(0xffffffffu, l);
         __syncthreads();
-        if ((threadIdx.x & 31) == 0)
-            sh.tot[threadIdx.x >> 5] = k;
-        mass_t any = nan;
-        mass_t none = 0;
-        block_sum(any, none);
-        mass_t m = 0;
-        for (int w = 0; w < NT / 32; ++w)
-            m = max(m, sh.tot[w]);
+        if ((threadIdx.x & 31) == 0) {
+            sh.red[0][threadIdx.x >> 5] = k;
+            sh.red[1][threadIdx.x >> 5] = l;
+        }
+        __syncthreads();
+        mass_t a = 0, b = 0xffffffffu;
+        for (int w = 0; w < W; ++w) {
+            a = max(a, sh.red[0][w]);
+            b = min(b, sh.red[1][w]);
+        }
         if (threadIdx.x == 0) {
-            sh.part[buf][0] = m;
-            sh.part[buf][1] = any;
+            sh.part[buf][0] = a;
+            sh.part[buf][1] = b;
         }
         cl.sync();
-        m = any = 0;
         for (unsigned r = 0; r < size; ++r) {
             const mass_t *p = peer(&sh.part[buf][0], r);
-            m = max(m, p[0]);
-            any += p[1];
+            a = max(a, p[0]);
+            b = min(b, p[1]);
         }
         buf ^= 1;
-        bad = any != 0 || m <= order_key(-INFINITY) || m >= order_key(INFINITY);
-        return (uint32_t)m;
+        bad = a <= none || a >= order_key(INFINITY);
+        least = (uint32_t)b;
+        return (uint32_t)a;
     }
     // The key at which the weight of the entries from the largest on reaches `target`
-    // (1 .. the total): returns it, the weight strictly above it and that at it.
-    template <typename W>
-    __device__ uint32_t select(mass_t target, W weight, mass_t &above, mass_t &equal)
+    // (1 .. the total), the weight strictly above it and that at it.  weight(z, key): an
+    // entry's, in whole numbers; approx(z, key): the same in fp32, `goal` the target likewise.
+    //
+    // Two levels of 32 bins, over [low, M] and then over the bin in which the fp32 weights
+    // reach the goal, each thread with a column of its own (no atomics); then one pass adds
+    // up the whole numbers above that bin and lists its entries, which the first CTA sorts.
+    // Where they do not fit, or the bin was not the one, a radix selection does it.
+    template <typename A, typename F>
+    __device__ uint32_t select(mass_t target, float goal, float low, float M, A approx, F weight,
+                               mass_t &above, mass_t &equal)
+    {
+        uint32_t khi = order_key(M), klo = 0;  // the entries with klo < key <= khi
+        float over = 0.0f;
+        bool edges = true;
+        for (int level = 0; level < 4 && edges; ++level) {
+            const float hi = key_value(khi), lo = klo ? key_value(klo) : low;
+            const float inv = (float)kBins / (hi - lo);
+            if (!(hi > lo) || !(inv < INFINITY) || !(inv > 0.0f))
+                break;
+            auto bin = [&](float z) {
+                const float b = (hi - z) * inv;
+                return b < (float)kBins ? (int)b : kBins - 1;
+            };
+            float *col = sh.cols + threadIdx.x;
+            for (int b = 0; b < kBins; ++b)
+                col[b * NT] = 0.0f;
+            each([&](int64_t, float z) {
+                const uint32_t k = order_key(z);
+                if (k <= khi && k > klo)
+                    col[bin(z) * NT] += approx(z, k);
+            });
+            __syncthreads();
+            const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+            for (int b = w; b < kBins; b += W) {
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+                    s += sh.cols[b * NT + lane + 32 * i];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == 0)
+                    sh.bins[buf][b] = s;
+            }
+            cl.sync();
+            if (w == 0) {
+                float s = 0.0f;
+                for (unsigned r = 0; r < size; ++r)
+                    s += peer(&sh.bins[buf][0], r)[lane];
+                float incl = s;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const float y = __shfl_up_sync(0xffffffffu, incl, o);
+                    incl += lane >= o ? y : 0.0f;
+                }
+                const unsigned reach = __ballot_sync(0xffffffffu, over + incl >= goal);
+                const int b = reach ? __ffs(reach) - 1 : kBins - 1;
+                const float before = __shfl_sync(0xffffffffu, incl, b ? b - 1 : 0);
+                if (lane == 0) {
+                    sh.bin = b;
+                    sh.bin_over = over + (b ? before : 0.0f);
+                    // the largest key whose bin is b or beyond, and the same for b + 1
+                    sh.edges = true;
+                    auto edge = [&](int at) {
+                        uint32_t k = order_key(hi - (float)at / inv);
+                        int n = 0;
+                        while (n < 64 && bin(key_value(k)) < at)
+                            --k, ++n;
+                        while (n < 64 && bin(key_value(k + 1)) >= at)
+                            ++k, ++n;
+                        sh.edges = sh.edges && n < 64;
+                        return k;
+                    };
+                    sh.digit = b ? min(edge(b), khi) : khi;
+                    sh.low_key = b < kBins - 1 ? max(edge(b + 1), klo) : klo;
+                }
+            }
+            buf ^= 1;
+            __syncthreads();
+            khi = sh.digit;
+            klo = sh.low_key;
+            over = sh.bin_over;
+            edges = sh.edges && khi > klo;
+            __syncthreads();
+            if (level == 0 || !edges)
+                continue;
+            // whole numbers above the bin, and its entries
+            if (threadIdx.x == 0)
+                sh.n = 0;
+            __syncthreads();
+            mass_t up = 0, n = 0, x, at;
+            each([&](int64_t j, float z) {
+                const uint32_t k = order_key(z);
+                if (k > khi) {
+                    up += weight(z, k);
+                } else if (k > klo && weight(z, k) != 0) {
+                    const int i = atomicAdd(&sh.n, 1);
+                    if (i < kListMax)
+                        sh.list[i] = order_pair(k, (uint32_t)j);
+                }
+            });
+            __syncthreads();
+            n = threadIdx.x == 0 ? (mass_t)sh.n : 0;
+            const int mine = sh.n;
+            cluster_sum(up, n, x, at);
+            if (n > kListMax)
+                continue;  // another level
+            mass_t *all = cl.map_shared_rank(reinterpret_cast<mass_t *>(sh.cols), 0);
+            for (int i = threadIdx.x; i < mine; i += NT)
+                all[at + i] = sh.list[i];
+            cl.sync();
+            if (rank == 0)
+                pick(reinterpret_cast<mass_t *>(sh.cols), (int)n, target, up, weight);
+            cl.sync();
+            const SelectShared<NT> *first = peer(&sh, 0);
+            const mass_t got = first->got;
+            above = first->above;
+            equal = first->equal;
+            cl.sync();
+            if (got)
+                return (uint32_t)(got - 1);
+            break;
+        }
+        return radix(target, weight, above, equal);
+    }
+    // Among n entries, `up` weight before them: got = key + 1 where `target` is reached.
+    template <typename F>
+    __device__ void pick(mass_t *all, int n, mass_t target, mass_t up, F weight)
+    {
+        sort_list<NT>(all, n);
+        const int per = (n + NT - 1) / NT, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+        auto own = [&](int i) {
+            const uint32_t k = (uint32_t)(all[i] >> 32);
+            return weight(key_value(k), k);
+        };
+        mass_t sum = 0;
+        for (int i = i0; i < i1; ++i)
+            sum += own(i);
+        mass_t run = sum;
+        const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const mass_t x = __shfl_up_sync(0xffffffffu, run, o);
+            run += lane >= o ? x : 0;
+        }
+        if (threadIdx.x == 0)
+            sh.got = 0;
+        __syncthreads();
+        if (lane == 31)
+            sh.red[0][w] = run;
+        __syncthreads();
+        run += up - sum;
+        for (int i = 0; i < w; ++i)
+            run += sh.red[0][i];
+        for (int i = i0; i < i1; ++i) {
+            const mass_t next = run + own(i);
+            if (run < target && next >= target)
+                sh.got = (all[i] >> 32) + 1;
+            run = next;
+        }
+        __syncthreads();
+        const mass_t got = sh.got;
+        mass_t a = 0, b = 0;
+        for (int i = i0; i < i1; ++i) {
+            const mass_t k = all[i] >> 32;
+            a += k + 1 > got ? own(i) : 0;
+            b += k + 1 == got ? own(i) : 0;
+        }
+        block_sum(a, b);
+        if (threadIdx.x == 0) {
+            sh.above = up + a;
+            sh.equal = b;
+        }
+    }
+    // The same by digits of 8 bits, whatever the entries.
+    template <typename F>
+    __device__ uint32_t radix(mass_t target, F weight, mass_t &above, mass_t &equal)
     {
         uint32_t prefix = 0;
         mass_t over = 0;
         for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += NT)
-                sh.hist[i] = 0;
+            sh.hist[threadIdx.x] = 0;
             __syncthreads();
             each([&](int64_t, float z) {
                 const uint32_t k = order_key(z);
@@ -392,16 +622,14 @@ template <typename InT, int NT> struct RowSelect {
                 }
             });
             cl.sync();
-            for (int i = threadIdx.x; i < 256; i += NT) {
-                mass_t s = 0;
-                for (unsigned r = 0; r < size; ++r)
-                    s += *peer(&sh.hist[i], r);
-                sh.tot[i] = s;
-            }
+            mass_t s = 0;
+            for (unsigned r = 0; r < size; ++r)
+                s += *peer(&sh.hist[threadIdx.x], r);
+            sh.tot[threadIdx.x] = s;
             __syncthreads();
             if (threadIdx.x < 32) {  // lane l: bins 255 - 8 l and the seven below it
                 const int lane = threadIdx.x;
-                mass_t s = 0;
+                s = 0;
                 for (int i = 0; i < 8; ++i)
                     s += sh.tot[255 - 8 * lane - i];
                 mass_t incl = s;
@@ -429,43 +657,65 @@ template <typename InT, int NT> struct RowSelect {
         __syncthreads();
         return prefix;
     }
-    // Mass above `key` and the number of entries at it, with the parts before this CTA.
+    // Mass above `key` and the number of entries at it, with the parts before this CTA; the
+    // warps' parts stay in sh.stretch.  raw: the row's mass at temperature 1, if wanted.
     __device__ void kept_mass(uint32_t key, float M, const Scale &sc, mass_t &gt, mass_t &eq,
-                              mass_t &gt_before, mass_t &eq_before)
+                              mass_t &gt_before, mass_t &eq_before, float *raw)
     {
         gt = eq = 0;
+        float s = 0.0f;
         each([&](int64_t, float z) {
             const uint32_t k = order_key(z);
             if (k > key)
                 gt += fixed_mass(z, M, sc);
             eq += k == key;
+            if (raw)
+                s += ex2_ftz((z - M) * kLog2e);
         });
+        if (raw)
+            *raw = s;
+        mass_t a = gt, b = eq;
+        warp_sums(a, b);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) {
+            sh.stretch[0][threadIdx.x >> 5] = a;
+            sh.stretch[1][threadIdx.x >> 5] = b;
+        }
         cluster_sum(gt, eq, gt_before, eq_before);
     }
     // The first entry, by index, whose running kept mass is above t (below the total): the
-    // CTA that has it returns true in all its threads, with the index.
+    // CTA that has it returns true in all its threads, with the index.  After kept_mass for
+    // this key.
     __device__ bool locate(const Kept &kept, mass_t wkey, mass_t t, mass_t gt_before,
-                           mass_t eq_before, float M, const Scale &sc, int64_t &index)
+                           mass_t eq_before, int64_t &index, float M, const Scale &sc)
     {
-        mass_t run = gt_before + min(eq_before, kept.ties) * wkey, ties = eq_before;
-        if (run > t)
+        auto upto = [&](mass_t gt, mass_t eq) { return gt + min(eq, kept.ties) * wkey; };
+        mass_t gt = gt_before, eq = eq_before;
+        if (upto(gt, eq) > t)
             return false;  // an earlier CTA's
+        int w = 0;
+        for (; w < W; ++w) {
+            const mass_t g = gt + sh.stretch[0][w], e = eq + sh.stretch[1][w];
+            if (upto(g, e) > t)
+                break;
+            gt = g;
+            eq = e;
+        }
+        if (w == W)
+            return false;  // a later one's
+        __syncthreads();
         if (threadIdx.x == 0)
             sh.got = 0;
-        for (int64_t b = j0; b < j1; b += NT) {
+        for (int64_t b = first(w); b < first(w + 1); b += NT) {
             const int64_t j = b + threadIdx.x;
-            mass_t w = 0;
-            uint32_t k = 0;
-            if (j < j1) {
-                const float z = to_f32(row[j]);
-                k = order_key(z);
-                if (k > kept.key)
-                    w = fixed_mass(z, M, sc);
-            }
-            const bool tie = j < j1 && k == kept.key;
+            const bool in = j < first(w + 1);
+            const float z = in ? to_f32(row[j]) : -INFINITY;
+            const uint32_t k = order_key(z);
+            const mass_t own = in && k > kept.key ? fixed_mass(z, M, sc) : 0;
+            const bool tie = in && k == kept.key;
             // this thread's place in the block's order: sums over the entries up to it
             const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-            mass_t iw = w, it = tie;
+            mass_t iw = own, it = tie;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const mass_t x = __shfl_up_sync(0xffffffffu, iw, o);
@@ -479,28 +729,23 @@ template <typename InT, int NT> struct RowSelect {
                 sh.red[1][wid] = it;
             }
             __syncthreads();
-            mass_t bw = 0, bt = 0, tw = 0, tt = 0;
-            for (int i = 0; i < NT / 32; ++i) {
+            mass_t tw = 0, tt = 0;
+            for (int i = 0; i < W; ++i) {
                 const mass_t x = sh.red[0][i], y = sh.red[1][i];
-                bw += i < wid ? x : 0;
-                bt += i < wid ? y : 0;
+                iw += i < wid ? x : 0;
+                it += i < wid ? y : 0;
                 tw += x;
                 tt += y;
             }
-            // kept masses before the block, up to and before this entry
-            const mass_t before_ties = min(ties, kept.ties);
-            const mass_t upto = run + bw + iw + (min(ties + bt + it, kept.ties) - before_ties) * wkey;
-            const mass_t prev = run + bw + iw - w +
-                                (min(ties + bt + it - tie, kept.ties) - before_ties) * wkey;
-            if (upto > t && prev <= t)
+            if (in && upto(gt + iw, eq + it) > t && upto(gt + iw - own, eq + it - tie) <= t)
                 sh.got = (mass_t)j + 1;
             __syncthreads();
             if (sh.got) {
                 index = (int64_t)sh.got - 1;
                 return true;
             }
-            run += tw + (min(ties + tt, kept.ties) - before_ties) * wkey;
-            ties += tt;
+            gt += tw;
+            eq += tt;
         }
         return false;
     }

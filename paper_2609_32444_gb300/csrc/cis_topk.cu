@@ -17,9 +17,6 @@
 namespace cis {
 namespace {
 
-constexpr int kSelThreads = 512;
-constexpr int kSelCluster = 8;
-
 __device__ __forceinline__ void fill_row(const TopkArgs &a, int64_t t, float lp, float lse)
 {
     for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
@@ -129,10 +126,11 @@ __global__ void __launch_bounds__(NT)
 
 // Any row, exactly: a cluster per row reads it from memory once for each step.
 template <typename InT>
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelThreads, 3)
     cis_topk_exact_kernel(const __grid_constant__ TopkArgs a, bool every)
 {
-    __shared__ SelectShared<kSelThreads> sh;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
+    SelectShared<kSelThreads> &sh = *reinterpret_cast<SelectShared<kSelThreads> *>(dyn_smem);
     int turn = 0;
     if (threadIdx.x == 0)
         allow_next_grid();
@@ -152,7 +150,8 @@ __global__ void __launch_bounds__(kSelThreads)
             continue;
         }
         bool bad;
-        const uint32_t mk = rs.max_key(bad);
+        uint32_t least;
+        const uint32_t mk = rs.max_key(least, bad);
         if (bad) {  // as every CTA of the cluster finds
             if (rs.rank == 0) {
                 fill_row(a, t, NAN, NAN);
@@ -161,11 +160,13 @@ __global__ void __launch_bounds__(kSelThreads)
             }
             continue;
         }
-        const float M = key_value(mk);
+        const float M = key_value(mk), bottom = key_value(least);
         const int K = (int)(a.K < a.V ? a.K : a.V);
         mass_t above, equal;
         const uint32_t key =
-            rs.select((mass_t)K, [](float, uint32_t) { return (mass_t)1; }, above, equal);
+            rs.select((mass_t)K, (float)K, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
+                      [](float, uint32_t) { return 1.0f; },
+                      [](float, uint32_t) { return (mass_t)1; }, above, equal);
         const mass_t ties = (mass_t)K - above;
         if (rs.rank == 0 && threadIdx.x == 0)
             sh.n = 0;
@@ -254,10 +255,16 @@ cudaError_t launch_fast(const TopkArgs &a, const PassPlan &p, cudaStream_t s)
 template <typename InT>
 cudaError_t launch_exact(const TopkArgs &a, bool every, cudaStream_t s)
 {
+    constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
+    const cudaError_t e = cudaFuncSetAttribute(
+        cis_topk_exact_kernel<InT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess)
+        return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 38 ? a.T : 38;
+    const int64_t groups = a.T < 57 ? a.T : 57;  // three CTAs an SM
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
