@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(NT)
 
 // Any row, exactly: a cluster per row.
 template <typename InT>
-__global__ void __launch_bounds__(kSelThreads, 3)
+__global__ void __launch_bounds__(kSelThreads, 2)
     cis_sample_exact_kernel(const __grid_constant__ SampleArgs a, bool every)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
@@ -536,11 +536,12 @@ __global__ void __launch_bounds__(kSelThreads, 3)
         const bool two = a.lp_out != nullptr && sc.hi != 1.0f;
         Kept kept{0, 0};
         mass_t above, equal;
+        bool parts = false;
         const int64_t k = rset.greedy ? 1 : rset.top_k;
         if (k > 0 && k < a.V) {
             kept.key = rs.select((mass_t)k, (float)k, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
                                  [](float, uint32_t) { return 1.0f; },
-                                 [](float, uint32_t) { return (mass_t)1; }, above, equal);
+                                 [](float, uint32_t) { return (mass_t)1; }, above, equal, parts);
             kept.ties = (mass_t)k - above;
         }
         mass_t gt, eq, gt0, eq0;
@@ -559,6 +560,7 @@ __global__ void __launch_bounds__(kSelThreads, 3)
         }
         mass_t wkey = kept.ties ? fixed_mass(key_value(kept.key), M, sc) : 0;
         bool moved = false;
+        parts = false;
         if (rset.top_p < 1.0f && !rset.greedy) {
             const mass_t target =
                 (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__(kSelThreads, 3)
                     [&](float z, uint32_t key) {
                         return key > floor_key ? fixed_mass(z, M, sc) : (mass_t)0;
                     },
-                    above, equal);
+                    above, equal, parts);
                 wkey = fixed_mass(key_value(kept.key), M, sc);
                 kept.ties = (target - above + wkey - 1) / wkey;
                 moved = true;
@@ -587,9 +589,12 @@ __global__ void __launch_bounds__(kSelThreads, 3)
                 kept = Kept{low - 1, 0};
                 wkey = 0;
                 moved = true;
+                parts = false;
             }
         }
-        if (moved)
+        if (parts)
+            rs.kept_parts(gt, eq, gt0, eq0);
+        else if (moved)
             rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0, nullptr);
         const mass_t Z = gt + min(eq, kept.ties) * wkey;
         const mass_t target = (mass_t)((double)rset.u * (double)Z);
@@ -639,7 +644,7 @@ cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 57 ? a.T : 57;  // three CTAs an SM
+    const int64_t groups = a.T < 38 ? a.T : 38;  // two CTAs an SM
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
     cfg.dynamicSmemBytes = smem;

@@ -65,8 +65,21 @@ __device__ const float2 kExp2Table[32] = {
     {0x1.d5818ep0f, -0x1.822dbcp-27f}, {0x1.dfc974p0f, -0x1.908c94p-25f},
     {0x1.ea4afap0f, 0x1.52486cp-27f}, {0x1.f50766p0f, -0x1.246ebp-26f}};
 
-// e^{x + x_lo} in units of 2^-43 for -80 < x <= 0, right to 2^-42 and half a unit: x is
-// reduced to n ln2/32 + r, |r| <= 0.011, with ln2/32 in three parts (n has 12 bits and the
+// a + b = s + e exactly, for finite numbers; ordered: |a| >= |b|.
+__device__ __forceinline__ float sum_pair(float a, float b, float &e)
+{
+    const float s = __fadd_rn(a, b), v = __fsub_rn(s, a);
+    e = __fadd_rn(__fsub_rn(a, __fsub_rn(s, v)), __fsub_rn(b, v));
+    return s;
+}
+__device__ __forceinline__ float sum_ordered(float a, float b, float &e)
+{
+    const float s = __fadd_rn(a, b);
+    e = __fsub_rn(b, __fsub_rn(s, a));
+    return s;
+}
+// e^{x + x_lo} in units of 2^-43 for -31 < x <= 0, right to 2^-42 and half a unit: x is
+// reduced to n ln2/32 + r, |r| <= 0.011, with ln2/32 in three parts (n has 11 bits and the
 // first part 12, so that the first product is exact), e^r is its Taylor series with the
 // terms up to r^2/2 kept as a pair, and 2^{n/32} comes from the table.
 __device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
@@ -75,29 +88,32 @@ __device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
     const float t0 = fmaf(n, -0x1.62ep-6f, x);
     float e1, e2, e3;
     const float p1 = n * -0x1.0bfbe8p-20f, p1e = fmaf(n, -0x1.0bfbe8p-20f, -p1);
-    const float r = two_sum(t0, p1, e1);
+    const float r = sum_pair(t0, p1, e1);
     const float rl = e1 + (p1e + fmaf(n, -0x1.cf79acp-45f, x_lo));
     float q = fmaf(1.0f / 120.0f, r, 1.0f / 24.0f);
     q = fmaf(q, r, 1.0f / 6.0f);
     const float h = 0.5f * r, s2 = h * r, s2e = fmaf(h, r, -s2);
-    const float w = two_sum(r, s2, e2);  // e^{r + rl} - 1 = w + wl
-    const float wl = e2 + (s2e + fmaf(q * r, r * r, rl * (1.0f + w)));
-    const int ni = (int)n;
+    const float w = sum_ordered(r, s2, e2);  // e^{r + rl} - 1 = w + wl
+    const float wl = e2 + (s2e + fmaf(q * r, r * r, fmaf(rl, w, rl)));
+    const int ni = __float2int_rn(n);
     const float2 T = __ldg(&kExp2Table[ni & 31]);
     const float p = T.x * w, pe = fmaf(T.x, w, -p);
-    const float s = two_sum(T.x, p, e3);
+    const float s = sum_ordered(T.x, p, e3);
     const float lo = e3 + (pe + (T.y + fmaf(T.x, wl, T.y * w)));
-    // (43 - 116 at the least: a normal number)
-    const float unit = __int_as_float((127 + kMassBits + (ni >> 5)) << 23);
-    return __float2ull_rz(s * unit) +
-           (unsigned long long)__float2ll_rn((s * unit - truncf(s * unit)) + lo * unit);
+    // in units of 2^-48 (s is a multiple of 2^-24 below 2.2, lo below 2^-23), then 2^{n >> 5}
+    const long long v = ((long long)__float2uint_rn(s * 0x1p24f) << 24) +
+                        (long long)__float2int_rn(lo * 0x1p48f);
+    const int down = 48 - kMassBits - (ni >> 5);  // 5 .. 50
+    return (unsigned long long)((v + (1ll << (down - 1))) >> down);
 }
-// e^{(z - M) / tau} in units of 2^-43, z <= M; 0 at -inf and below 2^-115.
+// e^{(z - M) / tau} in units of 2^-43, z <= M; 0 below e^-31, a quarter of a unit.
 __device__ __forceinline__ mass_t fixed_mass(float z, float M, const Scale &sc)
 {
-    float l;
-    const float x = scaled_diff(z, M, sc, l);
-    return x > -80.0f ? fixed_exp(x, l) : 0;
+    float dl;
+    const float d = sum_pair(z, -M, dl), x = d * sc.hi;
+    if (!(x > -31.0f))
+        return 0;
+    return fixed_exp(x, fmaf(d, sc.hi, -x) + fmaf(d, sc.lo, dl * sc.hi));
 }
 __device__ __forceinline__ double mass_value(mass_t m)
 {
@@ -231,8 +247,6 @@ template <int NT> struct SelectShared {
     float bins[2][kBins];
     uint32_t digit, low_key;
     float bin_over;
-    int bin;
-    bool edges;
     mass_t above, equal;
     mass_t got;             // the entry that was found, plus 1
     mass_t list[kListMax];  // candidates
@@ -433,18 +447,21 @@ template <typename InT, int NT> struct RowSelect {
     // (1 .. the total), the weight strictly above it and that at it.  weight(z, key): an
     // entry's, in whole numbers; approx(z, key): the same in fp32, `goal` the target likewise.
     //
+    // parts: the warps' weights above the key and their entries at it have been left in
+    // sh.stretch, as kept_mass leaves them.
+    //
     // Two levels of 32 bins, over [low, M] and then over the bin in which the fp32 weights
     // reach the goal, each thread with a column of its own (no atomics); then one pass adds
     // up the whole numbers above that bin and lists its entries, which the first CTA sorts.
     // Where they do not fit, or the bin was not the one, a radix selection does it.
     template <typename A, typename F>
     __device__ uint32_t select(mass_t target, float goal, float low, float M, A approx, F weight,
-                               mass_t &above, mass_t &equal)
+                               mass_t &above, mass_t &equal, bool &parts)
     {
+        parts = false;
         uint32_t khi = order_key(M), klo = 0;  // the entries with klo < key <= khi
         float over = 0.0f;
-        bool edges = true;
-        for (int level = 0; level < 4 && edges; ++level) {
+        for (int level = 0; level < 4; ++level) {
             const float hi = key_value(khi), lo = klo ? key_value(klo) : low;
             const float inv = (float)kBins / (hi - lo);
             if (!(hi > lo) || !(inv < INFINITY) || !(inv > 0.0f))
@@ -488,23 +505,25 @@ template <typename InT, int NT> struct RowSelect {
                 const unsigned reach = __ballot_sync(0xffffffffu, over + incl >= goal);
                 const int b = reach ? __ffs(reach) - 1 : kBins - 1;
                 const float before = __shfl_sync(0xffffffffu, incl, b ? b - 1 : 0);
-                if (lane == 0) {
-                    sh.bin = b;
-                    sh.bin_over = over + (b ? before : 0.0f);
-                    // the largest key whose bin is b or beyond, and the same for b + 1
-                    sh.edges = true;
-                    auto edge = [&](int at) {
-                        uint32_t k = order_key(hi - (float)at / inv);
-                        int n = 0;
-                        while (n < 64 && bin(key_value(k)) < at)
-                            --k, ++n;
-                        while (n < 64 && bin(key_value(k + 1)) >= at)
-                            ++k, ++n;
-                        sh.edges = sh.edges && n < 64;
-                        return k;
-                    };
-                    sh.digit = b ? min(edge(b), khi) : khi;
-                    sh.low_key = b < kBins - 1 ? max(edge(b + 1), klo) : klo;
+                // the largest key whose bin is b or beyond (lane 0), and the same for b + 1
+                // (lane 1): bins do not fall as keys do
+                if (lane < 2) {
+                    uint32_t in = klo, out = khi;  // bin(in) >= at, or in = klo
+                    if (bin(key_value(khi)) >= b + lane)
+                        in = khi;
+                    while (out - in > 1) {
+                        const uint32_t mid = in + (out - in) / 2;
+                        if (bin(key_value(mid)) >= b + lane)
+                            in = mid;
+                        else
+                            out = mid;
+                    }
+                    if (lane == 0) {
+                        sh.bin_over = over + (b ? before : 0.0f);
+                        sh.digit = in;
+                    } else {
+                        sh.low_key = b < kBins - 1 ? in : klo;
+                    }
                 }
             }
             buf ^= 1;
@@ -512,9 +531,8 @@ template <typename InT, int NT> struct RowSelect {
             khi = sh.digit;
             klo = sh.low_key;
             over = sh.bin_over;
-            edges = sh.edges && khi > klo;
             __syncthreads();
-            if (level == 0 || !edges)
+            if (level == 0)
                 continue;
             // whole numbers above the bin, and its entries
             if (threadIdx.x == 0)
@@ -531,7 +549,13 @@ template <typename InT, int NT> struct RowSelect {
                         sh.list[i] = order_pair(k, (uint32_t)j);
                 }
             });
+            mass_t a = up, b = 0;
+            warp_sums(a, b);
             __syncthreads();
+            if ((threadIdx.x & 31) == 0) {
+                sh.stretch[0][threadIdx.x >> 5] = a;
+                sh.stretch[1][threadIdx.x >> 5] = 0;
+            }
             n = threadIdx.x == 0 ? (mass_t)sh.n : 0;
             const int mine = sh.n;
             cluster_sum(up, n, x, at);
@@ -544,14 +568,28 @@ template <typename InT, int NT> struct RowSelect {
             if (rank == 0)
                 pick(reinterpret_cast<mass_t *>(sh.cols), (int)n, target, up, weight);
             cl.sync();
-            const SelectShared<NT> *first = peer(&sh, 0);
-            const mass_t got = first->got;
-            above = first->above;
-            equal = first->equal;
+            const SelectShared<NT> *lead = peer(&sh, 0);
+            const mass_t got = lead->got;
+            above = lead->above;
+            equal = lead->equal;
             cl.sync();
-            if (got)
-                return (uint32_t)(got - 1);
-            break;
+            if (!got)
+                break;
+            const uint32_t key = (uint32_t)(got - 1);
+            for (int i = threadIdx.x; i < mine; i += NT) {
+                const uint32_t k = (uint32_t)(sh.list[i] >> 32);
+                const int64_t j = (int64_t)(0xffffffffu - (uint32_t)sh.list[i]);
+                int of = 0;
+                while (of < W - 1 && j >= first(of + 1))
+                    ++of;
+                if (k > key)
+                    atomicAdd(&sh.stretch[0][of], weight(key_value(k), k));
+                else if (k == key)
+                    atomicAdd(&sh.stretch[1][of], (mass_t)1);
+            }
+            __syncthreads();
+            parts = true;
+            return key;
         }
         return radix(target, weight, above, equal);
     }
@@ -681,6 +719,14 @@ template <typename InT, int NT> struct RowSelect {
             sh.stretch[0][threadIdx.x >> 5] = a;
             sh.stretch[1][threadIdx.x >> 5] = b;
         }
+        cluster_sum(gt, eq, gt_before, eq_before);
+    }
+    // The same from the parts that a selection by these masses has left.
+    __device__ void kept_parts(mass_t &gt, mass_t &eq, mass_t &gt_before, mass_t &eq_before)
+    {
+        const bool one = threadIdx.x < W;
+        gt = one ? sh.stretch[0][threadIdx.x] : 0;
+        eq = one ? sh.stretch[1][threadIdx.x] : 0;
         cluster_sum(gt, eq, gt_before, eq_before);
     }
     // The first entry, by index, whose running kept mass is above t (below the total): the

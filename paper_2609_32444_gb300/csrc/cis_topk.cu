@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(NT)
 
 // Any row, exactly: a cluster per row reads it from memory once for each step.
 template <typename InT>
-__global__ void __launch_bounds__(kSelThreads, 3)
+__global__ void __launch_bounds__(kSelThreads, 2)
     cis_topk_exact_kernel(const __grid_constant__ TopkArgs a, bool every)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
@@ -163,10 +163,11 @@ __global__ void __launch_bounds__(kSelThreads, 3)
         const float M = key_value(mk), bottom = key_value(least);
         const int K = (int)(a.K < a.V ? a.K : a.V);
         mass_t above, equal;
+        bool parts;
         const uint32_t key =
             rs.select((mass_t)K, (float)K, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
                       [](float, uint32_t) { return 1.0f; },
-                      [](float, uint32_t) { return (mass_t)1; }, above, equal);
+                      [](float, uint32_t) { return (mass_t)1; }, above, equal, parts);
         const mass_t ties = (mass_t)K - above;
         if (rs.rank == 0 && threadIdx.x == 0)
             sh.n = 0;
@@ -261,7 +262,7 @@ cudaError_t launch_exact(const TopkArgs &a, bool every, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 57 ? a.T : 57;  // three CTAs an SM
+    const int64_t groups = a.T < 38 ? a.T : 38;  // two CTAs an SM
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
     cfg.dynamicSmemBytes = smem;
