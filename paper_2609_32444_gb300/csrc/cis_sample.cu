@@ -58,6 +58,14 @@ constexpr float kOpen = 0x1p-18f;
 constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
 constexpr int kAim = 256;      // candidates aimed at where top_k does not say
 
+// The row is left to the exact kernel, with its mass at temperature 1.
+__device__ __forceinline__ void leave_row(const SampleArgs &a, int64_t t, float S1)
+{
+    a.ids_out[t] = kTodo;
+    if (a.lp_out)
+        a.lp_out[t] = S1;
+}
+
 // Inclusive sums over the CTA's threads, in `scan`; with barriers.
 template <int NT, typename T> __device__ void block_scan(T v, T *scan, T *warps)
 {
@@ -402,7 +410,7 @@ __global__ void __launch_bounds__(NT)
         }
         __syncthreads();
         if (tid == 0 && !done)
-            a.ids_out[t] = kTodo;
+            leave_row(a, t, S1);
         return;
     }
 
@@ -432,7 +440,7 @@ __global__ void __launch_bounds__(NT)
     }
     if (n > cap) {
         if (tid == 0)
-            a.ids_out[t] = kTodo;
+            leave_row(a, t, S1);
         return;
     }
     sort_list<NT>(list, n);
@@ -487,7 +495,7 @@ __global__ void __launch_bounds__(NT)
     }
     if (tid == 0) {
         if (at < 0) {
-            a.ids_out[t] = kTodo;
+            leave_row(a, t, S1);
         } else {
             const float z = key_value((uint32_t)(pick >> 32));
             write_row(a, t, (int32_t)(0xffffffffu - (uint32_t)pick), log_share(z, M, one, S1),
@@ -504,8 +512,10 @@ __global__ void __launch_bounds__(kSelThreads, 2)
     extern __shared__ __align__(16) uint8_t dyn_smem[];
     SelectShared<kSelThreads> &sh = *reinterpret_cast<SelectShared<kSelThreads> *>(dyn_smem);
     int turn = 0;
-    if (threadIdx.x == 0)
+    if (threadIdx.x == 0) {
         allow_next_grid();
+        sh.ready = false;
+    }
     grid_wait();
     RowsLeft<kSelThreads> rows(sh, a.T, gridDim.x / kSelCluster, blockIdx.x / kSelCluster);
     for (;;) {
@@ -520,6 +530,13 @@ __global__ void __launch_bounds__(kSelThreads, 2)
                 write_row(a, t, -1, 0.0f, 0.0f);
             continue;
         }
+        if (!sh.ready) {
+            __syncthreads();
+            fill_row_table(sh.table);
+            if (threadIdx.x == 0)
+                sh.ready = true;
+            __syncthreads();
+        }
         const RowSettings rset = row_settings(a, t);
         bool bad;
         uint32_t least;
@@ -533,76 +550,79 @@ __global__ void __launch_bounds__(kSelThreads, 2)
         }
         const float M = key_value(mk), bottom = key_value(least);
         const Scale &sc = rset.sc;
-        const bool two = a.lp_out != nullptr && sc.hi != 1.0f;
+        const RowMass mass(sh.table, M, rset.tau, sc);
+        const float depth = M - 31.0f * rset.tau, floor_z = bottom > depth ? bottom : depth;
+        // entries' weights in a selection: 1 each, or the mass of those above zk
+        bool count = false;
+        float zk = -INFINITY;
+        auto approx = [&](float z) {
+            return count ? 1.0f : (z > zk ? ex2_ftz((z - M) * sc.kappa) : 0.0f);
+        };
+        auto weight = [&](float z) {
+            return count ? (mass_t)1 : (z > zk ? mass(z) : (mass_t)0);
+        };
         Kept kept{0, 0};
-        mass_t above, equal;
+        mass_t above, equal, gt, eq, gt0, eq0, target, wkey = 0;
         bool parts = false;
         const int64_t k = rset.greedy ? 1 : rset.top_k;
-        if (k > 0 && k < a.V) {
-            kept.key = rs.select((mass_t)k, (float)k, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
-                                 [](float, uint32_t) { return 1.0f; },
-                                 [](float, uint32_t) { return (mass_t)1; }, above, equal, parts);
-            kept.ties = (mass_t)k - above;
-        }
-        mass_t gt, eq, gt0, eq0;
-        float raw = 0.0f;
-        rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0, two ? &raw : nullptr);
-        // (the row's mass at temperature 1: fp32 exponentials, added up as whole numbers)
-        mass_t S1 = 0, none = 0, x, y;
-        if (two) {
-            S1 = (mass_t)((double)raw * (double)(1ull << kMassBits));
-            rs.cluster_sum(S1, none, x, y);
-        } else if (kept.key == 0) {
-            S1 = gt;
-        } else if (a.lp_out) {
-            rs.each([&](int64_t, float z) { S1 += fixed_mass(z, M, sc); });
-            rs.cluster_sum(S1, none, x, y);
-        }
-        mass_t wkey = kept.ties ? fixed_mass(key_value(kept.key), M, sc) : 0;
-        bool moved = false;
-        parts = false;
-        if (rset.top_p < 1.0f && !rset.greedy) {
-            const mass_t target =
-                (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
-            if (target <= gt) {
-                const uint32_t floor_key = kept.key;
-                const float low = M - 32.0f * rset.tau;
-                kept.key = rs.select(
-                    target, (float)mass_value(target), bottom > low ? bottom : low, M,
-                    [&](float z, uint32_t key) {
-                        return key > floor_key ? ex2_ftz((z - M) * sc.kappa) : 0.0f;
-                    },
-                    [&](float z, uint32_t key) {
-                        return key > floor_key ? fixed_mass(z, M, sc) : (mass_t)0;
-                    },
-                    above, equal, parts);
-                wkey = fixed_mass(key_value(kept.key), M, sc);
-                kept.ties = (target - above + wkey - 1) / wkey;
-                moved = true;
-            } else if (wkey) {
-                kept.ties = min(kept.ties, (target - gt + wkey - 1) / wkey);
+        const bool by_k = k > 0 && k < a.V, by_p = rset.top_p < 1.0f && !rset.greedy;
+        // top_k first, then top_p: one place for both, as the selection's code is large
+#pragma unroll 1
+        for (int step = by_k ? 0 : 1; step < (by_p ? 2 : 1); ++step) {
+            count = step == 0;
+            float goal = (float)k, share = 0.0f, low = M - bottom > 1024.0f ? M - 64.0f : bottom;
+            target = (mass_t)k;
+            if (!count) {
+                low = floor_z;
+                if (by_k) {
+                    rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
+                    target = (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
+                    if (target > gt) {  // within the entries at the key
+                        if (wkey)
+                            kept.ties = min(kept.ties, (target - gt + wkey - 1) / wkey);
+                        break;
+                    }
+                    goal = (float)mass_value(target);
+                    zk = key_value(kept.key);
+                } else {
+                    share = rset.top_p;
+                }
             }
+            kept.key = rs.select(target, goal, share, low, M, approx, weight, above, equal, parts);
+            parts = parts && !count;
+            wkey = mass(key_value(kept.key));
+            kept.ties = count ? target - above : (target - above + wkey - 1) / wkey;
         }
         if (rset.min_p > 0.0f) {
             const uint32_t low = min_p_key(M, rset.tau, rset.min_p);
             if (kept.key < low) {
                 kept = Kept{low - 1, 0};
                 wkey = 0;
-                moved = true;
                 parts = false;
             }
         }
         if (parts)
             rs.kept_parts(gt, eq, gt0, eq0);
-        else if (moved)
-            rs.kept_mass(kept.key, M, sc, gt, eq, gt0, eq0, nullptr);
+        else
+            rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
         const mass_t Z = gt + min(eq, kept.ties) * wkey;
-        const mass_t target = (mass_t)((double)rset.u * (double)Z);
+        target = (mass_t)((double)rset.u * (double)Z);
+        // the row's mass at temperature 1: the first kernel's, where it has left the row
+        float S1 = 0.0f;
+        if (a.lp_out && !every) {
+            S1 = a.lp_out[t];
+        } else if (a.lp_out) {
+            float s = 0.0f;
+            rs.each([&](int64_t, float z) { s += ex2_ftz((z - M) * kLog2e); });
+            mass_t sum = (mass_t)((double)s * (double)(1ull << kMassBits)), none = 0, x, y;
+            rs.cluster_sum(sum, none, x, y);
+            S1 = (float)mass_value(sum);
+        }
         int64_t j = 0;
-        if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, j, M, sc) && threadIdx.x == 0) {
+        if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, mass, j) && threadIdx.x == 0) {
             const float z = to_f32(rs.row[j]);
             const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
-            write_row(a, t, (int32_t)j, log_share(z, M, one, (float)mass_value(S1)),
+            write_row(a, t, (int32_t)j, log_share(z, M, one, S1),
                       rset.greedy ? 0.0f : log_share(z, M, sc, (float)mass_value(Z)));
         }
         __syncthreads();

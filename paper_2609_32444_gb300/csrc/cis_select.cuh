@@ -8,6 +8,8 @@
 // split and every call come to the same entry, and 2^63 holds a row of 2^20 maxima.
 #pragma once
 
+#include <stddef.h>
+
 #include "cis_expacc.cuh"
 #include "cis_slice.cuh"
 
@@ -232,6 +234,78 @@ __device__ __forceinline__ float nth_of(const float *v, int n, int r)
     return __shfl_sync(0xffffffffu, x, who ? __ffs(who) - 1 : 0);
 }
 
+// The same for the whole of a row: the masses of e^{(z - M) / tau}, right to 2^-34 of each.
+// With K = 512 log2e / tau as a pair, z K is n + f, |f| <= 1/2, by an FMA (rounded at 2^-26,
+// whatever the size of z K); f and n are taken less those of M, and the mass is
+// 2^{n >> 9} T[n & 511] e^{f ln2 / 512}, T[i] = 2^{i / 512} as a pair, the exponential by three
+// terms.  34 instructions an entry where fixed_mass takes some 60, which bounds the kernels
+// that add up whole rows.
+constexpr int kRowTable = 512;
+__device__ inline void fill_row_table(float2 *table)
+{
+    for (int i = threadIdx.x; i < kRowTable; i += blockDim.x) {
+        const double v = exp2((double)i / kRowTable);
+        const float hi = (float)v;
+        table[i] = make_float2(hi, (float)(v - (double)hi));
+    }
+}
+struct RowMass {
+    const float2 *table;
+    Scale sc;
+    float M, low;      // entries below `low` have no mass
+    float khi, klo, fM;
+    int nM;
+    bool fast;         // |z K| stays below 2^22
+
+    __device__ __forceinline__ RowMass(const float2 *t, float M_, float tau, const Scale &s)
+        : table(t), sc(s), M(M_)
+    {
+        low = M - 31.0f * tau;
+        fast = fabsf(M) < 5000.0f * tau;
+        // log2e = kLog2e + 1.9e-8, 1 / tau = hi + lo
+        constexpr float log2e_lo = (float)(1.4426950408889634074 - (double)kLog2e);
+        khi = 512.0f * kLog2e * sc.hi;
+        klo = fmaf(512.0f * kLog2e, sc.hi, -khi) +
+              512.0f * fmaf(kLog2e, sc.lo, log2e_lo * sc.hi);
+        nM = 0;
+        fM = 0.0f;
+        if (fast)
+            split(M, nM, fM);
+    }
+    __device__ __forceinline__ void split(float z, int &n, float &f) const
+    {
+        constexpr float magic = 12582912.0f;  // 1.5 * 2^23
+        const float t = fmaf(z, khi, magic), w = t - magic;
+        n = __float_as_int(t) - __float_as_int(magic);
+        f = fmaf(z, klo, fmaf(z, khi, -w));
+    }
+    __device__ __forceinline__ mass_t operator()(float z) const
+    {
+        if (!(z >= low))  // (M itself has, however far apart its neighbours are)
+            return 0;
+        if (!fast)
+            return fixed_mass(z, M, sc);
+        int n;
+        float f;
+        split(z, n, f);
+        n -= nM;
+        f -= fM;
+        const float2 T = table[n & (kRowTable - 1)];
+        constexpr float c1 = (float)(0.693147180559945309417 / kRowTable);
+        constexpr float c2 = (float)(0.5 * 0.693147180559945309417 / kRowTable *
+                                     0.693147180559945309417 / kRowTable);
+        constexpr float c3 = c1 * c2 / 3.0f;
+        const float u = f * fmaf(f, fmaf(f, c3, c2), c1);  // below 2^-9
+        const float lo = fmaf(T.x, u, T.y);
+        // in units of 2^-39, then of 2^-43 and by 2^{n >> 9} (a shift of 0 .. 45)
+        const long long v =
+            ((long long)((__float_as_uint(T.x) & 0x7fffffu) | 0x800000u) << 20) +
+            ((long long)__float2int_rn(lo * 0x1p39f) << 4);
+        const int down = -(n >> 9);
+        return (unsigned long long)((v + ((1ll << down) >> 1)) >> down);
+    }
+};
+
 // ------------------------------------------------------------------ clusters
 constexpr int kSelThreads = 256;
 constexpr int kSelCluster = 8;
@@ -239,21 +313,27 @@ constexpr int kBins = 32;
 constexpr int kListMax = 1024;  // entries that a selection may come down to
 
 template <int NT> struct SelectShared {
+    alignas(16) mass_t list[kListMax];   // candidates
+    alignas(16) float cols[kBins * NT];  // a selection's bins, a column a thread; then, as
+                                         // kListMax mass_t, the cluster's list
+    alignas(16) float2 table[kRowTable];
     mass_t part[2][2];      // this CTA's share of the running sums
     mass_t red[2][NT / 32];
     mass_t stretch[2][NT / 32];  // the warps' kept mass and ties
     mass_t hist[256];
     mass_t tot[256];
-    float bins[2][kBins];
-    uint32_t digit, low_key;
-    float bin_over;
     mass_t above, equal;
     mass_t got;             // the entry that was found, plus 1
-    mass_t list[kListMax];  // candidates
-    float cols[kBins * NT]; // a selection's bins, a column a thread; then the cluster's list
+    float bins[2][kBins];
+    float bin_over;
+    uint32_t digit, low_key;
     int n;
     unsigned left[NT / 32]; // rows left to do, a bit each
+    bool ready;             // the table is filled
 };
+static_assert(offsetof(SelectShared<kSelThreads>, cols) % alignof(mass_t) == 0 &&
+                  sizeof(float) * kBins * kSelThreads >= sizeof(mass_t) * kListMax,
+              "the columns hold the cluster's list");
 
 // The rows that one cluster of the exact kernel takes, in order: rows group, group + groups,
 // ... of which `left` says so, NT of them looked at together.  Every CTA of the cluster sees
@@ -444,8 +524,9 @@ template <typename InT, int NT> struct RowSelect {
         return (uint32_t)a;
     }
     // The key at which the weight of the entries from the largest on reaches `target`
-    // (1 .. the total), the weight strictly above it and that at it.  weight(z, key): an
-    // entry's, in whole numbers; approx(z, key): the same in fp32, `goal` the target likewise.
+    // (1 .. the total), the weight strictly above it and that at it.  weight(z): an entry's,
+    // in whole numbers; approx(z): the same in fp32, `goal` the target likewise.  share > 0:
+    // the target is ceil(share * the total), which the pass finds on its way.
     //
     // parts: the warps' weights above the key and their entries at it have been left in
     // sh.stretch, as kept_mass leaves them.
@@ -455,8 +536,8 @@ template <typename InT, int NT> struct RowSelect {
     // up the whole numbers above that bin and lists its entries, which the first CTA sorts.
     // Where they do not fit, or the bin was not the one, a radix selection does it.
     template <typename A, typename F>
-    __device__ uint32_t select(mass_t target, float goal, float low, float M, A approx, F weight,
-                               mass_t &above, mass_t &equal, bool &parts)
+    __device__ uint32_t select(mass_t &target, float goal, float share, float low, float M,
+                               A approx, F weight, mass_t &above, mass_t &equal, bool &parts)
     {
         parts = false;
         uint32_t khi = order_key(M), klo = 0;  // the entries with klo < key <= khi
@@ -476,7 +557,7 @@ template <typename InT, int NT> struct RowSelect {
             each([&](int64_t, float z) {
                 const uint32_t k = order_key(z);
                 if (k <= khi && k > klo)
-                    col[bin(z) * NT] += approx(z, k);
+                    col[bin(z) * NT] += approx(z);
             });
             __syncthreads();
             const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -502,6 +583,8 @@ template <typename InT, int NT> struct RowSelect {
                     const float y = __shfl_up_sync(0xffffffffu, incl, o);
                     incl += lane >= o ? y : 0.0f;
                 }
+                if (share > 0.0f && level == 0)
+                    goal = share * __shfl_sync(0xffffffffu, incl, 31);
                 const unsigned reach = __ballot_sync(0xffffffffu, over + incl >= goal);
                 const int b = reach ? __ffs(reach) - 1 : kBins - 1;
                 const float before = __shfl_sync(0xffffffffu, incl, b ? b - 1 : 0);
@@ -538,15 +621,20 @@ template <typename InT, int NT> struct RowSelect {
             if (threadIdx.x == 0)
                 sh.n = 0;
             __syncthreads();
-            mass_t up = 0, n = 0, x, at;
+            mass_t up = 0, n = 0, all_of = 0, x, y, at;
+            const float zhi = key_value(khi), zlo = klo ? key_value(klo) : -INFINITY;
             each([&](int64_t j, float z) {
-                const uint32_t k = order_key(z);
-                if (k > khi) {
-                    up += weight(z, k);
-                } else if (k > klo && weight(z, k) != 0) {
-                    const int i = atomicAdd(&sh.n, 1);
-                    if (i < kListMax)
-                        sh.list[i] = order_pair(k, (uint32_t)j);
+                // (z = -inf has weight only where entries are counted: klo = 0 lists it)
+                const bool over_it = z > zhi, in = !over_it && (z > zlo || klo == 0);
+                if (over_it || in || share > 0.0f) {
+                    const mass_t w = weight(z);
+                    up += over_it ? w : 0;
+                    all_of += w;
+                    if (in && w != 0) {
+                        const int i = atomicAdd(&sh.n, 1);
+                        if (i < kListMax)
+                            sh.list[i] = order_pair(order_key(z), (uint32_t)j);
+                    }
                 }
             });
             mass_t a = up, b = 0;
@@ -561,6 +649,11 @@ template <typename InT, int NT> struct RowSelect {
             cluster_sum(up, n, x, at);
             if (n > kListMax)
                 continue;  // another level
+            if (share > 0.0f) {
+                mass_t none = 0;
+                cluster_sum(all_of, none, x, y);
+                target = (mass_t)ceil((double)share * (double)all_of);
+            }
             mass_t *all = cl.map_shared_rank(reinterpret_cast<mass_t *>(sh.cols), 0);
             for (int i = threadIdx.x; i < mine; i += NT)
                 all[at + i] = sh.list[i];
@@ -583,13 +676,19 @@ template <typename InT, int NT> struct RowSelect {
                 while (of < W - 1 && j >= first(of + 1))
                     ++of;
                 if (k > key)
-                    atomicAdd(&sh.stretch[0][of], weight(key_value(k), k));
+                    atomicAdd(&sh.stretch[0][of], weight(key_value(k)));
                 else if (k == key)
                     atomicAdd(&sh.stretch[1][of], (mass_t)1);
             }
             __syncthreads();
             parts = true;
             return key;
+        }
+        if (share > 0.0f) {
+            mass_t all_of = 0, none = 0, x, y;
+            each([&](int64_t, float z) { all_of += weight(z); });
+            cluster_sum(all_of, none, x, y);
+            target = (mass_t)ceil((double)share * (double)all_of);
         }
         return radix(target, weight, above, equal);
     }
@@ -600,8 +699,7 @@ template <typename InT, int NT> struct RowSelect {
         sort_list<NT>(all, n);
         const int per = (n + NT - 1) / NT, i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
         auto own = [&](int i) {
-            const uint32_t k = (uint32_t)(all[i] >> 32);
-            return weight(key_value(k), k);
+            return weight(key_value((uint32_t)(all[i] >> 32)));
         };
         mass_t sum = 0;
         for (int i = i0; i < i1; ++i)
@@ -654,7 +752,7 @@ template <typename InT, int NT> struct RowSelect {
             each([&](int64_t, float z) {
                 const uint32_t k = order_key(z);
                 if (shift == 24 || ((k ^ prefix) >> (shift + 8)) == 0) {
-                    const mass_t w = weight(z, k);
+                    const mass_t w = weight(z);
                     if (w)
                         atomicAdd(&sh.hist[(k >> shift) & 255], w);
                 }
@@ -696,22 +794,17 @@ template <typename InT, int NT> struct RowSelect {
         return prefix;
     }
     // Mass above `key` and the number of entries at it, with the parts before this CTA; the
-    // warps' parts stay in sh.stretch.  raw: the row's mass at temperature 1, if wanted.
-    __device__ void kept_mass(uint32_t key, float M, const Scale &sc, mass_t &gt, mass_t &eq,
-                              mass_t &gt_before, mass_t &eq_before, float *raw)
+    // warps' parts stay in sh.stretch.
+    __device__ void kept_mass(uint32_t key, const RowMass &mass, mass_t &gt, mass_t &eq,
+                              mass_t &gt_before, mass_t &eq_before)
     {
         gt = eq = 0;
-        float s = 0.0f;
+        const float zk = key ? key_value(key) : -INFINITY;
         each([&](int64_t, float z) {
-            const uint32_t k = order_key(z);
-            if (k > key)
-                gt += fixed_mass(z, M, sc);
-            eq += k == key;
-            if (raw)
-                s += ex2_ftz((z - M) * kLog2e);
+            if (z > zk)
+                gt += mass(z);
+            eq += z == zk;
         });
-        if (raw)
-            *raw = s;
         mass_t a = gt, b = eq;
         warp_sums(a, b);
         __syncthreads();
@@ -733,7 +826,7 @@ template <typename InT, int NT> struct RowSelect {
     // CTA that has it returns true in all its threads, with the index.  After kept_mass for
     // this key.
     __device__ bool locate(const Kept &kept, mass_t wkey, mass_t t, mass_t gt_before,
-                           mass_t eq_before, int64_t &index, float M, const Scale &sc)
+                           mass_t eq_before, const RowMass &mass, int64_t &index)
     {
         auto upto = [&](mass_t gt, mass_t eq) { return gt + min(eq, kept.ties) * wkey; };
         mass_t gt = gt_before, eq = eq_before;
@@ -757,7 +850,7 @@ template <typename InT, int NT> struct RowSelect {
             const bool in = j < first(w + 1);
             const float z = in ? to_f32(row[j]) : -INFINITY;
             const uint32_t k = order_key(z);
-            const mass_t own = in && k > kept.key ? fixed_mass(z, M, sc) : 0;
+            const mass_t own = in && k > kept.key ? mass(z) : 0;
             const bool tie = in && k == kept.key;
             // this thread's place in the block's order: sums over the entries up to it
             const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;

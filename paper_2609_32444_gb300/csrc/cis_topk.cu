@@ -164,10 +164,11 @@ __global__ void __launch_bounds__(kSelThreads, 2)
         const int K = (int)(a.K < a.V ? a.K : a.V);
         mass_t above, equal;
         bool parts;
+        mass_t want = (mass_t)K;
         const uint32_t key =
-            rs.select((mass_t)K, (float)K, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
-                      [](float, uint32_t) { return 1.0f; },
-                      [](float, uint32_t) { return (mass_t)1; }, above, equal, parts);
+            rs.select(want, (float)K, 0.0f, M - bottom > 1024.0f ? M - 64.0f : bottom, M,
+                      [](float) { return 1.0f; }, [](float) { return (mass_t)1; }, above, equal,
+                      parts);
         const mass_t ties = (mass_t)K - above;
         if (rs.rank == 0 && threadIdx.x == 0)
             sh.n = 0;
