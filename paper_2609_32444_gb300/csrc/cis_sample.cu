@@ -58,12 +58,14 @@ constexpr float kOpen = 0x1p-18f;
 constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
 constexpr int kAim = 256;      // candidates aimed at where top_k does not say
 
-// The row is left to the exact kernel, with its mass at temperature 1.
-__device__ __forceinline__ void leave_row(const SampleArgs &a, int64_t t, float S1)
+// The row is left to the exact kernel, with its mass at temperature 1 and its maximum.
+__device__ __forceinline__ void leave_row(const SampleArgs &a, int64_t t, float S1, float M)
 {
     a.ids_out[t] = kTodo;
     if (a.lp_out)
         a.lp_out[t] = S1;
+    if (a.lps_out)
+        a.lps_out[t] = M;
 }
 
 // Inclusive sums over the CTA's threads, in `scan`; with barriers.
@@ -410,7 +412,7 @@ __global__ void __launch_bounds__(NT)
         }
         __syncthreads();
         if (tid == 0 && !done)
-            leave_row(a, t, S1);
+            leave_row(a, t, S1, M);
         return;
     }
 
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(NT)
     }
     if (n > cap) {
         if (tid == 0)
-            leave_row(a, t, S1);
+            leave_row(a, t, S1, M);
         return;
     }
     sort_list<NT>(list, n);
@@ -495,7 +497,7 @@ __global__ void __launch_bounds__(NT)
     }
     if (tid == 0) {
         if (at < 0) {
-            leave_row(a, t, S1);
+            leave_row(a, t, S1, M);
         } else {
             const float z = key_value((uint32_t)(pick >> 32));
             write_row(a, t, (int32_t)(0xffffffffu - (uint32_t)pick), log_share(z, M, one, S1),
@@ -538,17 +540,26 @@ __global__ void __launch_bounds__(kSelThreads, 2)
             __syncthreads();
         }
         const RowSettings rset = row_settings(a, t);
-        bool bad;
-        uint32_t least;
-        const uint32_t mk = rs.max_key(least, bad);
-        if (bad || !rset.ok) {  // as every CTA of the cluster finds
-            if (first) {
-                write_row(a, t, -1, NAN, NAN);
-                set_status(a.status, kStatusBadInput);
+        const int64_t k = rset.greedy ? 1 : rset.top_k;
+        const bool by_k = k > 0 && k < a.V, by_p = rset.top_p < 1.0f && !rset.greedy;
+        // The maximum: the first kernel's, where it has left the row, and the least entry is
+        // not needed
+        float M, bottom = -INFINITY;
+        if (!every && a.lps_out && !by_k) {
+            M = a.lps_out[t];
+        } else {
+            bool bad;
+            uint32_t least;
+            M = key_value(rs.max_key(least, bad));
+            bottom = key_value(least);
+            if (bad || !rset.ok) {  // as every CTA of the cluster finds
+                if (first) {
+                    write_row(a, t, -1, NAN, NAN);
+                    set_status(a.status, kStatusBadInput);
+                }
+                continue;
             }
-            continue;
         }
-        const float M = key_value(mk), bottom = key_value(least);
         const Scale &sc = rset.sc;
         const RowMass mass(sh.table, M, rset.tau, sc);
         const float depth = M - 31.0f * rset.tau, floor_z = bottom > depth ? bottom : depth;
@@ -564,8 +575,6 @@ __global__ void __launch_bounds__(kSelThreads, 2)
         Kept kept{0, 0};
         mass_t above, equal, gt, eq, gt0, eq0, target, wkey = 0;
         bool parts = false;
-        const int64_t k = rset.greedy ? 1 : rset.top_k;
-        const bool by_k = k > 0 && k < a.V, by_p = rset.top_p < 1.0f && !rset.greedy;
         // top_k first, then top_p: one place for both, as the selection's code is large
 #pragma unroll 1
         for (int step = by_k ? 0 : 1; step < (by_p ? 2 : 1); ++step) {

@@ -80,11 +80,11 @@ __device__ __forceinline__ float sum_ordered(float a, float b, float &e)
     e = __fsub_rn(b, __fsub_rn(s, a));
     return s;
 }
-// e^{x + x_lo} in units of 2^-43 for -31 < x <= 0, right to 2^-42 and half a unit: x is
-// reduced to n ln2/32 + r, |r| <= 0.011, with ln2/32 in three parts (n has 11 bits and the
-// first part 12, so that the first product is exact), e^r is its Taylor series with the
-// terms up to r^2/2 kept as a pair, and 2^{n/32} comes from the table.
-__device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
+// e^{x + x_lo} = (s + lo) 2^{n >> 5} for |x| < 31, right to 2^-42: x is reduced to n ln2/32 +
+// r, |r| <= 0.011, with ln2/32 in three parts (n has 11 bits and the first part 12, so that
+// the first product is exact), e^r is its Taylor series with the terms up to r^2/2 kept as a
+// pair, and 2^{n/32} comes from the table.  s is a multiple of 2^-24 below 2.2.
+__device__ __forceinline__ float exp_parts(float x, float x_lo, float &lo, int &ni)
 {
     const float n = rintf(x * (32.0f * kLog2e));
     const float t0 = fmaf(n, -0x1.62ep-6f, x);
@@ -97,12 +97,20 @@ __device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
     const float h = 0.5f * r, s2 = h * r, s2e = fmaf(h, r, -s2);
     const float w = sum_ordered(r, s2, e2);  // e^{r + rl} - 1 = w + wl
     const float wl = e2 + (s2e + fmaf(q * r, r * r, fmaf(rl, w, rl)));
-    const int ni = __float2int_rn(n);
+    ni = __float2int_rn(n);
     const float2 T = __ldg(&kExp2Table[ni & 31]);
     const float p = T.x * w, pe = fmaf(T.x, w, -p);
     const float s = sum_ordered(T.x, p, e3);
-    const float lo = e3 + (pe + (T.y + fmaf(T.x, wl, T.y * w)));
-    // in units of 2^-48 (s is a multiple of 2^-24 below 2.2, lo below 2^-23), then 2^{n >> 5}
+    lo = e3 + (pe + (T.y + fmaf(T.x, wl, T.y * w)));
+    return s;
+}
+// The same in units of 2^-43, for -31 < x <= 0.
+__device__ __forceinline__ unsigned long long fixed_exp(float x, float x_lo)
+{
+    float lo;
+    int ni;
+    const float s = exp_parts(x, x_lo, lo, ni);
+    // in units of 2^-48 (lo is below 2^-23), then 2^{n >> 5}
     const long long v = ((long long)__float2uint_rn(s * 0x1p24f) << 24) +
                         (long long)__float2int_rn(lo * 0x1p48f);
     const int down = 48 - kMassBits - (ni >> 5);  // 5 .. 50
@@ -152,11 +160,68 @@ __device__ inline uint32_t min_p_key(float M, float tau, float min_p)
 
 // ------------------------------------------------------------------ candidates
 // Sort n pairs in descending order (bitonic, padded with 0 up to a power of two); all threads.
+// Up to 4 a thread they stay in registers, R neighbouring ones a thread: strides within a
+// warp are shuffles, and shared memory and barriers are left for those across warps (512
+// pairs on 256 threads: 6 stages of 45; every stage through shared memory took 660 cycles).
+template <int NT, int R> __device__ void sort_regs(mass_t *list, int n, int size)
+{
+    const int first = (int)threadIdx.x * R;
+    mass_t x[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        x[r] = first + r < n ? list[first + r] : 0;
+    for (int k = 2; k <= size; k *= 2) {
+        auto keep = [&](int r, int j, mass_t y) {  // the larger goes first in descending runs
+            const int i = first + r;
+            const bool more = ((i & j) == 0) == ((i & k) == 0);
+            x[r] = (x[r] > y) == more ? x[r] : y;
+        };
+        int j = k / 2;
+        for (; j >= 32 * R; j /= 2) {
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                list[first + r] = x[r];
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                keep(r, j, list[(first + r) ^ j]);
+        }
+        for (; j >= R; j /= 2)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                keep(r, j, __shfl_xor_sync(0xffffffffu, x[r], j / R));
+#pragma unroll
+        for (int h = R / 2; h > 0; h /= 2)
+            if (h < k) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if ((r & h) == 0) {
+                        const mass_t a = x[r], b = x[r | h];
+                        keep(r, h, b);
+                        x[r | h] = x[r] == a ? b : a;
+                    }
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (first + r < size)
+            list[first + r] = x[r];
+    __syncthreads();
+}
 template <int NT> __device__ void sort_list(mass_t *list, int n)
 {
     int size = 2;
     while (size < n)
         size *= 2;
+    __syncthreads();
+    if (size <= NT)
+        return sort_regs<NT, 1>(list, n, size);
+    if (size <= 2 * NT)
+        return sort_regs<NT, 2>(list, n, size);
+    if (size <= 4 * NT)
+        return sort_regs<NT, 4>(list, n, size);
     for (int i = threadIdx.x; i < size; i += NT)
         if (i >= n)
             list[i] = 0;
@@ -164,7 +229,7 @@ template <int NT> __device__ void sort_list(mass_t *list, int n)
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
             for (int i = threadIdx.x; i < size / 2; i += NT) {
-                const int lo = 2 * j * (i / j) + i % j, hi = lo + j;
+                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;  // j a power of two
                 const mass_t x = list[lo], y = list[hi];
                 if ((x < y) == ((lo & k) == 0)) {
                     list[lo] = y;
@@ -238,39 +303,40 @@ __device__ __forceinline__ float nth_of(const float *v, int n, int r)
 // With K = 512 log2e / tau as a pair, z K is n + f, |f| <= 1/2, by an FMA (rounded at 2^-26,
 // whatever the size of z K); f and n are taken less those of M, and the mass is
 // 2^{n >> 9} T[n & 511] e^{f ln2 / 512}, T[i] = 2^{i / 512} as a pair, the exponential by three
-// terms.  34 instructions an entry where fixed_mass takes some 60, which bounds the kernels
-// that add up whole rows.
+// terms.  34 instructions an entry and no branch, where fixed_mass takes some 60 and several:
+// that bounds the kernels that add up whole rows.
 constexpr int kRowTable = 512;
 __device__ inline void fill_row_table(float2 *table)
 {
     for (int i = threadIdx.x; i < kRowTable; i += blockDim.x) {
-        const double v = exp2((double)i / kRowTable);
-        const float hi = (float)v;
-        table[i] = make_float2(hi, (float)(v - (double)hi));
+        const double x = (double)i * (0.693147180559945309417 / kRowTable);
+        const float hi = (float)x;
+        float lo;
+        int n;
+        const float s = exp_parts(hi, (float)(x - (double)hi), lo, n);
+        const float up = n == 32 ? 2.0f : 1.0f;
+        table[i] = make_float2(s * up, lo * up);  // (s * up in [1, 2))
     }
 }
 struct RowMass {
     const float2 *table;
-    Scale sc;
-    float M, low;      // entries below `low` have no mass
+    float low;         // entries below have no mass
+    float base;        // 0, or M where z K would leave the range: z - M is exact then, as the
+                       // entries that count are next to M
     float khi, klo, fM;
     int nM;
-    bool fast;         // |z K| stays below 2^22
 
-    __device__ __forceinline__ RowMass(const float2 *t, float M_, float tau, const Scale &s)
-        : table(t), sc(s), M(M_)
+    __device__ __forceinline__ RowMass(const float2 *t, float M, float tau, const Scale &sc)
+        : table(t)
     {
         low = M - 31.0f * tau;
-        fast = fabsf(M) < 5000.0f * tau;
+        base = fabsf(M) < 5000.0f * tau ? 0.0f : M;
         // log2e = kLog2e + 1.9e-8, 1 / tau = hi + lo
         constexpr float log2e_lo = (float)(1.4426950408889634074 - (double)kLog2e);
         khi = 512.0f * kLog2e * sc.hi;
         klo = fmaf(512.0f * kLog2e, sc.hi, -khi) +
               512.0f * fmaf(kLog2e, sc.lo, log2e_lo * sc.hi);
-        nM = 0;
-        fM = 0.0f;
-        if (fast)
-            split(M, nM, fM);
+        split(M - base, nM, fM);
     }
     __device__ __forceinline__ void split(float z, int &n, float &f) const
     {
@@ -281,13 +347,10 @@ struct RowMass {
     }
     __device__ __forceinline__ mass_t operator()(float z) const
     {
-        if (!(z >= low))  // (M itself has, however far apart its neighbours are)
-            return 0;
-        if (!fast)
-            return fixed_mass(z, M, sc);
+        const bool in = z >= low;  // (M itself, however far apart its neighbours are)
         int n;
         float f;
-        split(z, n, f);
+        split(in ? z - base : 0.0f, n, f);
         n -= nM;
         f -= fM;
         const float2 T = table[n & (kRowTable - 1)];
@@ -301,8 +364,9 @@ struct RowMass {
         const long long v =
             ((long long)((__float_as_uint(T.x) & 0x7fffffu) | 0x800000u) << 20) +
             ((long long)__float2int_rn(lo * 0x1p39f) << 4);
-        const int down = -(n >> 9);
-        return (unsigned long long)((v + ((1ll << down) >> 1)) >> down);
+        const int down = -(n >> 9) & 63;
+        const unsigned long long m = (unsigned long long)((v + ((1ll << down) >> 1)) >> down);
+        return in ? m : 0;
     }
 };
 
@@ -406,33 +470,54 @@ template <typename InT, int NT> struct RowSelect {
     {
         return w == 0 ? j0 : w == W ? j1 : head + (int64_t)seg(w) * EV;
     }
-    // f(index, entry) for this CTA's entries, each by a lane of its stretch's warp.
-    template <typename F> __device__ __forceinline__ void each(F f) const
+    // f(index of the first, entries, their number) for this CTA's entries, EV or fewer at a time
+    // (those absent are -inf), each by a lane of its stretch's warp.
+    template <typename F> __device__ __forceinline__ void vectors(F f) const
     {
         const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
         const uint4 *rv = reinterpret_cast<const uint4 *>(row + head);
+        const uint4 none = make_uint4(Vec<InT>::kNone, Vec<InT>::kNone, Vec<InT>::kNone,
+                                      Vec<InT>::kNone);
         const int s1 = seg(w + 1);
         int v = seg(w) + lane;
-        Vec<InT> x, y;
-        if (v < s1)
-            x.q = __ldg(rv + v);
-#pragma unroll 1
-        for (; v < s1; v += 32) {
-            if (v + 32 < s1)
-                y.q = __ldg(rv + v + 32);
-#pragma unroll
-            for (int k = 0; k < EV; ++k)
-                f(head + (int64_t)v * EV + k, x.entry(k));
-            x = y;
-        }
-        int64_t j = -1;  // the ragged ends
+        Vec<InT> x, y, t;  // two loads ahead
+        x.q = v < s1 ? __ldg(rv + v) : none;
+        y.q = v + 32 < s1 ? __ldg(rv + v + 32) : none;
+        int64_t j = -1;  // the ragged ends come last, one entry as a vector
         const int64_t tail = head + (V - head) / EV * EV;
         if (rank == 0 && w == 0 && lane < head)
             j = lane;
         if (rank == size - 1 && w == W - 1 && lane >= 16 && tail + lane - 16 < V)
             j = tail + lane - 16;
-        if (j >= 0)
-            f(j, to_f32(row[j]));
+#pragma unroll 1
+        for (;;) {
+            float z[EV];
+            const bool body = v < s1;
+            if (!body && j < 0)
+                break;
+            t.q = v + 64 < s1 ? __ldg(rv + v + 64) : none;
+#pragma unroll
+            for (int k = 0; k < EV; ++k)
+                z[k] = x.entry(k);  // (-inf past the stretch)
+            if (!body)
+                z[0] = to_f32(row[j]);
+            f(body ? head + (int64_t)v * EV : j, z, body ? EV : 1);
+            if (!body)
+                break;
+            x = y;
+            y = t;
+            v += 32;
+        }
+    }
+    // f(index, entry) for the same.
+    template <typename F> __device__ __forceinline__ void each(F f) const
+    {
+        vectors([&](int64_t j, const float (&z)[EV], int n) {
+#pragma unroll
+            for (int k = 0; k < EV; ++k)
+                if (k < n)
+                    f(j + k, z[k]);
+        });
     }
     template <typename T> __device__ __forceinline__ const T *peer(T *p, unsigned r)
     {
@@ -554,10 +639,19 @@ template <typename InT, int NT> struct RowSelect {
             float *col = sh.cols + threadIdx.x;
             for (int b = 0; b < kBins; ++b)
                 col[b * NT] = 0.0f;
-            each([&](int64_t, float z) {
-                const uint32_t k = order_key(z);
-                if (k <= khi && k > klo)
-                    col[bin(z) * NT] += approx(z);
+            const float zhi0 = hi, zlo0 = klo ? lo : -INFINITY;
+            const bool all_low = klo == 0;
+            vectors([&](int64_t, const float (&z)[EV], int n) {
+                float *c[EV], x[EV];
+#pragma unroll
+                for (int k = 0; k < EV; ++k) {
+                    const bool in = k < n && z[k] <= zhi0 && (z[k] > zlo0 || all_low);
+                    c[k] = col + (in ? bin(z[k]) : 0) * NT;
+                    x[k] = in ? approx(z[k]) : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < EV; ++k)
+                    *c[k] += x[k];
             });
             __syncthreads();
             const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -623,19 +717,25 @@ template <typename InT, int NT> struct RowSelect {
             __syncthreads();
             mass_t up = 0, n = 0, all_of = 0, x, y, at;
             const float zhi = key_value(khi), zlo = klo ? key_value(klo) : -INFINITY;
-            each([&](int64_t j, float z) {
-                // (z = -inf has weight only where entries are counted: klo = 0 lists it)
-                const bool over_it = z > zhi, in = !over_it && (z > zlo || klo == 0);
-                if (over_it || in || share > 0.0f) {
-                    const mass_t w = weight(z);
-                    up += over_it ? w : 0;
-                    all_of += w;
-                    if (in && w != 0) {
-                        const int i = atomicAdd(&sh.n, 1);
-                        if (i < kListMax)
-                            sh.list[i] = order_pair(order_key(z), (uint32_t)j);
-                    }
+            vectors([&](int64_t j, const float (&z)[EV], int m) {
+                mass_t w[EV];
+                unsigned in = 0;  // (z = -inf has weight only where entries are counted: klo = 0
+                                  // lists it)
+#pragma unroll
+                for (int k = 0; k < EV; ++k) {
+                    w[k] = k < m ? weight(z[k]) : 0;
+                    up += z[k] > zhi ? w[k] : 0;
+                    all_of += w[k];
+                    in |= (!(z[k] > zhi) && (z[k] > zlo || klo == 0) && w[k] != 0 ? 1u : 0u) << k;
                 }
+                if (in)
+#pragma unroll
+                    for (int k = 0; k < EV; ++k)
+                        if (in >> k & 1) {
+                            const int i = atomicAdd(&sh.n, 1);
+                            if (i < kListMax)
+                                sh.list[i] = order_pair(order_key(z[k]), (uint32_t)(j + k));
+                        }
             });
             mass_t a = up, b = 0;
             warp_sums(a, b);
@@ -800,10 +900,13 @@ template <typename InT, int NT> struct RowSelect {
     {
         gt = eq = 0;
         const float zk = key ? key_value(key) : -INFINITY;
-        each([&](int64_t, float z) {
-            if (z > zk)
-                gt += mass(z);
-            eq += z == zk;
+        vectors([&](int64_t, const float (&z)[EV], int n) {
+#pragma unroll
+            for (int k = 0; k < EV; ++k) {
+                const mass_t x = mass(z[k]);  // (0 where absent)
+                gt += z[k] > zk ? x : 0;
+                eq += k < n && z[k] == zk;
+            }
         });
         mass_t a = gt, b = eq;
         warp_sums(a, b);
