@@ -159,39 +159,36 @@ __device__ __forceinline__ float sum8_scaled(const float (&z)[8], float m, float
     return s.x + s.y;
 }
 
-// (max, sum of 2^{(z - max) kappa}) of two sets; empty: (-inf, 0).
-__device__ __forceinline__ MaxSum scaled_combine(MaxSum a, MaxSum b, float kappa)
-{
-    const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY)
-        return {m, a.s + b.s};
-    const float sa = a.m == -INFINITY ? a.s * 0.0f : a.s * ex2_ftz((a.m - m) * kappa);
-    const float sb = b.m == -INFINITY ? b.s * 0.0f : b.s * ex2_ftz((b.m - m) * kappa);
-    return {m, sa + sb};
-}
-
-// The CTA's (max, sum); every thread gets it.  sh: NT / 32 slots, used once.
+// The first NT threads' (max, sum), in all of them: the maximum first, then one rescaling a
+// thread.  sh: NT / 32 slots, used once; barrier 1.
 template <int NT>
 __device__ __forceinline__ MaxSum block_scaled(MaxSum v, MaxSum *sh, float kappa)
 {
+    auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); };
+    float M = v.m;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
-        v = scaled_combine(v, {__shfl_xor_sync(0xffffffffu, v.m, o),
-                               __shfl_xor_sync(0xffffffffu, v.s, o)}, kappa);
+        M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));  // (a NaN is kept by its sum)
     if ((threadIdx.x & 31) == 0)
-        sh[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float M = sh[0].m;
+        sh[threadIdx.x >> 5].m = M;
+    sync();
+    M = sh[0].m;
 #pragma unroll
     for (int i = 1; i < NT / 32; ++i)
         M = fmaxf(M, sh[i].m);
-    float S = 0.0f;
+    // an empty thread: s = 0, and e^{-inf} = 0
+    float s = M == -INFINITY ? v.s : v.s * ex2_ftz((v.m - M) * kappa);
 #pragma unroll
-    for (int i = 0; i < NT / 32; ++i) {
-        const MaxSum q = sh[i];
-        S += M == -INFINITY ? q.s : q.s * ex2_ftz((q.m - M) * kappa);
-    }
-    return {M, S};
+    for (int o = 16; o > 0; o >>= 1)
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0)
+        sh[threadIdx.x >> 5].s = s;
+    sync();
+    s = sh[0].s;
+#pragma unroll
+    for (int i = 1; i < NT / 32; ++i)
+        s += sh[i].s;
+    return {M, s};
 }
 
 // The pairs of a cluster's n CTAs, in rank order.
