@@ -29,8 +29,6 @@
 namespace cis {
 namespace {
 
-constexpr int kMaxList = CIS_MAX_TOPK;  // listed tokens of a row
-constexpr int kHash = 512;              // slots of the table that finds repeated ids
 constexpr unsigned kAll32 = 0xffffffffu;
 
 // e^{-d} - 1 + d: its series where the terms cancel (the first left out is below 2^-26 of
@@ -60,11 +58,26 @@ struct ListShared {
     alignas(8) uint64_t xbar;
     alignas(16) float2 part[kMaxCluster];
     MaxSum red[16];
-    int32_t table[kHash];
-    int32_t id[kMaxList];   // -1: empty
-    float z[kMaxList], a[kMaxList], value[kMaxList];
-    float2 row;             // the row's max and the rest's multiplier
+    float2 row;  // the row's max and the rest's multiplier
 };
+// The list, after the slab and sized by its length.
+struct ListView {
+    int32_t *table;          // finds repeated ids
+    int32_t *id;             // -1: empty
+    float *z, *a, *value;
+};
+// Slots of that table, a power of two: at most half of them are taken.
+__host__ __device__ constexpr int hash_slots(int K)
+{
+    int n = 64;
+    while (n < 2 * K)
+        n *= 2;
+    return n;
+}
+constexpr size_t list_bytes(int K)
+{
+    return (size_t)((K + 3) / 4 * 4) * 16 + (size_t)hash_slots(K) * 4;
+}
 
 // A barrier of the first NT threads.
 template <int NT> __device__ __forceinline__ void sync_warps()
@@ -106,16 +119,16 @@ __device__ __forceinline__ float list_gap(float z, float a, float ms, float c0, 
     return v + (e1 + e2 + l);
 }
 
-__device__ ListSums list_sums(const ListShared &sh, int K, int kind, const Scale &sc)
+__device__ __forceinline__ ListSums list_sums(const ListView &li, int K, int kind, const Scale &sc)
 {
     const int lane = threadIdx.x & 31;
     ListSums r{-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f, false};
     bool any = false;
     for (int k = lane; k < K; k += 32)
-        if (sh.id[k] >= 0) {
+        if (li.id[k] >= 0) {
             any = true;
-            r.ms = max_nan(r.ms, sh.z[k]);
-            r.am = max_nan(r.am, sh.a[k]);
+            r.ms = max_nan(r.ms, li.z[k]);
+            r.am = max_nan(r.am, li.a[k]);
         }
     r.any = __any_sync(kAll32, any);
     r.ms = warp_max_f(r.ms);
@@ -123,16 +136,16 @@ __device__ ListSums list_sums(const ListShared &sh, int K, int kind, const Scale
     float ss = 0.0f, sa = 0.0f, qh = 0.0f, ql = 0.0f;
 #pragma unroll 2
     for (int k = lane; k < K; k += 32)
-        if (sh.id[k] >= 0) {
+        if (li.id[k] >= 0) {
             float l;
-            const float x = scaled_diff(sh.z[k], r.ms, sc, l);
+            const float x = scaled_diff(li.z[k], r.ms, sc, l);
             if (r.ms != -INFINITY)
                 ss += expf(x + l);
             if (kind == CIS_DISTILL_TOPK) {
-                sa += expf(sh.a[k] - r.am);
+                sa += expf(li.a[k] - r.am);
             } else {
                 float e, lo;
-                const float hi = exp_pair(sh.a[k], 0.0f, lo);
+                const float hi = exp_pair(li.a[k], 0.0f, lo);
                 qh = two_sum(qh, hi, e);
                 ql += e + lo;
             }
@@ -157,18 +170,18 @@ __device__ ListSums list_sums(const ListShared &sh, int K, int kind, const Scale
         float c0 = 0.0f;
         bool have = false;
         for (int k = lane; k < K; k += 32)
-            if (!have && sh.id[k] >= 0 && sh.z[k] != -INFINITY) {
-                c0 = list_gap(sh.z[k], sh.a[k], r.ms, 0.0f, sc);
+            if (!have && li.id[k] >= 0 && li.z[k] != -INFINITY) {
+                c0 = list_gap(li.z[k], li.a[k], r.ms, 0.0f, sc);
                 have = true;
             }
         const unsigned who = __ballot_sync(kAll32, have);
         r.c0 = who ? __shfl_sync(kAll32, c0, __ffs(who) - 1) : 0.0f;
         float A = 0.0f;
         for (int k = lane; k < K; k += 32)
-            if (sh.id[k] >= 0 && sh.z[k] != -INFINITY) {
+            if (li.id[k] >= 0 && li.z[k] != -INFINITY) {
                 float l;
-                const float x = scaled_diff(sh.z[k], r.ms, sc, l);
-                A = fmaf(expf(x + l), list_gap(sh.z[k], sh.a[k], r.ms, r.c0, sc), A);
+                const float x = scaled_diff(li.z[k], r.ms, sc, l);
+                A = fmaf(expf(x + l), list_gap(li.z[k], li.a[k], r.ms, r.c0, sc), A);
             }
         r.A = warp_sum_f(A);
     }
@@ -257,6 +270,11 @@ __global__ void __launch_bounds__(NT + 32)
 
     if (tid == 0)
         allow_next_grid();
+    // this thread's first slot of the list, asked for ahead of the mask's answer
+    const int32_t *ids = a.ids + t * a.ld_list;
+    const float *lps = a.lp + t * a.ld_list;
+    const int id0 = tid < K ? ids[tid] : -1;
+    const float lp0 = tid < K ? lps[tid] : 0.0f;
     auto leave = [&](float kl) {  // a row without a gradient
         if (grad)
             zero_entries<OutT, NA>(orow, sl.n);
@@ -273,8 +291,15 @@ __global__ void __launch_bounds__(NT + 32)
         leave(0.0f);
         return;
     }
-    for (int i = tid; i < kHash; i += NA)
-        sh.table[i] = -1;
+    const int slots = hash_slots(K), pad = (K + 3) / 4 * 4;
+    ListView li;
+    li.table = reinterpret_cast<int32_t *>(slab + slab_bytes(slice, sizeof(InT)) - 128);
+    li.id = li.table + slots;
+    li.z = reinterpret_cast<float *>(li.id + pad);
+    li.a = li.z + pad;
+    li.value = li.a + pad;
+    for (int i = tid; i < slots; i += NA)
+        li.table[i] = -1;
     if (tid == 0) {
         for (int c = 0; c < kChunks; ++c)
             mbar_init_only(smem_u32(&sh.bar[c]), 1);
@@ -289,8 +314,8 @@ __global__ void __launch_bounds__(NT + 32)
     // The list, while the copy is in flight; a repeated id is found in the table.
     bool bad = false;
     for (int k = tid; k < K; k += NA) {
-        int id = a.ids[t * a.ld_list + k];
-        const float lp = a.lp[t * a.ld_list + k];
+        int id = k == tid ? id0 : ids[k];
+        const float lp = k == tid ? lp0 : lps[k];
         float z = 0.0f;
         if (id == -1 || lp == -INFINITY) {
             id = -1;
@@ -299,9 +324,9 @@ __global__ void __launch_bounds__(NT + 32)
             id = -1;
         } else {
             z = to_f32(reinterpret_cast<const InT *>(a.logits)[t * a.ld + id]);
-            unsigned h = ((unsigned)id * 2654435761u) >> 23;
-            for (int i = 0; i < kHash; ++i, h = (h + 1) & (kHash - 1)) {
-                const int32_t was = atomicCAS(&sh.table[h], -1, id);
+            unsigned h = ((unsigned)id * 2654435761u) >> 16 & (slots - 1);
+            for (int i = 0; i < slots; ++i, h = (h + 1) & (slots - 1)) {
+                const int32_t was = atomicCAS(&li.table[h], -1, id);
                 if (was == -1)
                     break;
                 if (was == id) {
@@ -310,9 +335,9 @@ __global__ void __launch_bounds__(NT + 32)
                 }
             }
         }
-        sh.id[k] = id;
-        sh.z[k] = z;
-        sh.a[k] = lp;
+        li.id[k] = id;
+        li.z[k] = z;
+        li.a[k] = lp;
     }
     bad = __syncthreads_or(bad) != 0;
     const float kappa = a.sc.kappa;
@@ -335,8 +360,8 @@ __global__ void __launch_bounds__(NT + 32)
     if (!list_warp) {
         landed();
         for (int k = tid; k < K; k += NT) {
-            const int64_t e = (int64_t)sh.id[k] - v0;
-            if (sh.id[k] >= 0 && e >= 0 && e < sl.n)
+            const int64_t e = (int64_t)li.id[k] - v0;
+            if (li.id[k] >= 0 && e >= 0 && e < sl.n)
                 poke_neg_inf<InT>(slab, sl.pad + (int)e);
         }
         sync_warps<NT>();
@@ -369,7 +394,7 @@ __global__ void __launch_bounds__(NT + 32)
         }
         __syncwarp();
         sw = __shfl_sync(kAll32, sw, 0);
-        ls = list_sums(sh, K, a.kind, a.sc);
+        ls = list_sums(li, K, a.kind, a.sc);
         cluster_wait();
         if (!mbar_wait_cluster(smem_u32(&sh.xbar), 0)) {
             if (tid == NT)
@@ -378,7 +403,7 @@ __global__ void __launch_bounds__(NT + 32)
         }
         cluster_arrive_relaxed();
         // The row's numbers, in every lane.
-        const MaxSum rest = combine_scaled(sh.part, cl.size, kappa);
+        const MaxSum rest = warp_combine(sh.part, cl.size, kappa);
         M = fmaxf(rest.m, ls.ms);
         float l, lr;
         const float xr = scaled_diff(rest.m, M, a.sc, lr), xs = scaled_diff(ls.ms, M, a.sc, l);
@@ -396,7 +421,7 @@ __global__ void __launch_bounds__(NT + 32)
                 qr = 0.0f;
                 Q = ls.qh + ls.ql;
             }
-            mult = er > 0.0f ? fmaf(-qr, S / er, Q) : 0.0f;
+            mult = er > 0.0f ? fmaf(-qr, S / er, Q) : 0.0f;  // (0 exactly where nothing is listed)
         } else {
             qr = fmaxf(qr, a.tail_min);
             if (ls.qh != ls.qh)
@@ -411,7 +436,8 @@ __global__ void __launch_bounds__(NT + 32)
             }
         }
         if (tid == NT)
-            sh.row = make_float2(M, S != S ? NAN : er == 0.0f ? 0.0f : sw * a.sc.hi * mult / S);
+            sh.row = make_float2(
+                M, S != S ? NAN : er == 0.0f ? 0.0f : __fdividef(sw * a.sc.hi * mult, S));
     }
     __syncthreads();
 
@@ -422,12 +448,12 @@ __global__ void __launch_bounds__(NT + 32)
         float sum = 0.0f;
 #pragma unroll 2
         for (int k = tid - NT; k < K; k += 32) {
-            const int64_t e = (int64_t)sh.id[k] - v0;
+            const int64_t e = (int64_t)li.id[k] - v0;
             const bool mine = grad && e >= 0 && e < sl.n;
-            if (sh.id[k] < 0 || !(first || mine))
+            if (li.id[k] < 0 || !(first || mine))
                 continue;
             float l, e1;
-            const float z = sh.z[k], lp = sh.a[k], x = scaled_diff(z, M, a.sc, l);
+            const float z = li.z[k], lp = li.a[k], x = scaled_diff(z, M, a.sc, l);
             const float u = two_sum(x, -logS, e1), ul = e1 + l - logSl;
             const float p = expf(u + ul);
             float lq = lp, lql = 0.0f;
@@ -444,7 +470,7 @@ __global__ void __launch_bounds__(NT + 32)
                     d = p == 0.0f ? 0.0f : p * (list_gap(z, lp, ls.ms, ls.c0, a.sc) - mean);
                 else
                     d = fmaf(Q, p, -q);
-                sh.value[k] = c * d;
+                li.value[k] = c * d;
             }
             if (first) {
                 float e2;
@@ -512,9 +538,9 @@ __global__ void __launch_bounds__(NT + 32)
     __syncthreads();  // the listed entries' values come after the zeros
     if (grad)
         for (int k = tid; k < K; k += NA) {
-            const int64_t e = (int64_t)sh.id[k] - v0;
-            if (sh.id[k] >= 0 && e >= 0 && e < sl.n)
-                orow[e] = from_float<OutT>(sh.value[k]);
+            const int64_t e = (int64_t)li.id[k] - v0;
+            if (li.id[k] >= 0 && e >= 0 && e < sl.n)
+                orow[e] = from_float<OutT>(li.value[k]);
         }
     cluster_wait();
 }
@@ -523,7 +549,7 @@ template <typename InT, typename OutT, int NT>
 cudaError_t launch_nt(const DistillArgs &a, const RowPlan &p, cudaStream_t s)
 {
     auto kern = cis_distill_kernel<InT, OutT, NT>;
-    const size_t smem = slab_bytes(p.slice, sizeof(InT));
+    const size_t smem = slab_bytes(p.slice, sizeof(InT)) + list_bytes(a.K);
     const cudaError_t e = cudaFuncSetAttribute(
         kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess)
