@@ -506,7 +506,124 @@ __global__ void __launch_bounds__(NT)
     }
 }
 
-// Any row, exactly: a cluster per row.
+// One row, exactly, by the CTAs of a cluster.  every: no first kernel has seen it.
+template <typename InT, int NT>
+__device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, bool every,
+                          int &turn)
+{
+    RowSelect<InT, NT> rs(sh, reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, turn);
+    const bool first = rs.rank == 0 && threadIdx.x == 0;
+    if (a.mask && a.mask[t] == 0) {
+        if (first)
+            write_row(a, t, -1, 0.0f, 0.0f);
+        return;
+    }
+    if (!sh.ready) {
+        __syncthreads();
+        fill_row_table(sh.table);
+        if (threadIdx.x == 0)
+            sh.ready = true;
+        __syncthreads();
+    }
+    const RowSettings rset = row_settings(a, t);
+    const int64_t k = rset.greedy ? 1 : rset.top_k;
+    const bool by_k = k > 0 && k < a.V, by_p = rset.top_p < 1.0f && !rset.greedy;
+    // The maximum: the first kernel's, where it has left the row, and the least entry is
+    // not needed
+    float M, bottom = -INFINITY;
+    if (!every && a.lps_out && !by_k) {
+        M = a.lps_out[t];
+    } else {
+        bool bad;
+        uint32_t least;
+        M = key_value(rs.max_key(least, bad));
+        bottom = key_value(least);
+        if (bad || !rset.ok) {  // as every CTA of the cluster finds
+            if (first) {
+                write_row(a, t, -1, NAN, NAN);
+                set_status(a.status, kStatusBadInput);
+            }
+            return;
+        }
+    }
+    const Scale &sc = rset.sc;
+    const RowMass mass(sh.table, M, rset.tau, sc);
+    const float depth = M - 31.0f * rset.tau, floor_z = bottom > depth ? bottom : depth;
+    // entries' weights in a selection: 1 each, or the mass of those above zk
+    bool count = false;
+    float zk = -INFINITY;
+    auto approx = [&](float z) {
+        return count ? 1.0f : (z > zk ? ex2_ftz((z - M) * sc.kappa) : 0.0f);
+    };
+    auto weight = [&](float z) {
+        return count ? (mass_t)1 : (z > zk ? mass(z) : (mass_t)0);
+    };
+    Kept kept{0, 0};
+    mass_t above, equal, gt, eq, gt0, eq0, target, wkey = 0;
+    bool parts = false;
+    // top_k first, then top_p: one place for both, as the selection's code is large
+#pragma unroll 1
+    for (int step = by_k ? 0 : 1; step < (by_p ? 2 : 1); ++step) {
+        count = step == 0;
+        float goal = (float)k, share = 0.0f, low = M - bottom > 1024.0f ? M - 64.0f : bottom;
+        target = (mass_t)k;
+        if (!count) {
+            low = floor_z;
+            if (by_k) {
+                rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
+                target = (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
+                if (target > gt) {  // within the entries at the key
+                    if (wkey)
+                        kept.ties = min(kept.ties, (target - gt + wkey - 1) / wkey);
+                    break;
+                }
+                goal = (float)mass_value(target);
+                zk = key_value(kept.key);
+            } else {
+                share = rset.top_p;
+            }
+        }
+        kept.key = rs.select(target, goal, share, low, M, approx, weight, above, equal, parts);
+        parts = parts && !count;
+        wkey = mass(key_value(kept.key));
+        kept.ties = count ? target - above : (target - above + wkey - 1) / wkey;
+    }
+    if (rset.min_p > 0.0f) {
+        const uint32_t low = min_p_key(M, rset.tau, rset.min_p);
+        if (kept.key < low) {
+            kept = Kept{low - 1, 0};
+            wkey = 0;
+            parts = false;
+        }
+    }
+    if (parts)
+        rs.kept_parts(gt, eq, gt0, eq0);
+    else
+        rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
+    const mass_t Z = gt + min(eq, kept.ties) * wkey;
+    target = (mass_t)((double)rset.u * (double)Z);
+    // the row's mass at temperature 1: the first kernel's, where it has left the row
+    float S1 = 0.0f;
+    if (a.lp_out && !every) {
+        S1 = a.lp_out[t];
+    } else if (a.lp_out) {
+        float s = 0.0f;
+        rs.each([&](int64_t, float z) { s += ex2_ftz((z - M) * kLog2e); });
+        mass_t sum = (mass_t)((double)s * (double)(1ull << kMassBits)), none = 0, x, y;
+        rs.cluster_sum(sum, none, x, y);
+        S1 = (float)mass_value(sum);
+    }
+    int64_t j = 0;
+    if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, mass, j) && threadIdx.x == 0) {
+        const float z = to_f32(rs.row[j]);
+        const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
+        write_row(a, t, (int32_t)j, log_share(z, M, one, S1),
+                  rset.greedy ? 0.0f : log_share(z, M, sc, (float)mass_value(Z)));
+    }
+    __syncthreads();
+}
+
+// Any row: a cluster per row.
 template <typename InT>
 __global__ void __launch_bounds__(kSelThreads, 2)
     cis_sample_exact_kernel(const __grid_constant__ SampleArgs a, bool every)
@@ -524,119 +641,353 @@ __global__ void __launch_bounds__(kSelThreads, 2)
         const int64_t t = rows.next([&](int64_t i) { return every || a.ids_out[i] == kTodo; });
         if (t < 0)
             break;
-        RowSelect<InT, kSelThreads> rs(sh, reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V,
-                                       turn);
-        const bool first = rs.rank == 0 && threadIdx.x == 0;
-        if (a.mask && a.mask[t] == 0) {
-            if (first)
-                write_row(a, t, -1, 0.0f, 0.0f);
+        exact_row<InT>(sh, a, t, every, turn);
+    }
+    cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
+}
+
+// bf16 rows, exactly, by counting: a row's entries take few values, and how many there are of
+// each is all that its filters and masses depend on.  One CTA a row: one pass counts the values
+// 2^-26 <= |z| < 2^8 and zero, a bin each in shared memory; 19 bins a thread then give the
+// masses in the order of the values, the kept set's end and the kept mass; a second pass
+// looks the kept entries' masses up, to find the warp's stretch, the thread's part and the entry
+// at which the running mass passes its goal.  Entries at or below -256 are left out where they
+// have no mass; a row with others outside the bins (or with none inside) goes to exact_row: of
+// rows of 151,936 entries from a bell of width 2.5 one in 400 (with bins from 2^-17 on every
+// third).
+//
+// Bound: shared-memory atomics and lookups, one of each an entry (32,000 and 37,000 cycles of
+// 92,000 a row of 151,936 entries).
+constexpr int kCountThreads = 512;
+constexpr int kLoBits = (127 - 26) << 7, kHiBits = (127 + 8) << 7;  // of bf16 magnitudes
+constexpr int kSide = kHiBits - kLoBits;   // bins of either sign
+constexpr int kZero = 2 * kSide, kValues = 2 * kSide + 1;
+// a thread's bins: an odd number, so that neighbouring threads are on different banks
+constexpr int kPer = (kValues + kCountThreads - 1) / kCountThreads | 1;
+
+struct CountShared {
+    SelectShared<kCountThreads> select;
+    alignas(16) mass_t mass[kValues];  // of one entry of a bin; 0: not kept
+    mass_t warps[2][kCountThreads / 32];
+    mass_t scan[kCountThreads];
+    mass_t gt, at;     // mass before the kept set's last bin, of an entry in it
+    mass_t ties;
+    int end;           // that bin's place in the order (kValues: no last bin)
+    int top;
+    uint32_t low;      // min_p's lowest key
+    int far[kCountThreads / 32];
+};
+static_assert(sizeof(int) * kValues <= sizeof(float) * kBins * kCountThreads,
+              "the counts fit the selection's columns");
+
+// The bin of a bf16's bits; -1: none.
+__device__ __forceinline__ int value_bin(uint32_t h)
+{
+    const uint32_t r = (h & 0x7fffu) - kLoBits;
+    return r < (uint32_t)kSide ? (int)(r + (h & 0x8000u ? kSide : 0))
+                               : ((h & 0x7fffu) == 0 ? kZero : -1);
+}
+// The bin at a place of the order (largest value first), and its value's bits.
+__device__ __forceinline__ int place_bin(int o)
+{
+    return o < kSide ? kSide - 1 - o : (o == kSide ? kZero : o - 1);
+}
+__device__ __forceinline__ float place_value(int o)
+{
+    if (o == kSide)
+        return 0.0f;
+    const uint32_t m = o < kSide ? kHiBits - 1 - o : kLoBits + (o - kSide - 1);
+    return __uint_as_float((m | (o < kSide ? 0u : 0x8000u)) << 16);
+}
+
+__global__ void __launch_bounds__(kCountThreads, 1)
+    cis_sample_counts_kernel(const __grid_constant__ SampleArgs a)
+{
+    constexpr int NT = kCountThreads, W = NT / 32, EV = 8;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
+    CountShared &sh = *reinterpret_cast<CountShared *>(dyn_smem);
+    int *count = reinterpret_cast<int *>(sh.select.cols);
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    int turn = 0;
+    if (tid == 0) {
+        allow_next_grid();
+        sh.select.ready = false;
+    }
+    grid_wait();
+    RowsLeft<NT> rows(sh.select, a.T, gridDim.x, blockIdx.x);
+    for (;;) {
+        const int64_t t = rows.next([&](int64_t i) { return a.ids_out[i] == kTodo; });
+        if (t < 0)
+            break;
+        const RowSettings rset = row_settings(a, t);
+        RowSelect<__nv_bfloat16, NT> rs(
+            sh.select, reinterpret_cast<const __nv_bfloat16 *>(a.logits) + t * a.ld, a.V, turn);
+        const uint4 *rv = reinterpret_cast<const uint4 *>(rs.row + rs.head);
+        const uint16_t *bits = reinterpret_cast<const uint16_t *>(rs.row);
+        if (!sh.select.ready) {
+            __syncthreads();
+            fill_row_table(sh.select.table);
+            if (tid == 0)
+                sh.select.ready = true;
+        }
+        for (int i = tid; i < kValues; i += NT)
+            count[i] = 0;
+        if (tid == 0)
+            sh.top = kValues;
+        __syncthreads();
+        // Counts.
+        bool odd = false;
+        float far = -INFINITY;
+        auto add = [&](uint32_t h) {
+            const int b = value_bin(h);
+            if (b >= 0) {
+                atomicAdd(&count[b], 1);
+            } else {
+                const float z = __uint_as_float(h << 16);
+                odd = odd || !(z <= -256.0f);  // small, large, +inf or NaN
+                far = fmaxf(far, z);
+            }
+        };
+        const int s0 = rs.seg(w), s1 = rs.seg(w + 1);
+        for (int v = s0 + lane; v < s1; v += 128) {
+            uint4 q[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                q[k] = v + 32 * k < s1 ? __ldg(rv + v + 32 * k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (v + 32 * k < s1) {
+                    const uint32_t x[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        add(x[i] & 0xffffu);
+                        add(x[i] >> 16);
+                    }
+                }
+        }
+        const int64_t tail = rs.head + (rs.V - rs.head) / EV * EV;  // the ragged ends
+        if (w == 0 && lane < rs.head)
+            add(bits[lane]);
+        if (w == W - 1 && lane >= 16 && tail + lane - 16 < rs.V)
+            add(bits[tail + lane - 16]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            far = fmaxf(far, __shfl_xor_sync(0xffffffffu, far, o));
+        if (lane == 0)
+            sh.far[w] = __float_as_int(far);
+        odd = __syncthreads_or(odd) != 0;
+        // The maximum.
+        const int o0 = min(kValues, tid * kPer), o1 = min(kValues, o0 + kPer);
+        for (int o = o0; o < o1; ++o)
+            if (count[place_bin(o)] > 0) {
+                atomicMin(&sh.top, o);
+                break;
+            }
+        for (int i = 0; i < W; ++i)
+            far = fmaxf(far, __int_as_float(sh.far[i]));
+        __syncthreads();
+        const float M = sh.top < kValues ? place_value(sh.top) : 0.0f;
+        if (odd || sh.top == kValues || far >= M - 32.0f * rset.tau) {
+            __syncthreads();
+            exact_row<__nv_bfloat16>(sh.select, a, t, false, turn);
             continue;
         }
-        if (!sh.ready) {
-            __syncthreads();
-            fill_row_table(sh.table);
-            if (threadIdx.x == 0)
-                sh.ready = true;
-            __syncthreads();
+        // Masses, and this thread's place in their order.
+        const RowMass mass(sh.select.table, M, rset.tau, rset.sc);
+        mass_t own = 0, n = 0;
+        for (int o = o0; o < o1; ++o) {
+            const int b = place_bin(o), c = count[b];
+            const mass_t m = mass(place_value(o));
+            sh.mass[b] = m;
+            own += c * m;
+            n += c;
         }
-        const RowSettings rset = row_settings(a, t);
+        mass_t before = own, place = n;  // inclusive sums, then those before
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const mass_t x = __shfl_up_sync(0xffffffffu, before, o);
+            const mass_t y = __shfl_up_sync(0xffffffffu, place, o);
+            before += lane >= o ? x : 0;
+            place += lane >= o ? y : 0;
+        }
+        if (lane == 31) {
+            sh.warps[0][w] = before;
+            sh.warps[1][w] = place;
+        }
+        __syncthreads();
+        mass_t total = 0, all = 0;
+        before -= own;
+        place -= n;
+        for (int i = 0; i < W; ++i) {
+            before += i < w ? sh.warps[0][i] : 0;
+            place += i < w ? sh.warps[1][i] : 0;
+            total += sh.warps[0][i];
+            all += sh.warps[1][i];
+        }
+        // The kept set: bins before `end`, and the first `ties` entries of that bin.
+        if (tid == 0) {
+            sh.end = kValues;
+            sh.ties = 0;
+            sh.gt = total;
+            sh.at = 0;
+        }
+        __syncthreads();
+        // f(place, mass before it, entries before it, its entries, an entry's mass)
+        auto places = [&](auto f) {
+            mass_t m = before, c = place;
+            for (int o = o0; o < o1; ++o) {
+                const int b = place_bin(o), k = count[b];
+                f(o, m, c, k, sh.mass[b]);
+                m += k * sh.mass[b];
+                c += k;
+            }
+        };
         const int64_t k = rset.greedy ? 1 : rset.top_k;
-        const bool by_k = k > 0 && k < a.V, by_p = rset.top_p < 1.0f && !rset.greedy;
-        // The maximum: the first kernel's, where it has left the row, and the least entry is
-        // not needed
-        float M, bottom = -INFINITY;
-        if (!every && a.lps_out && !by_k) {
-            M = a.lps_out[t];
-        } else {
-            bool bad;
-            uint32_t least;
-            M = key_value(rs.max_key(least, bad));
-            bottom = key_value(least);
-            if (bad || !rset.ok) {  // as every CTA of the cluster finds
-                if (first) {
-                    write_row(a, t, -1, NAN, NAN);
-                    set_status(a.status, kStatusBadInput);
+        if (k > 0 && (mass_t)k < all)
+            places([&](int o, mass_t m, mass_t c, int here, mass_t one) {
+                if (c < (mass_t)k && c + here >= (mass_t)k) {
+                    sh.end = o;
+                    sh.ties = (mass_t)k - c;
+                    sh.gt = m;
+                    sh.at = one;
                 }
-                continue;
-            }
-        }
-        const Scale &sc = rset.sc;
-        const RowMass mass(sh.table, M, rset.tau, sc);
-        const float depth = M - 31.0f * rset.tau, floor_z = bottom > depth ? bottom : depth;
-        // entries' weights in a selection: 1 each, or the mass of those above zk
-        bool count = false;
-        float zk = -INFINITY;
-        auto approx = [&](float z) {
-            return count ? 1.0f : (z > zk ? ex2_ftz((z - M) * sc.kappa) : 0.0f);
-        };
-        auto weight = [&](float z) {
-            return count ? (mass_t)1 : (z > zk ? mass(z) : (mass_t)0);
-        };
-        Kept kept{0, 0};
-        mass_t above, equal, gt, eq, gt0, eq0, target, wkey = 0;
-        bool parts = false;
-        // top_k first, then top_p: one place for both, as the selection's code is large
-#pragma unroll 1
-        for (int step = by_k ? 0 : 1; step < (by_p ? 2 : 1); ++step) {
-            count = step == 0;
-            float goal = (float)k, share = 0.0f, low = M - bottom > 1024.0f ? M - 64.0f : bottom;
-            target = (mass_t)k;
-            if (!count) {
-                low = floor_z;
-                if (by_k) {
-                    rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
-                    target = (mass_t)ceil((double)rset.top_p * (double)(gt + kept.ties * wkey));
-                    if (target > gt) {  // within the entries at the key
-                        if (wkey)
-                            kept.ties = min(kept.ties, (target - gt + wkey - 1) / wkey);
-                        break;
+            });
+        __syncthreads();
+        if (rset.top_p < 1.0f && !rset.greedy) {
+            const mass_t gt = sh.gt, at = sh.at, ties = sh.ties;
+            const mass_t target = (mass_t)ceil((double)rset.top_p * (double)(gt + ties * at));
+            __syncthreads();
+            if (target <= gt) {
+                places([&](int o, mass_t m, mass_t, int here, mass_t one) {
+                    if (m < target && m + here * one >= target) {
+                        sh.end = o;
+                        sh.ties = (target - m + one - 1) / one;
+                        sh.gt = m;
+                        sh.at = one;
                     }
-                    goal = (float)mass_value(target);
-                    zk = key_value(kept.key);
-                } else {
-                    share = rset.top_p;
-                }
+                });
+            } else if (tid == 0 && at) {
+                sh.ties = min(ties, (target - gt + at - 1) / at);
             }
-            kept.key = rs.select(target, goal, share, low, M, approx, weight, above, equal, parts);
-            parts = parts && !count;
-            wkey = mass(key_value(kept.key));
-            kept.ties = count ? target - above : (target - above + wkey - 1) / wkey;
+            __syncthreads();
         }
         if (rset.min_p > 0.0f) {
-            const uint32_t low = min_p_key(M, rset.tau, rset.min_p);
-            if (kept.key < low) {
-                kept = Kept{low - 1, 0};
-                wkey = 0;
-                parts = false;
+            if (tid == 0)
+                sh.low = min_p_key(M, rset.tau, rset.min_p);
+            const int end = sh.end;
+            __syncthreads();
+            const uint32_t low = sh.low;
+            places([&](int o, mass_t m, mass_t, int, mass_t) {
+                if (o <= end && order_key(place_value(o)) < low &&
+                    (o == 0 || order_key(place_value(o - 1)) >= low)) {
+                    sh.end = o;
+                    sh.ties = 0;
+                    sh.gt = m;
+                    sh.at = 0;
+                }
+            });
+            __syncthreads();
+        }
+        const int end = sh.end, kbin = end < kValues ? place_bin(end) : -1;
+        const mass_t at = sh.at, ties = sh.ties, Z = sh.gt + ties * at;
+        const mass_t goal = min((mass_t)((double)rset.u * (double)Z), Z - 1);
+        __syncthreads();
+        for (int o = max(o0, end); o < o1; ++o)  // the rest has no mass
+            sh.mass[place_bin(o)] = 0;
+        __syncthreads();
+        // The warps' stretches.
+        mass_t gt = 0, eq = 0;
+        const float least = end < kValues ? place_value(end) : -INFINITY;
+        auto look = [&](uint32_t h) {
+            if (__uint_as_float(h << 16) >= least) {
+                const int b = value_bin(h);
+                gt += b >= 0 ? sh.mass[b] : 0;
+                eq += b == kbin;
             }
+        };
+        auto look8 = [&](const uint4 &q) {
+            const uint32_t x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                look(x[i] & 0xffffu);
+                look(x[i] >> 16);
+            }
+        };
+        if (kbin < 0)
+            eq = 0;
+        for (int v = s0 + lane; v < s1; v += 64) {
+            const uint4 q0 = __ldg(rv + v);
+            const uint4 q1 = v + 32 < s1 ? __ldg(rv + v + 32) : make_uint4(0, 0, 0, 0);
+            look8(q0);
+            if (v + 32 < s1)
+                look8(q1);
         }
-        if (parts)
-            rs.kept_parts(gt, eq, gt0, eq0);
-        else
-            rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
-        const mass_t Z = gt + min(eq, kept.ties) * wkey;
-        target = (mass_t)((double)rset.u * (double)Z);
-        // the row's mass at temperature 1: the first kernel's, where it has left the row
-        float S1 = 0.0f;
-        if (a.lp_out && !every) {
-            S1 = a.lp_out[t];
-        } else if (a.lp_out) {
-            float s = 0.0f;
-            rs.each([&](int64_t, float z) { s += ex2_ftz((z - M) * kLog2e); });
-            mass_t sum = (mass_t)((double)s * (double)(1ull << kMassBits)), none = 0, x, y;
-            rs.cluster_sum(sum, none, x, y);
-            S1 = (float)mass_value(sum);
+        if (w == 0 && lane < rs.head)
+            look(bits[lane]);
+        if (w == W - 1 && lane >= 16 && tail + lane - 16 < rs.V)
+            look(bits[tail + lane - 16]);
+        rs.warp_sums(gt, eq);
+        if (lane == 0) {
+            sh.warps[0][w] = gt;
+            sh.warps[1][w] = kbin < 0 ? 0 : eq;
         }
-        int64_t j = 0;
-        if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, mass, j) && threadIdx.x == 0) {
-            const float z = to_f32(rs.row[j]);
+        __syncthreads();
+        auto upto = [&](mass_t g, mass_t e) { return g + min(e, ties) * at; };
+        mass_t g0 = 0, e0 = 0;
+        int sw = 0;
+        for (; sw < W - 1; ++sw) {
+            const mass_t g = g0 + sh.warps[0][sw], e = e0 + sh.warps[1][sw];
+            if (upto(g, e) > goal)
+                break;
+            g0 = g;
+            e0 = e;
+        }
+        // Within the stretch: consecutive entries a thread.
+        const int64_t f0 = rs.first(sw), f1 = rs.first(sw + 1);
+        const int64_t per = (f1 - f0 + NT - 1) / NT, j0 = min(f1, f0 + tid * per),
+                      j1 = min(f1, j0 + per);
+        gt = eq = 0;
+        for (int64_t j = j0; j < j1; ++j)
+            look(bits[j]);
+        if (kbin < 0)
+            eq = 0;
+        mass_t ig = gt, ie = eq;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const mass_t x = __shfl_up_sync(0xffffffffu, ig, o);
+            const mass_t y = __shfl_up_sync(0xffffffffu, ie, o);
+            ig += lane >= o ? x : 0;
+            ie += lane >= o ? y : 0;
+        }
+        __syncthreads();
+        if (lane == 31) {
+            sh.warps[0][w] = ig;
+            sh.warps[1][w] = ie;
+        }
+        __syncthreads();
+        ig += g0 - gt;
+        ie += e0 - eq;
+        for (int i = 0; i < w; ++i) {
+            ig += sh.warps[0][i];
+            ie += sh.warps[1][i];
+        }
+        if (upto(ig, ie) <= goal && upto(ig + gt, ie + eq) > goal) {
+            gt = ig;
+            eq = ie;
+            int64_t j = j0;
+            for (; j < j1; ++j) {
+                look(bits[j]);
+                if (upto(gt, kbin < 0 ? 0 : eq) > goal)
+                    break;
+            }
+            const float z = __uint_as_float((uint32_t)bits[j] << 16) + 0.0f;
             const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
+            const float S1 = a.lp_out ? a.lp_out[t] : 1.0f;
             write_row(a, t, (int32_t)j, log_share(z, M, one, S1),
-                      rset.greedy ? 0.0f : log_share(z, M, sc, (float)mass_value(Z)));
+                      rset.greedy ? 0.0f : log_share(z, M, rset.sc, (float)mass_value(Z)));
         }
         __syncthreads();
     }
-    cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
 
 template <typename InT, int NT, int kB>
@@ -690,6 +1041,27 @@ cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, cis_sample_exact_kernel<InT>, a, every);
 }
 
+// bf16 rows that the first kernel has left.
+inline cudaError_t launch_counts(const SampleArgs &a, cudaStream_t s)
+{
+    constexpr size_t smem = sizeof(CountShared);
+    const cudaError_t e = cudaFuncSetAttribute(
+        cis_sample_counts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.T < 152 ? a.T : 152));
+    cfg.blockDim = dim3(kCountThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, cis_sample_counts_kernel, a);
+}
+
 template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStream_t s)
 {
     const PassPlan p = pass_plan(a.T, a.V, (int)sizeof(InT));
@@ -698,7 +1070,12 @@ template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStrea
     const cudaError_t e = p.nt == 64  ? launch_fast<InT, 64, 1>(a, p, s)
                           : p.kb == 1 ? launch_fast<InT, 256, 1>(a, p, s)
                                       : launch_fast<InT, 256, 4>(a, p, s);
-    return e != cudaSuccess ? e : launch_exact<InT>(a, false, s);
+    if (e != cudaSuccess)
+        return e;
+    if constexpr (sizeof(InT) == 2)
+        return launch_counts(a, s);
+    else
+        return launch_exact<InT>(a, false, s);
 }
 
 }  // namespace

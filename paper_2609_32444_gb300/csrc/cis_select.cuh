@@ -440,7 +440,7 @@ template <int NT> struct RowsLeft {
 // stretch of them; the row is read from memory (L2 after the first time) once for each step.
 template <typename InT, int NT> struct RowSelect {
     static constexpr int EV = Vec<InT>::kN, W = NT / 32;
-    static_assert(NT == 256, "a histogram's bin a thread");
+    static_assert(NT >= 256, "a histogram's bin a thread");
     SelectShared<NT> &sh;
     cg::cluster_group cl;
     unsigned rank, size;
@@ -847,7 +847,8 @@ template <typename InT, int NT> struct RowSelect {
         uint32_t prefix = 0;
         mass_t over = 0;
         for (int shift = 24; shift >= 0; shift -= 8) {
-            sh.hist[threadIdx.x] = 0;
+            const int bin = threadIdx.x & 255;
+            sh.hist[bin] = 0;
             __syncthreads();
             each([&](int64_t, float z) {
                 const uint32_t k = order_key(z);
@@ -860,8 +861,8 @@ template <typename InT, int NT> struct RowSelect {
             cl.sync();
             mass_t s = 0;
             for (unsigned r = 0; r < size; ++r)
-                s += *peer(&sh.hist[threadIdx.x], r);
-            sh.tot[threadIdx.x] = s;
+                s += *peer(&sh.hist[bin], r);
+            sh.tot[bin] = s;
             __syncthreads();
             if (threadIdx.x < 32) {  // lane l: bins 255 - 8 l and the seven below it
                 const int lane = threadIdx.x;
