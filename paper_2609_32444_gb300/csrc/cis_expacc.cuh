@@ -29,13 +29,14 @@ __device__ __forceinline__ float exp2_accurate(float x)
 
 // Running (m, S[, U]) of one thread in the exponent form above; U = sum e x with
 // x = z log2e - c.  With |m| >= kHugeLogit x = (z - m) log2e and c is not used.
-// kScaled: a temperature, kappa = log2e / tau in the place of log2e (without kEnt).
+// kScaled: a temperature, kappa = log2e / tau in the place of log2e (without kEnt), and what the
+// growing sum's roundings lose in a sum of its own (6 operations a batch).
 template <bool kScaled> struct ExpScale {
     __device__ __forceinline__ static constexpr float kappa() { return kLog2e; }
     __device__ __forceinline__ static constexpr float huge() { return kHugeLogit; }
 };
 template <> struct ExpScale<true> {
-    float k, h;
+    float k, h, lost = 0.0f;
     __device__ __forceinline__ float kappa() const { return k; }
     __device__ __forceinline__ float huge() const { return h; }
 };
@@ -59,6 +60,8 @@ template <bool kEnt, bool kScaled = false> struct ExpAcc : ExpScale<kScaled> {
             if (kEnt)
                 U = f == 0.0f ? 0.0f : fmaf(d, S, U) * f;
             S = f == 0.0f ? 0.0f : S * f;
+            if constexpr (kScaled)
+                this->lost *= f;
             m = mx;
             c = c1;
         }
@@ -93,7 +96,13 @@ template <bool kEnt, bool kScaled = false> struct ExpAcc : ExpScale<kScaled> {
                 if (kEnt)
                     u[k] = __fadd2_rn(u[k], u[k + w]);
             }
-        S += s[0].x + s[0].y;
+        if constexpr (kScaled) {
+            float e;
+            S = two_sum(S, s[0].x + s[0].y, e);
+            this->lost += e;
+        } else {
+            S += s[0].x + s[0].y;
+        }
         if (kEnt)
             U += u[0].x + u[0].y;
     }
@@ -114,6 +123,8 @@ template <bool kEnt, bool kScaled = false> struct ExpAcc : ExpScale<kScaled> {
             return {m, 0.0f, 0.0f};
         const float err = fast() ? fmaf(m, kappa(), -c) : 0.0f;
         const float f = fast() ? exp2_accurate(-err) : 1.0f;
+        if constexpr (kScaled)
+            return {m, (S + this->lost) * f, 0.0f};
         return {m, S * f, kEnt ? f * kLn2 * fmaf(-err, S, U) : 0.0f};
     }
 };
@@ -147,6 +158,8 @@ __device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt, kScaled> &acc, M
     if (all.fast()) {
         d = acc.fast() ? acc.c - all.c : fmaf(acc.m, acc.kappa(), -all.c);
         t.s = acc.S;
+        if constexpr (kScaled)
+            t.s += acc.lost;
         t.u = acc.U;
     } else {
         d = acc.m == -INFINITY ? -INFINITY : (acc.m - M) * acc.kappa();
@@ -165,6 +178,8 @@ __device__ __forceinline__ MaxSumU block_exp(const ExpAcc<kEnt, kScaled> &acc, M
         red[wid].u = u;
     }
     __syncthreads();
+    if constexpr (kScaled)
+        all.lost = 0.0f;
     all.S = red[0].s;
     all.U = red[0].u;
 #pragma unroll

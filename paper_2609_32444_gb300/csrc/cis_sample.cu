@@ -15,12 +15,13 @@
 //                     whole CTA, the thread in whose part the running mass passes u Z;
 //   else              the row's candidates, sorted by the first CTA, with masses in whole
 //                     numbers (cis_select.cuh).
-// Masses of fp32 exponentials decide only where their error cannot matter: each is off by
-// less than 2^-20 (the exponential 2^-22, the rounding of an exponent of up to 16 and of
-// kappa), and the sums' roundings together by less than 2^-19, so that a running mass within
-// 2^-18 Z of its goal is left open.  Rows left open, and those with more candidates than fit
-// or a kept set that reaches beyond them, are left to the exact kernel that follows, which
-// takes every decision on whole numbers.
+// Masses of fp32 exponentials decide only where their error cannot matter.  Each is off by less
+// than 2^-20 (the exponential 2^-22, the rounding of an exponent of up to 16 and of kappa), and
+// the sums' roundings (the batches', the warps', the CTAs') by as much again, so that a running
+// mass C is off from u Z by less than 2^-19 ((1 - u) C + u (Z - C)): nearer to its goal than
+// that, it is left open.  Rows left open, and those with more candidates than fit or a kept set
+// that reaches beyond them, are left to a second kernel, which takes every decision on whole
+// numbers: bf16 rows by counting their values, fp32 rows by cis_select.cuh's selection.
 #include <math.h>
 
 #include "cis_nvtx.h"
@@ -54,7 +55,7 @@ __device__ __forceinline__ void write_row(const SampleArgs &a, int64_t t, int32_
 }
 
 constexpr int32_t kTodo = -2;  // as a row's id: left to the exact kernel
-constexpr float kOpen = 0x1p-18f;
+constexpr float kOpen = 0x1p-19f;
 constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
 constexpr int kAim = 256;      // candidates aimed at where top_k does not say
 
@@ -110,7 +111,7 @@ __device__ __forceinline__ float log_share(float z, float M, const Scale &sc, fl
 // is `base`, the warps' masses red[w].s * unit.  True and the index in the thread that has it.
 template <typename InT, int NT, int kB>
 __device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &ps, float base,
-                              float unit, float g, float M, float Z, const Scale &sc,
+                              float unit, float g, float u, float M, float Z, const Scale &sc,
                               unsigned rank, unsigned cs, int &index, float &zi)
 {
     constexpr int W = NT / 32, EV = Vec<InT>::kN;
@@ -154,7 +155,7 @@ __device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &
     for (int j = j0; j < j1; ++j) {
         const float z = to_f32(ps.row[j]), x = weight(z), next = part + x;
         if (lo + next > g && x > 0.0f) {
-            const float open = kOpen * Z;
+            const float open = 2.0f * kOpen * u * (1.0f - u) * Z + 0x1p-28f * Z;
             // before the row's first mass there is nothing to be off
             const bool sure = (lo + next) - g > open &&
                               (g - (lo + part) > open || (lo == 0.0f && part == 0.0f));
@@ -230,7 +231,7 @@ __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t
         } else {
             const double unit = (double)(1ull << kMassBits);
             goal = (double)rs.top_p * (double)Z * unit;
-            slack = (double)kOpen * (double)Z * unit;
+            slack = 2.0 * (double)kOpen * (double)Z * unit;  // (the candidates' masses are exact)
         }
         for (int i = tid; i < m; i += NT) {
             const double c = (double)mass[i], b = i ? (double)mass[i - 1] : 0.0;
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(NT)
         if (tid == 0)
             done = 0;
         __syncthreads();
-        if (draw_by_index<InT, NT, kB>(sh, ps, base, unit, goal, M, Z, rs.sc, rank, cs, j, z)) {
+        if (draw_by_index<InT, NT, kB>(sh, ps, base, unit, goal, rs.u, M, Z, rs.sc, rank, cs, j, z)) {
             write_row(a, t, j, log_share(z, M, one, S1), log_share(z, M, rs.sc, Z));
             done = 1;
         }
@@ -1072,10 +1073,12 @@ template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStrea
                                       : launch_fast<InT, 256, 4>(a, p, s);
     if (e != cudaSuccess)
         return e;
+    // Without a filter a row that is left needs one pass of masses, and eight CTAs are faster at
+    // that than one with its counts (T=256, V=151936: 65 us a call against 152).
     if constexpr (sizeof(InT) == 2)
-        return launch_counts(a, s);
-    else
-        return launch_exact<InT>(a, false, s);
+        if (a.top_k || a.top_p || a.min_p)
+            return launch_counts(a, s);
+    return launch_exact<InT>(a, false, s);
 }
 
 }  // namespace
