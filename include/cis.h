@@ -463,7 +463,8 @@ CIS_API cis_status_t cis_mismatch_diagnostics(const void *logits_train, const vo
  * A row with NaN, +inf or no finite logit, or a setting outside its range:
  * CIS_ERR_BAD_INPUT, id -1 and NaN.  Entries at -inf are never sampled.  The
  * decisions are taken on masses that are right to 2^-34 of each and 2^-44 of the
- * row's largest.  Deterministic.  Errors: CIS_ERR_INVALID_ARG for NULL required
+ * row's largest.  Deterministic.  The outputs may not overlap each other or the
+ * inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required
  * pointers, T < 0, V <= 0, ld < V, an unknown dtype or logits not aligned to
  * their type; CIS_ERR_UNSUPPORTED for V above 2^20.
  */

@@ -1097,7 +1097,8 @@ extern "C" CIS_API cis_status_t cis_sample_tokens(
         return CIS_ERR_INVALID_ARG;
     if (T == 0)
         return CIS_OK;
-    if (logits == nullptr || u == nullptr || ids_out == nullptr)
+    if (logits == nullptr || u == nullptr || ids_out == nullptr ||
+        (lp_out != nullptr && lp_out == lp_sampled_out))
         return CIS_ERR_INVALID_ARG;
     if (V > kMaxRowEntries)
         return CIS_ERR_UNSUPPORTED;

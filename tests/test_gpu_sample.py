@@ -197,6 +197,35 @@ def test_masked_vocabularies(dtype, fill):
         _check(z, u, **_named(8, s))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_sets_with_unusual_values(dtype):
+    """Kept sets beyond any list of candidates, with what a count of values has to look out for:
+    exact zeros, tiny values of both signs, entries at 256 and above, masked ones at -1e9 and
+    -inf, entries near -300 that weigh (a high temperature), a row of one value."""
+    T, V = 10, 30001
+    g = _gen(57)
+    z = _rows(T, V, dtype, g, 3, 1, width=1.0).contiguous()
+    z[1, ::3] = 0.0
+    z[2, ::5] = 1e-20
+    z[2, 1::5] = -1e-30
+    z[3] += 300
+    z[4, ::2] = -1e9
+    z[5, ::2] = -math.inf
+    z[6] -= 300
+    z[7] = 0.0
+    z[8] = -0.0
+    z[9, ::4] = z[9, ::4] * 1e-8
+    u = torch.rand(T, generator=g, device=DEV)
+    for s in ({"top_p": 0.9}, {"top_p": 0.5, "tau": 0.5}, {"top_k": 9001}, {"min_p": 0.02},
+              {"top_k": 20000, "top_p": 0.8, "min_p": 1e-3}, {"top_p": 0.95, "tau": 100.0},
+              {"top_p": 0.999, "min_p": 0.3, "tau": 2.0}):
+        _check(z, u, **_named(T, s), on_border=True)
+        mixed = _named(T, s)
+        mixed["top_p"] = mixed.get("top_p", _full(T, 1.0))
+        mixed["top_p"][:5] = 1.0  # rows without it beside the others
+        _check(z, u, **mixed, on_border=True)
+
+
 def test_extreme_rows():
     """Large magnitudes and temperatures, maxima far apart, rows at the lowest values."""
     V = 3000
