@@ -523,8 +523,15 @@ __global__ void __launch_bounds__(NT + 32)
             float z[W], v[W];
             load_w<InT, W>(slab, g, z);
 #pragma unroll
-            for (int i = 0; i < W; ++i)
-                v[i] = value(z[i]);
+            for (int i = 0; i < W; i += 2) {  // value(), two entries an instruction
+                const float2 x = __fmul2_rn(
+                    __fadd2_rn(make_float2(z[i], z[i + 1]), make_float2(-row.x, -row.x)),
+                    make_float2(kappa, kappa));
+                const float2 y = __fmul2_rn(make_float2(ex2_ftz(x.x), ex2_ftz(x.y)),
+                                            make_float2(row.y, row.y));
+                v[i] = y.x;
+                v[i + 1] = y.y;
+            }
             store_w<OutT, W>(orow + (W * g - sl.pad), v);
         }
         const int e0 = whole ? min(sl.n, g0 ? W * g0 - sl.pad : 0) : 0;

@@ -1,7 +1,6 @@
 // cis_slice.cuh -- one CTA's slice of a row in shared memory, for rows of any
-// alignment and length: the kernels that read a row several times (the distillation
-// loss, the teacher's lists, the sampler) split it over the CTAs of a cluster and hold
-// every slice on chip.
+// alignment and length: the distillation loss, which reads a row more than once, splits
+// it over the CTAs of a cluster and holds every slice on chip.
 //
 // The slab starts at the 8-entry boundary of global memory at or before the slice:
 // `pad` entries before the slice, and those after it up to a whole group of 8, are
@@ -49,12 +48,6 @@ template <typename InT> struct Slice {
     }
     __device__ __forceinline__ int chunk_begin(int c) const { return c * qg; }
     __device__ __forceinline__ int chunk_end(int c) const { return min(ng, (c + 1) * qg); }
-    // This thread's first group in chunk c, where group g is thread g % NT's.
-    template <int NT> __device__ __forceinline__ int first(int c) const
-    {
-        const int g0 = chunk_begin(c);
-        return g0 + (int)(threadIdx.x + NT - (unsigned)g0 % NT) % NT;
-    }
     // The 16-byte blocks inside the slice, as addresses.
     __device__ __forceinline__ void blocks(uintptr_t &a0, uintptr_t &a1) const
     {
