@@ -651,17 +651,19 @@ __global__ void __launch_bounds__(kSelThreads, 2)
 }
 
 // bf16 rows, exactly, by counting: a row's entries take few values, and how many there are of
-// each is all that its filters and masses depend on.  One CTA a row: one pass counts the values
-// 2^-26 <= |z| < 2^8 and zero, a bin each in shared memory; 19 bins a thread then give the
-// masses in the order of the values, the kept set's end and the kept mass; a second pass
-// looks the kept entries' masses up, to find the warp's stretch, the thread's part and the entry
-// at which the running mass passes its goal.  Entries at or below -256 are left out where they
+// each is all that its filters and masses depend on.  One CTA a row, or two or four where there
+// are few rows: one pass counts the values 2^-26 <= |z| < 2^8 and zero, a bin each in shared
+// memory (each CTA then adds up all the cluster's counts); 19 bins a thread give the masses in
+// the order of the values, the kept set's end and the kept mass; a second pass looks the kept
+// entries' masses up, to find the CTA, its warp's stretch, the thread's part and the entry at
+// which the running mass passes its goal.  Entries at or below -256 are left out where they
 // have no mass; a row with others outside the bins (or with none inside) goes to exact_row: of
 // rows of 151,936 entries from a bell of width 2.5 one in 400 (with bins from 2^-17 on every
 // third).
 //
 // Bound: shared-memory atomics and lookups, one of each an entry (32,000 and 37,000 cycles of
-// 92,000 a row of 151,936 entries).
+// 92,000 a row of 151,936 entries).  All 1,024 rows of that length take 300 us here; 64 of them
+// 63 us with two CTAs a row and 77 us with one.
 constexpr int kCountThreads = 512;
 constexpr int kLoBits = (127 - 26) << 7, kHiBits = (127 + 8) << 7;  // of bf16 magnitudes
 constexpr int kSide = kHiBits - kLoBits;   // bins of either sign
@@ -679,6 +681,8 @@ struct CountShared {
     int end;           // that bin's place in the order (kValues: no last bin)
     int top;
     uint32_t low;      // min_p's lowest key
+    bool odd;
+    float most;        // the largest entry left out
     int far[kCountThreads / 32];
 };
 static_assert(sizeof(int) * kValues <= sizeof(float) * kBins * kCountThreads,
@@ -718,7 +722,8 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         sh.select.ready = false;
     }
     grid_wait();
-    RowsLeft<NT> rows(sh.select, a.T, gridDim.x, blockIdx.x);
+    const ClusterPlace cl = cluster_place();
+    RowsLeft<NT> rows(sh.select, a.T, gridDim.x / cl.size, blockIdx.x / cl.size);
     for (;;) {
         const int64_t t = rows.next([&](int64_t i) { return a.ids_out[i] == kTodo; });
         if (t < 0)
@@ -770,9 +775,12 @@ __global__ void __launch_bounds__(kCountThreads, 1)
                 }
         }
         const int64_t tail = rs.head + (rs.V - rs.head) / EV * EV;  // the ragged ends
-        if (w == 0 && lane < rs.head)
+        const bool at_head = cl.rank == 0 && w == 0 && lane < rs.head;
+        const bool at_tail = cl.rank == cl.size - 1 && w == W - 1 && lane >= 16 &&
+                             tail + lane - 16 < rs.V;
+        if (at_head)
             add(bits[lane]);
-        if (w == W - 1 && lane >= 16 && tail + lane - 16 < rs.V)
+        if (at_tail)
             add(bits[tail + lane - 16]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
@@ -780,6 +788,37 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         if (lane == 0)
             sh.far[w] = __float_as_int(far);
         odd = __syncthreads_or(odd) != 0;
+        for (int i = 0; i < W; ++i)
+            far = fmaxf(far, __int_as_float(sh.far[i]));
+        if (cl.size > 1) {
+            // the other CTAs' counts to these, once all have read them
+            const cg::cluster_group cluster = cg::this_cluster();
+            if (tid == 0) {
+                sh.odd = odd;
+                sh.most = far;
+            }
+            cluster.sync();
+            int sum[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int b = tid + i * NT;
+                sum[i] = 0;
+                if (b < kValues)
+                    for (unsigned r = 0; r < cl.size; ++r)
+                        sum[i] += cluster.map_shared_rank(count, (int)r)[b];
+            }
+            for (unsigned r = 0; r < cl.size; ++r) {
+                const CountShared *peer = cluster.map_shared_rank(&sh, (int)r);
+                odd = odd || peer->odd;
+                far = fmaxf(far, peer->most);
+            }
+            cluster.sync();
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (tid + i * NT < kValues)
+                    count[tid + i * NT] = sum[i];
+            __syncthreads();
+        }
         // The maximum.
         const int o0 = min(kValues, tid * kPer), o1 = min(kValues, o0 + kPer);
         for (int o = o0; o < o1; ++o)
@@ -787,13 +826,12 @@ __global__ void __launch_bounds__(kCountThreads, 1)
                 atomicMin(&sh.top, o);
                 break;
             }
-        for (int i = 0; i < W; ++i)
-            far = fmaxf(far, __int_as_float(sh.far[i]));
         __syncthreads();
         const float M = sh.top < kValues ? place_value(sh.top) : 0.0f;
         if (odd || sh.top == kValues || far >= M - 32.0f * rset.tau) {
             __syncthreads();
             exact_row<__nv_bfloat16>(sh.select, a, t, false, turn);
+            cg::this_cluster().sync();  // before the columns are counts again
             continue;
         }
         // Masses, and this thread's place in their order.
@@ -930,9 +968,9 @@ __global__ void __launch_bounds__(kCountThreads, 1)
             if (v + 32 < s1)
                 look8(q1);
         }
-        if (w == 0 && lane < rs.head)
+        if (at_head)
             look(bits[lane]);
-        if (w == W - 1 && lane >= 16 && tail + lane - 16 < rs.V)
+        if (at_tail)
             look(bits[tail + lane - 16]);
         rs.warp_sums(gt, eq);
         if (lane == 0) {
@@ -942,13 +980,30 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         __syncthreads();
         auto upto = [&](mass_t g, mass_t e) { return g + min(e, ties) * at; };
         mass_t g0 = 0, e0 = 0;
+        if (cl.size > 1) {  // the CTAs before this one
+            const cg::cluster_group cluster = cg::this_cluster();
+            cluster.sync();
+            for (unsigned r = 0; r < cl.rank; ++r) {
+                const CountShared *peer = cluster.map_shared_rank(&sh, (int)r);
+                for (int i = 0; i < W; ++i) {
+                    g0 += peer->warps[0][i];
+                    e0 += peer->warps[1][i];
+                }
+            }
+            cluster.sync();
+        }
         int sw = 0;
-        for (; sw < W - 1; ++sw) {
+        bool here = upto(g0, e0) <= goal;
+        for (; sw < W; ++sw) {
             const mass_t g = g0 + sh.warps[0][sw], e = e0 + sh.warps[1][sw];
             if (upto(g, e) > goal)
                 break;
             g0 = g;
             e0 = e;
+        }
+        if (!here || sw == W) {  // in another CTA's part
+            __syncthreads();
+            continue;
         }
         // Within the stretch: consecutive entries a thread.
         const int64_t f0 = rs.first(sw), f1 = rs.first(sw + 1);
@@ -996,6 +1051,7 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         }
         __syncthreads();
     }
+    cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
 
 template <typename InT, int NT, int kB>
@@ -1032,7 +1088,8 @@ cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    const int64_t groups = a.T < 38 ? a.T : 38;  // two CTAs an SM
+    // two CTAs an SM are 38 clusters; four times as many share the rows that are left more evenly
+    const int64_t groups = a.T < 152 ? a.T : 152;
     cfg.gridDim = dim3((unsigned)(groups * kSelCluster));
     cfg.blockDim = dim3(kSelThreads);
     cfg.dynamicSmemBytes = smem;
@@ -1058,15 +1115,21 @@ inline cudaError_t launch_counts(const SampleArgs &a, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.T < 152 ? a.T : 152));
+    // Few rows: two or four CTAs each, as many as the SMs take (one a SM).
+    const int cs = a.T <= 38 ? 4 : a.T <= 76 ? 2 : 1;
+    cfg.gridDim = dim3((unsigned)((a.T < 152 ? a.T : 152) * cs));
     cfg.blockDim = dim3(kCountThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cs;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, cis_sample_counts_kernel, a);
 }
 
