@@ -662,8 +662,8 @@ __global__ void __launch_bounds__(kSelThreads, 2)
 // third).
 //
 // Bound: shared-memory atomics and lookups, one of each an entry (32,000 and 37,000 cycles of
-// 92,000 a row of 151,936 entries).  All 1,024 rows of that length take 300 us here; 64 of them
-// 63 us with two CTAs a row and 77 us with one.
+// 92,000 a row of 151,936 entries).  All 1,024 rows of that length take 300 us here; a call
+// with 64 of them 93 us with two CTAs a row and 114 with one.
 constexpr int kCountThreads = 512;
 constexpr int kLoBits = (127 - 26) << 7, kHiBits = (127 + 8) << 7;  // of bf16 magnitudes
 constexpr int kSide = kHiBits - kLoBits;   // bins of either sign
@@ -798,14 +798,12 @@ __global__ void __launch_bounds__(kCountThreads, 1)
                 sh.most = far;
             }
             cluster.sync();
-            int sum[kPer];
+            int sum[kPer] = {};
+            for (unsigned r = 0; r < cl.size; ++r) {
+                const int *theirs = cluster.map_shared_rank(count, (int)r);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int b = tid + i * NT;
-                sum[i] = 0;
-                if (b < kValues)
-                    for (unsigned r = 0; r < cl.size; ++r)
-                        sum[i] += cluster.map_shared_rank(count, (int)r)[b];
+                for (int i = 0; i < kPer; ++i)
+                    sum[i] += tid + i * NT < kValues ? theirs[tid + i * NT] : 0;
             }
             for (unsigned r = 0; r < cl.size; ++r) {
                 const CountShared *peer = cluster.map_shared_rank(&sh, (int)r);
