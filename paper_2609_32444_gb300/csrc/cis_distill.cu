@@ -58,7 +58,7 @@ struct ListShared {
     alignas(8) uint64_t xbar;
     alignas(16) float2 part[kMaxCluster];
     MaxSum red[16];
-    float2 row;  // the row's max and the rest's multiplier
+    float2 row;  // the rest's max (or the row's, without a rest) and its entries' multiplier
 };
 // The list, after the slab and sized by its length.
 struct ListView {
@@ -356,7 +356,9 @@ __global__ void __launch_bounds__(NT + 32)
 
     // The list warp's own: what the loss needs of the row.
     ListSums ls;
-    float M = 0.0f, S = 0.0f, er = 0.0f, es = 0.0f, qr = 0.0f, mean = 0.0f, Q = 1.0f, sw = 0.0f;
+    MaxSum rest{0.0f, 0.0f};
+    float M = 0.0f, S = 0.0f, er = 0.0f, es = 0.0f, pr = 0.0f, qr = 0.0f, mean = 0.0f, Q = 1.0f;
+    float sw = 0.0f;
     if (!list_warp) {
         landed();
         for (int k = tid; k < K; k += NT) {
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(NT + 32)
         }
         cluster_arrive_relaxed();
         // The row's numbers, in every lane.
-        const MaxSum rest = warp_combine(sh.part, cl.size, kappa);
+        rest = warp_combine(sh.part, cl.size, kappa);
         M = fmaxf(rest.m, ls.ms);
         float l, lr;
         const float xr = scaled_diff(rest.m, M, a.sc, lr), xs = scaled_diff(ls.ms, M, a.sc, l);
@@ -413,15 +415,18 @@ __global__ void __launch_bounds__(NT + 32)
         if (M == -INFINITY || ls.ms != ls.ms)
             S = NAN;  // no finite entry, or NaN among the listed
         qr = (1.0f - ls.qh) - ls.ql;
+        pr = er / S;
+        // The sum of the rest's gradients; each entry has its share e^{(z - max) / tau} / sum of
+        // it, which holds where p_r itself is below fp32's range.
         float mult = 0.0f;
         if (a.kind == CIS_DISTILL_TOPK) {
-            mult = ls.any ? 1.0f : 0.0f;
+            mult = ls.any ? pr : 0.0f;
         } else if (a.kind == CIS_DISTILL_FORWARD) {
             if (qr < a.tail_min) {
                 qr = 0.0f;
                 Q = ls.qh + ls.ql;
             }
-            mult = er > 0.0f ? fmaf(-qr, S / er, Q) : 0.0f;  // (0 exactly where nothing is listed)
+            mult = fmaf(Q, pr, -qr);  // (0 exactly where nothing is listed)
         } else {
             qr = fmaxf(qr, a.tail_min);
             if (ls.qh != ls.qh)
@@ -432,12 +437,13 @@ __global__ void __launch_bounds__(NT + 32)
                                                       ls.c0)
                                                : 0.0f;
                 mean = (ls.A * (es / ls.ss) + er * gr) / S;
-                mult = rest.s > 0.0f ? gr - mean : 0.0f;
+                mult = pr * (gr - mean);
             }
         }
         if (tid == NT)
             sh.row = make_float2(
-                M, S != S ? NAN : er == 0.0f ? 0.0f : __fdividef(sw * a.sc.hi * mult, S));
+                rest.m == -INFINITY ? M : rest.m,
+                S != S ? NAN : rest.s == 0.0f ? 0.0f : __fdividef(sw * a.sc.hi * mult, rest.s));
     }
     __syncthreads();
 
@@ -484,17 +490,18 @@ __global__ void __launch_bounds__(NT + 32)
         }
         if (first) {  // the row's loss
             sum = warp_sum_f(sum);
-            const float pr = er / S;
             float kl;
             if (a.kind == CIS_DISTILL_TOPK) {
                 kl = ls.any ? sum + pr : 0.0f;  // sum q - sum_S p = p_r
                 if (S != S)
                     kl = NAN;
             } else {
-                // d_r = log(q_r / p_r)
+                // d_r = log(q_r / p_r), from the logarithms where p_r leaves fp32's range
                 const float ratio = qr * (S / er);
-                const float dr =
-                    fabsf(ratio - 1.0f) < 0.25f ? log1pf(fmaf(qr, S / er, -1.0f)) : logf(ratio);
+                float l, dr = fabsf(ratio - 1.0f) < 0.25f ? log1pf(fmaf(qr, S / er, -1.0f))
+                                                          : logf(ratio);
+                if (er < 1e-30f && rest.s > 0.0f)
+                    dr = (logf(qr) - logf(rest.s) + logS) - (scaled_diff(rest.m, M, a.sc, l) + l);
                 if (a.kind == CIS_DISTILL_FORWARD)
                     kl = qr > 0.0f ? sum + bregman(qr, pr, dr)
                                    : sum + (((ls.qh - 1.0f) + ls.ql) + pr);

@@ -181,6 +181,39 @@ def test_temperatures(kind, tau):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("above", [60.0, 87.0, 95.0, 104.0, 300.0])
+def test_rest_far_below_the_list(kind, dtype, above):
+    """A rest whose probability is at, or far below, the end of fp32's range, and a teacher who
+    leaves it 0.3: the loss is finite, and the rest's gradients add up to -0.3 c (forward).
+    An entry's share of that is e^{(z - max of the rest) / tau} / sum, so its error is that of the
+    file's rule with the rest's maximum in M's place."""
+    g = _gen(11)
+    T, V, K, tau = 5, 5001, 16, 0.5
+    z = _rows(T, V, dtype, g, width=0.5)
+    ids = torch.stack([torch.randperm(V, generator=g, device=DEV)[:K] for _ in range(T)])
+    z.scatter_(1, ids, z.gather(1, ids) + above * tau)
+    lp = torch.log_softmax(torch.randn((T, K), generator=g, device=DEV), 1) + math.log(0.7)
+    ids = ids.int()
+    P = binding.cis_distill_default_params(kind, temperature=tau)
+    out = binding.cis_distill_fwd_bwd(z, ids, lp, P, dlogits_dtype=torch.float32)
+    L, grad, tol, tolL = _reference(z, ids, lp, kind, tau)
+    assert bool(torch.isfinite(L).all())
+    assert bool(((out["kl"].double() - L).abs() <= tolL + 2.0 ** -24 * L.abs()).all())
+    inside = torch.zeros((T, V), dtype=torch.bool, device=DEV).scatter_(1, ids.long(), True)
+    x = (z.double() / tau).masked_fill(inside, -math.inf)
+    rest = (x.amax(1, keepdim=True) - x).masked_fill(inside, 0.0)
+    tol = torch.where(inside, tol, grad.abs() * (2.0 ** -20 + 2.0 ** -22 * rest) + tol)
+    c = 1 / (T * tau)
+    off = (out["dlogits"].double() - c * grad).abs() - c * tol * (1 + 2.0 ** -24) \
+        - 2.0 ** -24 * c * grad.abs() - 2.0 ** -126
+    assert not bool((off > 0).any()), float(off.max())
+    if kind == "forward":
+        total = out["dlogits"].double().masked_fill(inside, 0.0).sum(1)
+        assert bool(((total + 0.3 * c).abs() < 2.0 ** -18 * c).all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_near_equal_distributions(kind):
     """Divergences far below their terms' size."""
     g = _gen(3)
