@@ -510,18 +510,11 @@ __global__ void __launch_bounds__(NT)
     }
 }
 
-// One row, exactly, by the CTAs of a cluster.  every: no first kernel has seen it.
+// One row that the first kernel has left, exactly, by the CTAs of a cluster.
 template <typename InT, int NT>
-__device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, bool every,
-                          int &turn)
+__device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, int &turn)
 {
     RowSelect<InT, NT> rs(sh, reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V, turn);
-    const bool first = rs.rank == 0 && threadIdx.x == 0;
-    if (a.mask && a.mask[t] == 0) {
-        if (first)
-            write_row(a, t, -1, 0.0f, 0.0f);
-        return;
-    }
     if (!sh.ready) {
         __syncthreads();
         fill_row_table(sh.table);
@@ -535,20 +528,12 @@ __device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, 
     // The maximum: the first kernel's, where it has left the row, and the least entry is
     // not needed
     float M, bottom = -INFINITY;
-    if (!every && a.lps_out && !by_k) {
+    if (a.lps_out && !by_k) {
         M = a.lps_out[t];
     } else {
-        bool bad;
         uint32_t least;
-        M = key_value(rs.max_key(least, bad));
+        M = key_value(rs.max_key(least));
         bottom = key_value(least);
-        if (bad || !rset.ok) {  // as every CTA of the cluster finds
-            if (first) {
-                write_row(a, t, -1, NAN, NAN);
-                set_status(a.status, kStatusBadInput);
-            }
-            return;
-        }
     }
     const Scale &sc = rset.sc;
     const RowMass mass(sh.table, M, rset.tau, sc);
@@ -607,16 +592,7 @@ __device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, 
     const mass_t Z = gt + min(eq, kept.ties) * wkey;
     target = (mass_t)((double)rset.u * (double)Z);
     // the row's mass at temperature 1: the first kernel's, where it has left the row
-    float S1 = 0.0f;
-    if (a.lp_out && !every) {
-        S1 = a.lp_out[t];
-    } else if (a.lp_out) {
-        float s = 0.0f;
-        rs.each([&](int64_t, float z) { s += ex2_ftz((z - M) * kLog2e); });
-        mass_t sum = (mass_t)((double)s * (double)(1ull << kMassBits)), none = 0, x, y;
-        rs.cluster_sum(sum, none, x, y);
-        S1 = (float)mass_value(sum);
-    }
+    const float S1 = a.lp_out ? a.lp_out[t] : 1.0f;
     int64_t j = 0;
     if (rs.locate(kept, wkey, min(target, Z - 1), gt0, eq0, mass, j) && threadIdx.x == 0) {
         const float z = to_f32(rs.row[j]);
@@ -627,10 +603,10 @@ __device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, 
     __syncthreads();
 }
 
-// Any row: a cluster per row.
+// The rows left, a cluster per row.
 template <typename InT>
 __global__ void __launch_bounds__(kSelThreads, 2)
-    cis_sample_exact_kernel(const __grid_constant__ SampleArgs a, bool every)
+    cis_sample_exact_kernel(const __grid_constant__ SampleArgs a)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
     SelectShared<kSelThreads> &sh = *reinterpret_cast<SelectShared<kSelThreads> *>(dyn_smem);
@@ -642,10 +618,10 @@ __global__ void __launch_bounds__(kSelThreads, 2)
     grid_wait();
     RowsLeft<kSelThreads> rows(sh, a.T, gridDim.x / kSelCluster, blockIdx.x / kSelCluster);
     for (;;) {
-        const int64_t t = rows.next([&](int64_t i) { return every || a.ids_out[i] == kTodo; });
+        const int64_t t = rows.next([&](int64_t i) { return a.ids_out[i] == kTodo; });
         if (t < 0)
             break;
-        exact_row<InT>(sh, a, t, every, turn);
+        exact_row<InT>(sh, a, t, turn);
     }
     cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
@@ -828,7 +804,7 @@ __global__ void __launch_bounds__(kCountThreads, 1)
         const float M = sh.top < kValues ? place_value(sh.top) : 0.0f;
         if (odd || sh.top == kValues || far >= M - 32.0f * rset.tau) {
             __syncthreads();
-            exact_row<__nv_bfloat16>(sh.select, a, t, false, turn);
+            exact_row<__nv_bfloat16>(sh.select, a, t, turn);
             cg::this_cluster().sync();  // before the columns are counts again
             continue;
         }
@@ -1076,9 +1052,9 @@ cudaError_t launch_fast(const SampleArgs &a, const PassPlan &p, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, kern, a, (unsigned)p.cs, kCap);
 }
 
-// The exact kernel: every row, or those that the fast one before it left.
+// The exact kernel.
 template <typename InT>
-cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
+cudaError_t launch_exact(const SampleArgs &a, cudaStream_t s)
 {
     constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
     const cudaError_t e = cudaFuncSetAttribute(
@@ -1100,8 +1076,8 @@ cudaError_t launch_exact(const SampleArgs &a, bool every, cudaStream_t s)
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = every ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, cis_sample_exact_kernel<InT>, a, every);
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, cis_sample_exact_kernel<InT>, a);
 }
 
 // bf16 rows that the first kernel has left.
@@ -1135,7 +1111,7 @@ template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStrea
 {
     const PassPlan p = pass_plan(a.T, a.V, (int)sizeof(InT));
     if (a.T * p.cs > 0x7fffffffLL)
-        return launch_exact<InT>(a, true, s);
+        return cudaErrorNotSupported;
     const cudaError_t e = p.nt == 64  ? launch_fast<InT, 64, 1>(a, p, s)
                           : p.kb == 1 ? launch_fast<InT, 256, 1>(a, p, s)
                                       : launch_fast<InT, 256, 4>(a, p, s);
@@ -1146,7 +1122,7 @@ template <typename InT> cudaError_t launch_sample(const SampleArgs &a, cudaStrea
     if constexpr (sizeof(InT) == 2)
         if (a.top_k || a.top_p || a.min_p)
             return launch_counts(a, s);
-    return launch_exact<InT>(a, false, s);
+    return launch_exact<InT>(a, s);
 }
 
 }  // namespace
@@ -1188,5 +1164,6 @@ extern "C" CIS_API cis_status_t cis_sample_tokens(
     const cudaError_t e = dtype == CIS_BF16
                               ? launch_sample<__nv_bfloat16>(a, (cudaStream_t)stream)
                               : launch_sample<float>(a, (cudaStream_t)stream);
-    return e == cudaSuccess ? CIS_OK : CIS_ERR_CUDA;
+    return e == cudaSuccess ? CIS_OK
+                            : (e == cudaErrorNotSupported ? CIS_ERR_UNSUPPORTED : CIS_ERR_CUDA);
 }

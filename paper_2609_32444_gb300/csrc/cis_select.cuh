@@ -584,14 +584,13 @@ template <typename InT, int NT> struct RowSelect {
         }
         buf ^= 1;
     }
-    // The row's largest key, and its least but that of -inf; bad: NaN, +inf or no finite entry.
-    __device__ uint32_t max_key(uint32_t &least, bool &bad)
+    // The row's largest key, and its least but that of -inf.
+    __device__ uint32_t max_key(uint32_t &least)
     {
         const uint32_t none = order_key(-INFINITY);
         uint32_t k = 0, l = 0xffffffffu;
         each([&](int64_t, float z) {
-            // (NaN as the largest)
-            const uint32_t q = z != z ? 0xffffffffu : order_key(z);
+            const uint32_t q = order_key(z);
             k = max(k, q);
             l = q > none ? min(l, q) : l;
         });
@@ -619,7 +618,6 @@ template <typename InT, int NT> struct RowSelect {
             b = min(b, p[1]);
         }
         buf ^= 1;
-        bad = a <= none || a >= order_key(INFINITY);
         least = (uint32_t)b;
         return (uint32_t)a;
     }

@@ -126,10 +126,10 @@ __global__ void __launch_bounds__(NT, kB == 4 ? 6 : 1)
     }
 }
 
-// Any row, exactly: a cluster per row reads it from memory once for each step.
+// The rows left, exactly: a cluster per row reads it from memory once for each step.
 template <typename InT>
 __global__ void __launch_bounds__(kSelThreads, 2)
-    cis_topk_exact_kernel(const __grid_constant__ TopkArgs a, bool every)
+    cis_topk_exact_kernel(const __grid_constant__ TopkArgs a)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
     SelectShared<kSelThreads> &sh = *reinterpret_cast<SelectShared<kSelThreads> *>(dyn_smem);
@@ -139,29 +139,13 @@ __global__ void __launch_bounds__(kSelThreads, 2)
     grid_wait();
     RowsLeft<kSelThreads> rows(sh, a.T, gridDim.x / kSelCluster, blockIdx.x / kSelCluster);
     for (;;) {
-        const int64_t t = rows.next([&](int64_t i) {
-            return every || a.ids_out[i * a.K] == kTodo;
-        });
+        const int64_t t = rows.next([&](int64_t i) { return a.ids_out[i * a.K] == kTodo; });
         if (t < 0)
             break;
         RowSelect<InT, kSelThreads> rs(sh, reinterpret_cast<const InT *>(a.logits) + t * a.ld, a.V,
                                        turn);
-        if (a.mask && a.mask[t] == 0) {
-            if (rs.rank == 0)
-                fill_row(a, t, -INFINITY, 0.0f);
-            continue;
-        }
-        bool bad;
         uint32_t least;
-        const uint32_t mk = rs.max_key(least, bad);
-        if (bad) {  // as every CTA of the cluster finds
-            if (rs.rank == 0) {
-                fill_row(a, t, NAN, NAN);
-                if (threadIdx.x == 0)
-                    set_status(a.status, kStatusBadInput);
-            }
-            continue;
-        }
+        const uint32_t mk = rs.max_key(least);
         const float M = key_value(mk), bottom = key_value(least);
         const int K = (int)(a.K < a.V ? a.K : a.V);
         mass_t above, equal;
@@ -255,9 +239,9 @@ cudaError_t launch_fast(const TopkArgs &a, const PassPlan &p, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, kern, a, (unsigned)p.cs, (a.K + p.cs - 1) / p.cs, cap);
 }
 
-// The exact kernel: every row, or those that the fast one before it left.
+// The exact kernel.
 template <typename InT>
-cudaError_t launch_exact(const TopkArgs &a, bool every, cudaStream_t s)
+cudaError_t launch_exact(const TopkArgs &a, cudaStream_t s)
 {
     constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
     const cudaError_t e = cudaFuncSetAttribute(
@@ -278,19 +262,19 @@ cudaError_t launch_exact(const TopkArgs &a, bool every, cudaStream_t s)
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = every ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, cis_topk_exact_kernel<InT>, a, every);
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, cis_topk_exact_kernel<InT>, a);
 }
 
 template <typename InT> cudaError_t launch_topk(const TopkArgs &a, cudaStream_t s)
 {
     const PassPlan p = pass_plan(a.T, a.V, (int)sizeof(InT));
     if (a.T * p.cs > 0x7fffffffLL)
-        return launch_exact<InT>(a, true, s);
+        return cudaErrorNotSupported;
     const cudaError_t e = p.nt == 64   ? launch_fast<InT, 64, 1>(a, p, s)
                           : p.kb == 1 ? launch_fast<InT, 256, 1>(a, p, s)
                                       : launch_fast<InT, 256, 4>(a, p, s);
-    return e != cudaSuccess ? e : launch_exact<InT>(a, false, s);
+    return e != cudaSuccess ? e : launch_exact<InT>(a, s);
 }
 
 }  // namespace
@@ -329,5 +313,6 @@ extern "C" CIS_API cis_status_t cis_topk_logprobs(const void *logits, int32_t dt
     const cudaError_t e = dtype == CIS_BF16
                               ? launch_topk<__nv_bfloat16>(a, (cudaStream_t)stream)
                               : launch_topk<float>(a, (cudaStream_t)stream);
-    return e == cudaSuccess ? CIS_OK : CIS_ERR_CUDA;
+    return e == cudaSuccess ? CIS_OK
+                            : (e == cudaErrorNotSupported ? CIS_ERR_UNSUPPORTED : CIS_ERR_CUDA);
 }
