@@ -464,9 +464,9 @@ CIS_API cis_status_t cis_mismatch_diagnostics(const void *logits_train, const vo
  * CIS_ERR_BAD_INPUT, id -1 and NaN.  Entries at -inf are never sampled.  The
  * decisions are taken on masses that are right to 2^-34 of each and 2^-44 of the
  * row's largest.  Deterministic.  The outputs may not overlap each other or the
- * inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required
- * pointers, T < 0, V <= 0, ld < V, an unknown dtype or logits not aligned to
- * their type; CIS_ERR_UNSUPPORTED for V above 2^20.
+ * inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, T < 0, V <= 0,
+ * ld < V, an unknown dtype or a pointer that is not aligned to its type;
+ * CIS_ERR_UNSUPPORTED for V above 2^20.
  */
 CIS_API cis_status_t cis_sample_tokens(const void *logits, int32_t dtype, int64_t T, int64_t V,
                                        int64_t ld, const float *u, const float *temperature,
@@ -492,8 +492,9 @@ CIS_API cis_status_t cis_sample_tokens(const void *logits, int32_t dtype, int64_
  *   dev_status  device int32 [1] or NULL: device status bits are OR-ed in.
  * A row with NaN, +inf or no finite logit: CIS_ERR_BAD_INPUT, ids -1 and NaN.
  * Deterministic.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, T < 0,
- * V <= 0, ld < V, an unknown dtype, logits not aligned to their type, K or the
- * temperature out of range; CIS_ERR_UNSUPPORTED for V above 2^20.
+ * V <= 0, ld < V, an unknown dtype, a pointer that is not aligned to its type, K
+ * or the temperature out of range; CIS_ERR_UNSUPPORTED for V above 2^20.  The
+ * outputs may not overlap each other or the inputs.
  */
 CIS_API cis_status_t cis_topk_logprobs(const void *logits, int32_t dtype, int64_t T, int64_t V,
                                        int64_t ld, int32_t K, double temperature,

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import operator
 import os
 import threading
 import warnings
@@ -573,6 +574,7 @@ def cis_sample_tokens(logits: torch.Tensor, u: torch.Tensor, temperature=None, t
                       (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
                       (min_p, torch.float32, "min_p"), (mask, torch.uint8, "mask")):
         _vec(x, dt, T, nm)
+    _status(dev_status)
     _on(dev, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, mask=mask,
         dev_status=dev_status)
     with torch.cuda.device(dev):
@@ -604,10 +606,11 @@ def cis_topk_logprobs(logits: torch.Tensor, K: int, temperature=1.0, mask=None, 
     if V > logits.shape[1]:
         raise ValueError("V is larger than the logits' rows")
     dev = logits.device
-    K = int(K)
+    K = operator.index(K)
     if not 1 <= K <= CIS_MAX_TOPK:
         raise ValueError(f"K must be between 1 and {CIS_MAX_TOPK}")
     _vec(mask, torch.uint8, T, "mask")
+    _status(dev_status)
     _on(dev, mask=mask, dev_status=dev_status)
     with torch.cuda.device(dev):
         ids = torch.empty((T, K), dtype=torch.int32, device=dev)
@@ -644,6 +647,11 @@ def _on(dev, **named):
     for name, x in named.items():
         if x is not None and x.device != dev:
             raise ValueError(f"{name} is on {x.device}, the logits on {dev}")
+
+
+def _status(x):
+    if x is not None and (x.dtype != torch.int32 or x.numel() < 1):
+        raise ValueError("dev_status must be an int32 tensor of 1 element")
 
 
 def _list(x, dtype, T, name):
@@ -696,6 +704,8 @@ def cis_distill_fwd_bwd(logits: torch.Tensor, top_ids: torch.Tensor, top_lp: tor
             raise ValueError("dlogits must be [T, >= V]")
     _on(dev, top_ids=top_ids, top_lp=top_lp, token_weight=token_weight, mask=mask,
         cu_seqlens=cu_seqlens, dlogits=dlogits, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     nws = cis_distill_workspace_size(T)
     with torch.cuda.device(dev):
         kl = torch.empty(T, dtype=torch.float32, device=dev)

@@ -639,7 +639,8 @@ CIS_API cis_status_t cis_distill_fwd_bwd(const void *logits, int32_t dtype, int6
 {
     NvtxRange nvtx_range("cis_distill_fwd_bwd");
     if (!row_args_ok(logits, dtype, T, V, ld) || K < 1 || K > CIS_MAX_TOPK || ld_top < K ||
-        !distill_params_ok(params))
+        !distill_params_ok(params) || !aligned4(top_ids, top_lp, token_weight, cu_seqlens, kl_out) ||
+        (reinterpret_cast<uintptr_t>(loss_out) & 7))
         return CIS_ERR_INVALID_ARG;
     const bool grad = dlogits != nullptr;
     if (grad && !row_args_ok(dlogits, dlogits_dtype, T, V, ld_out))

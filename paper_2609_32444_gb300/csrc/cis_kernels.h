@@ -71,6 +71,12 @@ inline bool row_args_ok(const void *p, int32_t dtype, int64_t T, int64_t V, int6
            (reinterpret_cast<uintptr_t>(p) & (dtype == CIS_BF16 ? 1 : 3)) == 0;
 }
 
+// Pointers to 4-byte elements, each aligned to them (null is).
+template <typename... P> inline bool aligned4(const P *...p)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0;
+}
+
 // One launch of the distillation loss (cis_distill.cu).
 struct DistillArgs {
     const void *logits;

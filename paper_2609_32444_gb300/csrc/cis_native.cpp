@@ -114,6 +114,11 @@ template <typename P> bool params_of(PyObject *o, const PyObject *type, P &p)
     PyBuffer_Release(&b);
     return ok;
 }
+// None, or a status word.
+bool status(const Tensor *t)
+{
+    return t == nullptr || (t->scalar_type() == at::kInt && t->numel() >= 1);
+}
 bool params(PyObject *o, cis_params_t &p) { return params_of(o, params_type, p); }
 // Every given tensor is on the device of x, and that is the current one.
 bool together(const Tensor &x, std::initializer_list<const Tensor *> ts)
@@ -432,7 +437,8 @@ PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!z || !u || !together(*z, {u, tau, k, p, m, mask, st}) || !rows(*z, T, ld) ||
         !dtype_code(z->scalar_type(), code) || !vocabulary(a[7], *z, V) ||
         !vec(u, at::kFloat, T) || !vec(tau, at::kFloat, T) || !vec(k, at::kInt, T) ||
-        !vec(p, at::kFloat, T) || !vec(m, at::kFloat, T) || !vec(mask, at::kByte, T))
+        !vec(p, at::kFloat, T) || !vec(m, at::kFloat, T) || !vec(mask, at::kByte, T) ||
+        !status(st))
         return none();
     const at::Device dev = z->device();
     const Tensor ids = fresh({T}, at::kInt, dev), lp = fresh_if(want_lp, T, at::kFloat, dev);
@@ -468,7 +474,7 @@ PyObject *topk_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
         return none();
     if (!z || !together(*z, {mask, st}) || !rows(*z, T, ld) ||
         !dtype_code(z->scalar_type(), code) || !vocabulary(a[4], *z, V) ||
-        !vec(mask, at::kByte, T) || K < 1 || K > CIS_MAX_TOPK)
+        !vec(mask, at::kByte, T) || !status(st) || K < 1 || K > CIS_MAX_TOPK)
         return none();
     const double tau = PyFloat_AS_DOUBLE(a[2]);
     const at::Device dev = z->device();
@@ -509,7 +515,8 @@ PyObject *distill_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         ldl != ldp || ids->size(1) != lp->size(1) || ids->scalar_type() != at::kInt ||
         lp->scalar_type() != at::kFloat || !vec(w, at::kFloat, T) || !vec(mask, at::kByte, T))
         return none();
-    if (cu && (cu->scalar_type() != at::kInt || cu->dim() != 1 || !cu->is_contiguous()))
+    if ((cu && (cu->scalar_type() != at::kInt || cu->dim() != 1 || !cu->is_contiguous())) ||
+        (ws_in && !ws_in->is_contiguous()))
         return none();
     at::ScalarType dt = z->scalar_type();
     if (a[8] != Py_None) {

@@ -1137,7 +1137,8 @@ extern "C" CIS_API cis_status_t cis_sample_tokens(
     int32_t *dev_status, void *stream)
 {
     NvtxRange nvtx_range("cis_sample_tokens");
-    if (!row_args_ok(logits, dtype, T, V, ld))
+    if (!row_args_ok(logits, dtype, T, V, ld) ||
+        !aligned4(u, temperature, top_k, top_p, min_p, ids_out, lp_out, lp_sampled_out, dev_status))
         return CIS_ERR_INVALID_ARG;
     if (T == 0)
         return CIS_OK;

@@ -290,7 +290,7 @@ extern "C" CIS_API cis_status_t cis_topk_logprobs(const void *logits, int32_t dt
 {
     NvtxRange nvtx_range("cis_topk_logprobs");
     if (!row_args_ok(logits, dtype, T, V, ld) || K < 1 || K > CIS_MAX_TOPK ||
-        !temperature_ok(temperature))
+        !temperature_ok(temperature) || !aligned4(ids_out, lp_out, lse_out, dev_status))
         return CIS_ERR_INVALID_ARG;
     if (T == 0)
         return CIS_OK;

@@ -52,14 +52,18 @@ ROWS = [dict(T=-1), dict(V=0), dict(V=-3), dict(ld=7), dict(dt=2), dict(dt=-1), 
         dict(T=1 << 31), dict(V=1 << 31, ld=1 << 31)]
 
 
-@pytest.mark.parametrize("over", ROWS + [dict(u=None), dict(ids=None), dict(lp=OTHER, lps=OTHER)])
+ODD = ctypes.c_void_p(0x30002)
+
+
+@pytest.mark.parametrize("over", ROWS + [dict(u=None), dict(ids=None), dict(lp=OTHER, lps=OTHER),
+                                         dict(u=ODD), dict(ids=ODD), dict(lp=ODD), dict(lps=ODD)])
 def test_sample_refuses(binding, over):
     assert _sample(binding, **over) == INVALID
 
 
 @pytest.mark.parametrize("over", ROWS + [
     dict(ids=None), dict(lp=None), dict(K=0), dict(K=257), dict(K=-1), dict(tau=0.0),
-    dict(tau=-1.0), dict(tau=9e-4), dict(tau=1001.0), dict(tau=float("nan")),
+    dict(ids=ODD), dict(lp=ODD), dict(tau=-1.0), dict(tau=9e-4), dict(tau=1001.0), dict(tau=float("nan")),
     dict(tau=float("inf"))])
 def test_topk_refuses(binding, over):
     assert _topk(binding, **over) == INVALID
@@ -68,7 +72,7 @@ def test_topk_refuses(binding, over):
 @pytest.mark.parametrize("over", ROWS + [
     dict(ids=None), dict(lp=None), dict(K=0), dict(K=257), dict(K=4), dict(ldo=7), dict(dzt=3),
     dict(dz=ctypes.c_void_p(0x4000001)), dict(dz=ctypes.c_void_p(0x10010)), dict(ws=None),
-    dict(ws=ctypes.c_void_p(0x20040)), dict(nws=64),
+    dict(ws=ctypes.c_void_p(0x20040)), dict(nws=64), dict(ids=ODD), dict(lp=ODD), dict(cu=ODD),
     dict(params=dict(kind=3)), dict(params=dict(kind=-1)), dict(params=dict(agg=2)),
     dict(params=dict(agg=1)), dict(params=dict(temperature=0.0)),
     dict(params=dict(temperature=float("nan"))), dict(params=dict(coef=float("inf"))),

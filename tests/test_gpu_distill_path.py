@@ -155,6 +155,10 @@ def test_binding_refuses():
         lambda: sample(z.t(), u), lambda: sample(z, u.cpu()), lambda: sample(z, u, top_k=u),
         lambda: sample(z, u, temperature=k), lambda: sample(z, u, V=778),
         lambda: sample(z, u, V=0), lambda: sample(z, u, mask=u), lambda: sample(z[0], u),
+        lambda: sample(z, u, dev_status=k.byte()), lambda: sample(z, u, dev_status=k[:0]),
+        lambda: topk(z, 3, dev_status=u), lambda: topk(z, 2.5),
+        lambda: distill(z, ids, lp, P, workspace=torch.zeros(
+            1, dtype=torch.uint8, device=DEV).expand(1 << 20)),
         lambda: topk(z, 0), lambda: topk(z, 257), lambda: topk(z, 3, 0.0),
         lambda: topk(z, 3, math.nan), lambda: topk(z, 3, V=1000), lambda: topk(z.int(), 3),
         lambda: distill(z, ids.long(), lp, P), lambda: distill(z, ids, lp.double(), P),
