@@ -733,23 +733,37 @@ __global__ void __launch_bounds__(kCountThreads, 1)
                 far = fmaxf(far, z);
             }
         };
-        const int s0 = rs.seg(w), s1 = rs.seg(w + 1);
-        for (int v = s0 + lane; v < s1; v += 128) {
-            uint4 q[4];
+        // f(bits) for the entries of the warp's stretch, four vectors a lane ahead of their use
+        auto stretch = [&](auto f) {
+            constexpr int kN = 4;
+            const int s1 = rs.seg(w + 1);
+            auto load = [&](uint4 (&q)[kN], int v) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                q[k] = v + 32 * k < s1 ? __ldg(rv + v + 32 * k) : make_uint4(0, 0, 0, 0);
+                for (int k = 0; k < kN; ++k)
+                    q[k] = v + 32 * k < s1 ? __ldg(rv + v + 32 * k) : make_uint4(0, 0, 0, 0);
+            };
+            uint4 q[kN], next[kN];
+            int v = rs.seg(w) + lane;
+            load(q, v);
+#pragma unroll 1
+            for (; v < s1; v += 32 * kN) {
+                load(next, v + 32 * kN);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (v + 32 * k < s1) {
-                    const uint32_t x[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+                for (int k = 0; k < kN; ++k)
+                    if (v + 32 * k < s1) {
+                        const uint32_t x[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        add(x[i] & 0xffffu);
-                        add(x[i] >> 16);
+                        for (int i = 0; i < 4; ++i) {
+                            f(x[i] & 0xffffu);
+                            f(x[i] >> 16);
+                        }
                     }
-                }
-        }
+#pragma unroll
+                for (int k = 0; k < kN; ++k)
+                    q[k] = next[k];
+            }
+        };
+        stretch(add);
         const int64_t tail = rs.head + (rs.V - rs.head) / EV * EV;  // the ragged ends
         const bool at_head = cl.rank == 0 && w == 0 && lane < rs.head;
         const bool at_tail = cl.rank == cl.size - 1 && w == W - 1 && lane >= 16 &&
@@ -925,23 +939,7 @@ __global__ void __launch_bounds__(kCountThreads, 1)
                 eq += b == kbin;
             }
         };
-        auto look8 = [&](const uint4 &q) {
-            const uint32_t x[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                look(x[i] & 0xffffu);
-                look(x[i] >> 16);
-            }
-        };
-        if (kbin < 0)
-            eq = 0;
-        for (int v = s0 + lane; v < s1; v += 64) {
-            const uint4 q0 = __ldg(rv + v);
-            const uint4 q1 = v + 32 < s1 ? __ldg(rv + v + 32) : make_uint4(0, 0, 0, 0);
-            look8(q0);
-            if (v + 32 < s1)
-                look8(q1);
-        }
+        stretch(look);
         if (at_head)
             look(bits[lane]);
         if (at_tail)
