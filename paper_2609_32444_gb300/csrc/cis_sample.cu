@@ -54,7 +54,8 @@ __device__ __forceinline__ void write_row(const SampleArgs &a, int64_t t, int32_
     if (a.lps_out) a.lps_out[t] = lps;
 }
 
-constexpr int32_t kTodo = -2;  // as a row's id: left to the exact kernel
+constexpr int32_t kTodo = -2;   // as a row's id: left to the second kernel
+constexpr int32_t kTaken = -3;  // which has begun with it
 constexpr float kOpen = 0x1p-19f;
 constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
 constexpr int kAim = 256;      // candidates aimed at where top_k does not say
@@ -660,6 +661,8 @@ struct CountShared {
     bool odd;
     float most;        // the largest entry left out
     int far[kCountThreads / 32];
+    int next[kCountThreads / 32];
+    bool got;
 };
 static_assert(sizeof(int) * kValues <= sizeof(float) * kBins * kCountThreads,
               "the counts fit the selection's columns");
@@ -684,6 +687,54 @@ __device__ __forceinline__ float place_value(int o)
     return __uint_as_float((m | (o < kSide ? 0u : 0x8000u)) << 16);
 }
 
+// The rows left, one at a time to whichever CTA is free: which rows are left, and so how many
+// of a fixed share of them, is up to the data (with fixed shares of 1,024 rows of which half
+// were left, the busiest SM had 2.3 times the mean's work: 308 us).  A CTA looks for marks from
+// a place of its own on, 8 a thread at a time, and takes the first row by exchanging its mark;
+// what a row's outputs are does not depend on the CTA.
+struct RowClaims {
+    static constexpr int NT = kCountThreads, kN = 8;
+    CountShared &sh;
+    int64_t T, first, base = 0;
+
+    __device__ __forceinline__ int64_t row(int64_t i) const
+    {
+        return first + i < T ? first + i : first + i - T;
+    }
+    __device__ int64_t next(int32_t *marks)
+    {
+        const int tid = threadIdx.x;
+        while (base < T) {
+            int best = NT * kN;
+#pragma unroll
+            for (int k = kN - 1; k >= 0; --k) {
+                const int64_t i = base + tid + k * NT;
+                if (i < T && __ldcg(marks + row(i)) == kTodo)
+                    best = tid + k * NT;
+            }
+            best = __reduce_min_sync(0xffffffffu, best);
+            __syncthreads();
+            if ((tid & 31) == 0)
+                sh.next[tid >> 5] = best;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NT / 32; ++w)
+                best = min(best, sh.next[w]);
+            if (best == NT * kN) {  // no mark comes back
+                base += NT * kN;
+                continue;
+            }
+            const int64_t t = row(base + best);
+            if (tid == 0)
+                sh.got = atomicCAS(marks + t, kTodo, kTaken) == kTodo;
+            __syncthreads();
+            if (sh.got)
+                return t;
+        }
+        return -1;
+    }
+};
+
 __global__ void __launch_bounds__(kCountThreads, 1)
     cis_sample_counts_kernel(const __grid_constant__ SampleArgs a)
 {
@@ -699,9 +750,13 @@ __global__ void __launch_bounds__(kCountThreads, 1)
     }
     grid_wait();
     const ClusterPlace cl = cluster_place();
-    RowsLeft<NT> rows(sh.select, a.T, gridDim.x / cl.size, blockIdx.x / cl.size);
+    const int64_t groups = gridDim.x / cl.size, group = blockIdx.x / cl.size;
+    RowsLeft<NT> own(sh.select, a.T, groups, group);
+    RowClaims any{sh, a.T, group * a.T / groups};
     for (;;) {
-        const int64_t t = rows.next([&](int64_t i) { return a.ids_out[i] == kTodo; });
+        const int64_t t = a.T <= groups
+                              ? own.next([&](int64_t i) { return a.ids_out[i] == kTodo; })
+                              : any.next(a.ids_out);
         if (t < 0)
             break;
         const RowSettings rset = row_settings(a, t);

@@ -281,6 +281,45 @@ def test_rows_that_cannot_be_sampled():
             bad(z, u, **{name: s})
 
 
+@pytest.mark.parametrize("T", [153, 1000, 4700, 9000])
+def test_many_rows_with_some_left(T):
+    """More rows than CTAs, of which an uneven part, in runs, has a nucleus that no list holds:
+    the same as in calls of a few rows, and every seventieth against the reference.  Masked rows
+    and rows that cannot be sampled are among them."""
+    V = 2501
+    g = _gen(T)
+    z = _rows(T, V, torch.bfloat16, g, width=0.3)
+    i = torch.arange(T, device=DEV)
+    peaked = (i // 61) % 3 == 0
+    z[peaked, 17] = 14.0
+    z[5::977, 3] = math.nan
+    mask = (i % 11 != 10).to(torch.uint8)
+    u = torch.rand(T, generator=g, device=DEV)
+    p, tau = _full(T, 0.93), _full(T, 0.8)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ids, lp, lps = binding.cis_sample_tokens(z, u, temperature=tau, top_p=p, mask=mask,
+                                             want_lp_sampled=True, dev_status=st)
+    assert int(st) == binding.CIS_ERR_BAD_INPUT
+    bad = torch.zeros(T, dtype=torch.bool, device=DEV)
+    bad[5::977] = True
+    on = (mask != 0) & ~bad
+    assert bool((ids[~on] == -1).all()) and bool(((ids >= 0) & (ids < V))[on].all())
+    for n in (30, 100):
+        for a in list(range(0, T, n))[:40]:
+            c = slice(a, a + n)
+            few = binding.cis_sample_tokens(z[c], u[c], temperature=tau[c], top_p=p[c],
+                                            mask=mask[c], want_lp_sampled=True)
+            assert torch.equal(few[0], ids[c]), (n, a)
+            for x, y in zip(few[1:], (lp[c], lps[c])):
+                assert bool(((x - y).abs() <= 2.0 ** -19)[on[c]].all())
+    r = on.nonzero().view(-1)[::70]
+    want, wlp, wlps, near = _reference(z[r], u[r], tau[r], None, p[r])
+    assert near > 2.0 ** -32
+    assert torch.equal(ids[r].long(), want)
+    assert float((lp[r].double() - wlp).abs().max()) <= 2.0 ** -19
+    assert float((lps[r].double() - wlps).abs().max()) <= 2.0 ** -19
+
+
 def test_frequencies():
     """20,000 draws from one small distribution: each count is binomial, so its distance
     from n p is below 5 sqrt(n p (1 - p)) + 1."""
