@@ -22,6 +22,12 @@
 // that, it is left open.  Rows left open, and those with more candidates than fit or a kept set
 // that reaches beyond them, are left to a second kernel, which takes every decision on whole
 // numbers: bf16 rows by counting their values, fp32 rows by cis_select.cuh's selection.
+//
+// Bound: instruction issue in the first kernel (two exponentials an entry where the temperature is
+// not 1; four CTAs of 60 registers an SM, and forcing five into 48 took 126 us a call for 110 at
+// T=1024, V=151936, top-k), and the rows left.  T=1024, V=151936, top-p at temperature 0.7: 118 us
+// and, for the half of the rows that is left, 165; T=256, nothing cut off: 25 us and 31 for 3% of
+// the rows, a row's steps one after another on eight CTAs; T=1, top-k and top-p: 23 us a call.
 #include <math.h>
 
 #include "cis_nvtx.h"
@@ -638,9 +644,10 @@ __global__ void __launch_bounds__(kSelThreads, 2)
 // rows of 151,936 entries from a bell of width 2.5 one in 400 (with bins from 2^-17 on every
 // third).
 //
-// Bound: shared-memory atomics and lookups, one of each an entry (32,000 and 37,000 cycles of
-// 92,000 a row of 151,936 entries).  All 1,024 rows of that length take 300 us here; a call
-// with 64 of them 93 us with two CTAs a row and 114 with one.
+// Bound: the passes' dependent steps an entry (bin, then an atomic or a lookup in shared memory)
+// on the 16 warps that the counts and the registers leave room for: 32,000 and 37,000 of a row's
+// 92,000 cycles (151,936 entries), 0.45 instructions a cycle and scheduler.  A call with 64 such
+// rows takes 93 us with two CTAs a row and 114 with one.
 constexpr int kCountThreads = 512;
 constexpr int kLoBits = (127 - 26) << 7, kHiBits = (127 + 8) << 7;  // of bf16 magnitudes
 constexpr int kSide = kHiBits - kLoBits;   // bins of either sign

@@ -7,8 +7,11 @@
 // with more candidates than fit (long runs of equal entries) is left to the exact kernel,
 // which follows.
 //
-// Before (slices of the row in the shared memory of four CTAs, read three times): T=8192,
-// V=151936, K=64 took 1336 us, at 16 warps an SM and 4900 issue slots a slice.
+// Bound: HBM and instruction issue (64%) for many long rows, six CTAs an SM: T=8192, V=151936,
+// K=64 takes 451 us, 5.5 TB/s.  Short rows and few rows wait for a row's last steps (the bound,
+// the candidates, their order), in which a CTA loads next to nothing: T=2048, V=32003 fp32,
+// K=128 65 us, 3.1 TB/s of the rows that are read; T=24, V=151936, K=20 16 us.  Slices of the row
+// in the shared memory of four CTAs, read three times, took 1336 us at the first of these sizes.
 #include <math.h>
 
 #include "cis_nvtx.h"
