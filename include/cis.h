@@ -566,7 +566,7 @@ CIS_API cis_status_t cis_distill_workspace_size(int64_t T, size_t *bytes);
  * logit gives NaN.  Deterministic.  Errors: as cis_loss_fwd_bwd, plus
  * CIS_ERR_INVALID_ARG for K or parameters out of range, ld_top < K or a pointer
  * that is not aligned to its type, and CIS_ERR_UNSUPPORTED for V above 819200
- * (bf16 logits) or 409600 (fp32).
+ * (bf16 logits) or 409600 (fp32), or T of 2^28 or more.
  */
 CIS_API cis_status_t cis_distill_fwd_bwd(const void *logits, int32_t dtype, int64_t T, int64_t V,
                                          int64_t ld, const int32_t *top_ids, const float *top_lp,

@@ -89,6 +89,8 @@ def test_rows_that_are_too_long(binding):
     far = ctypes.c_void_p(0x40000000)
     assert _distill(binding, V=819208, ld=819208, ldo=819208, dz=far) == UNSUPPORTED
     assert _distill(binding, dt=0, V=409608, ld=409608, ldo=409608, dz=far) == UNSUPPORTED
+    n = 1 << 28
+    assert _distill(binding, T=n, V=1, ld=1, ldo=1, dz=far, nws=1 << 40) == UNSUPPORTED
 
 
 def test_no_rows_is_no_work(binding):
