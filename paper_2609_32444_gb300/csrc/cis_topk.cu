@@ -8,7 +8,7 @@
 // which follows.
 //
 // Bound: HBM and instruction issue (64%) for many long rows, six CTAs an SM: T=8192, V=151936,
-// K=64 takes 451 us, 5.5 TB/s.  Short rows and few rows wait for a row's last steps (the bound,
+// K=64 takes 440 us, 5.7 TB/s.  Short rows and few rows wait for a row's last steps (the bound,
 // the candidates, their order), in which a CTA loads next to nothing: T=2048, V=32003 fp32,
 // K=128 65 us, 3.1 TB/s of the rows that are read; T=24, V=151936, K=20 16 us.  Slices of the row
 // in the shared memory of four CTAs, read three times, took 1336 us at the first of these sizes.
@@ -35,8 +35,14 @@ constexpr int32_t kTodo = -2;  // in a row's first id: left to the exact kernel
 // r = ceil(K / CTAs of the row); cap: items and candidates that fit, a power of two.  Dynamic
 // shared memory: cap candidates, cap items, the batches' maxima (and, in their place, the
 // candidates of all CTAs).
-template <typename InT, int NT, int kB>
-__global__ void __launch_bounds__(NT, kB == 4 ? 6 : 1)
+//
+// kMin: CTAs an SM that the registers are to leave room for.  1 (56 registers) where no SM has
+// more than three (T=24, V=151936, K=20: 21.4 us with a cold L2 against 23.0; T=39: 25.5 against
+// 27.1), 6 (40) for long fp32 rows (T=2048, V=32003, K=128: 74 against 78), else the compiler's
+// choice, 40 to 48 (T=8192, V=151936 bf16, K=64: 453 against 464 with 6; T=2048, V=32000 bf16,
+// K=20: 70 against 79 with 1; T=150, V=32000 bf16, K=64, 600 CTAs: 25 against 29).
+template <typename InT, int NT, int kB, int kMin>
+__global__ void __launch_bounds__(NT, kMin)
     cis_topk_kernel(const __grid_constant__ TopkArgs a, unsigned cs, int r, int cap)
 {
     extern __shared__ __align__(16) uint8_t dyn_smem[];
@@ -214,10 +220,10 @@ __global__ void __launch_bounds__(kSelThreads, 2)
     cg::this_cluster().sync();  // no CTA leaves while a peer reads its shared memory
 }
 
-template <typename InT, int NT, int kB>
+template <typename InT, int NT, int kB, int kMin>
 cudaError_t launch_fast(const TopkArgs &a, const PassPlan &p, cudaStream_t s)
 {
-    auto kern = cis_topk_kernel<InT, NT, kB>;
+    auto kern = cis_topk_kernel<InT, NT, kB, kMin>;
     // short rows always fit, whatever their entries
     const int cap = a.V <= 1024 ? 1024 : a.V <= 2048 ? 2048 : a.K <= 64 ? 512 : 1024;
     const size_t all = p.cs > 1 ? cap * sizeof(mass_t) : 0;
@@ -274,9 +280,11 @@ template <typename InT> cudaError_t launch_topk(const TopkArgs &a, cudaStream_t 
     const PassPlan p = pass_plan(a.T, a.V, (int)sizeof(InT));
     if (a.T * p.cs > 0x7fffffffLL)
         return cudaErrorNotSupported;
-    const cudaError_t e = p.nt == 64   ? launch_fast<InT, 64, 1>(a, p, s)
-                          : p.kb == 1 ? launch_fast<InT, 256, 1>(a, p, s)
-                                      : launch_fast<InT, 256, 4>(a, p, s);
+    const bool few = a.T * p.cs <= 3 * 152;
+    const cudaError_t e = p.nt == 64   ? launch_fast<InT, 64, 1, 0>(a, p, s)
+                          : p.kb == 4 ? launch_fast<InT, 256, 4, sizeof(InT) == 2 ? 0 : 6>(a, p, s)
+                          : few       ? launch_fast<InT, 256, 1, 1>(a, p, s)
+                                      : launch_fast<InT, 256, 1, 0>(a, p, s);
     return e != cudaSuccess ? e : launch_exact<InT>(a, s);
 }
 
