@@ -15,13 +15,20 @@
 //                     whole CTA, the thread in whose part the running mass passes u Z;
 //   else              the row's candidates, sorted by the first CTA, with masses in whole
 //                     numbers (cis_select.cuh).
-// Masses of fp32 exponentials decide only where their error cannot matter.  Each is off by less
-// than 2^-20 (the exponential 2^-22, the rounding of an exponent of up to 16 and of kappa), and
-// the sums' roundings (the batches', the warps', the CTAs') by as much again, so that a running
-// mass C is off from u Z by less than 2^-19 ((1 - u) C + u (Z - C)): nearer to its goal than
-// that, it is left open.  Rows left open, and those with more candidates than fit or a kept set
-// that reaches beyond them, are left to a second kernel, which takes every decision on whole
-// numbers: bf16 rows by counting their values, fp32 rows by cis_select.cuh's selection.
+// Masses of fp32 exponentials decide only where their error cannot matter.  With E = 2^-20: of an
+// entry within 32 bits of the maximum an exponential is off by 2.4 E of itself at most (its
+// exponent, in bits, is rounded by 2^-20, kappa by 2^-24 of it, and the instruction by 2^-22), the
+// share of a CTA's sum in the row's by 0.3 E, and a sum of fp32 numbers by 2^-24 for each of the
+// 22 roundings on an entry's way to the row's sum, 1.4 E.  A running mass C from the row's nearer
+// end, with v = u or 1 - u its goal in units of Z, is therefore off from v Z by less than twice
+// 4.1 E v Z: within 8.5 E v Z of its goal it is left open (from the first entry on, the sums'
+// roundings would not shrink with 1 - u).  Entries farther below the maximum (to 44 bits, from
+// where on a mass may as well be 0) are off by up to 3.6 E, of a mass of 2^-32 each at most.  Z
+// itself, which top_p's goal is taken from where the list does not hold the row, is off by less
+// than 4.3 E.  Rows left open, those with more candidates than fit or a kept set that reaches
+// beyond them, and rows with |M| / tau above 5e5, whose exponents have another form, are left to a
+// second kernel, which takes every decision on whole numbers: bf16 rows by counting their values,
+// fp32 rows by cis_select.cuh's selection.
 //
 // Bound: instruction issue in the first kernel (two exponentials an entry where the temperature is
 // not 1; four CTAs of 60 registers an SM, and forcing five into 48 took 126 us a call for 110 at
@@ -62,7 +69,8 @@ __device__ __forceinline__ void write_row(const SampleArgs &a, int64_t t, int32_
 
 constexpr int32_t kTodo = -2;   // as a row's id: left to the second kernel
 constexpr int32_t kTaken = -3;  // which has begun with it
-constexpr float kOpen = 0x1p-19f;
+constexpr float kOpen = 8.5f * 0x1p-20f;   // of the goal: a running mass from the nearer end
+constexpr float kSlack = 4.5f * 0x1p-20f;   // of the row's mass: top_p's goal
 constexpr int kCap = 1024;     // batches to read again, and candidates, of a row
 constexpr int kAim = 256;      // candidates aimed at where top_k does not say
 
@@ -97,8 +105,7 @@ template <int NT, typename T> __device__ void block_scan(T v, T *scan, T *warps)
 
 template <int NT> struct SampleShared {
     PassShared<NT> pass;
-    float scan[NT];
-    float warps[NT / 32];
+    mass_t scan[NT];
     mass_t warps64[NT / 32];
     mass_t goal, slack;
     uint32_t low;   // min_p's lowest key
@@ -115,22 +122,35 @@ __device__ __forceinline__ float log_share(float z, float M, const Scale &sc, fl
     return u + (e + l - log_residual(mass, ls));
 }
 
-// A row with nothing cut off, in the CTA that has its goal g: the running mass before the CTA
-// is `base`, the warps' masses red[w].s * unit.  True and the index in the thread that has it.
+// A mass in units of 2^-43 of the maximum's.
+__device__ __forceinline__ mass_t to_mass(float x) { return __float2ull_rn(x * 0x1p43f); }
+
+// e^{(m - M) / tau}, to 2^-22.
+__device__ __forceinline__ float share_of(float m, float M, const Scale &sc)
+{
+    float lo;
+    const float e = expf(scaled_diff(m, M, sc, lo));
+    return fmaf(e, lo, e);
+}
+
+// A row with nothing cut off, in the CTA that has its goal: running masses from the row's first
+// entry or, `back`, from its last one, `base` those of the CTAs passed, red[w].s * unit the
+// warps'.  Whole numbers, so that only the fp32 sums that they start from are rounded.  True and
+// the index in the thread that has it.
 template <typename InT, int NT, int kB>
-__device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &ps, float base,
-                              float unit, float g, float u, float M, float Z, const Scale &sc,
+__device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &ps, mass_t base,
+                              float unit, mass_t goal, bool back, float M, const Scale &sc,
                               unsigned rank, unsigned cs, int &index, float &zi)
 {
     constexpr int W = NT / 32, EV = Vec<InT>::kN;
     const int tid = threadIdx.x;
-    int w = 0;
-    float run = base;
-    for (; w < W - 1; ++w) {
-        const float next = run + sh.pass.red[w].s * unit;
-        if (next > g)
+    int w = back ? W - 1 : 0;
+    for (int i = 0; i < W - 1; ++i) {
+        const mass_t next = base + to_mass(sh.pass.red[w].s * unit);
+        if (next > goal)
             break;
-        run = next;
+        base = next;
+        w += back ? -1 : 1;
     }
     const int s0 = ps.seg(w), n = ps.seg(w + 1) - s0;
     const int per = (n + NT - 1) / NT, a0 = s0 + min(n, tid * per), a1 = s0 + min(n, tid * per + per);
@@ -140,50 +160,65 @@ __device__ bool draw_by_index(SampleShared<NT> &sh, const RowPass<InT, NT, kB> &
         j0 = 0;
     if (rank == cs - 1 && w == W - 1 && tid == NT - 1)
         j1 = ps.V;
-    auto weight = [&](float z) { return ex2_ftz((z - M) * sc.kappa); };
-    float sum = 0.0f;
+    // the sums' own form: a whole offset, and what it is short of M
+    const float c = ceilf(M * sc.kappa), f = exp2_accurate(-fmaf(M, sc.kappa, -c));
+    auto weight = [&](float z) { return ex2_ftz(fmaf(z, sc.kappa, -c)); };
+    float sum = 0.0f, lost = 0.0f;
+    auto add = [&](float x) {
+        float e;
+        sum = two_sum(sum, x, e);
+        lost += e;
+    };
     for (int j = j0; j < ps.head + a0 * EV; ++j)
-        sum += weight(to_f32(ps.row[j]));
+        add(weight(to_f32(ps.row[j])));
     for (int v = a0; v < a1; ++v) {
         Vec<InT> x;
         x.q = __ldg(ps.rv + v);
-        float p = 0.0f;
+        float p[EV];
 #pragma unroll
         for (int k = 0; k < EV; ++k)
-            p += weight(x.entry(k));
-        sum += p;
+            p[k] = weight(x.entry(k));
+#pragma unroll
+        for (int h = EV / 2; h > 0; h /= 2)
+#pragma unroll
+            for (int k = 0; k < h; ++k)
+                p[k] += p[k + h];
+        add(p[0]);
     }
     for (int j = ps.head + a1 * EV; j < j1; ++j)
-        sum += weight(to_f32(ps.row[j]));
-    block_scan<NT>(sum, sh.scan, sh.warps);
-    const float lo = run + (tid ? sh.scan[tid - 1] : 0.0f), hi = run + sh.scan[tid];
-    if (!(lo <= g && g < hi))
+        add(weight(to_f32(ps.row[j])));
+    const mass_t own = to_mass((sum + lost) * f);
+    block_scan<NT>(own, sh.scan, sh.warps64);
+    mass_t at = base + (back ? sh.scan[NT - 1] - sh.scan[tid] : sh.scan[tid] - own);
+    if (!(at <= goal && goal < at + own))
         return false;
-    float part = 0.0f;
-    for (int j = j0; j < j1; ++j) {
-        const float z = to_f32(ps.row[j]), x = weight(z), next = part + x;
-        if (lo + next > g && x > 0.0f) {
-            const float open = 2.0f * kOpen * u * (1.0f - u) * Z + 0x1p-28f * Z;
-            // before the row's first mass there is nothing to be off
-            const bool sure = (lo + next) - g > open &&
-                              (g - (lo + part) > open || (lo == 0.0f && part == 0.0f));
+    for (int i = 0; i < j1 - j0; ++i) {
+        const int j = back ? j1 - 1 - i : j0 + i;
+        const float z = to_f32(ps.row[j]);
+        const mass_t next = at + to_mass(weight(z) * f);
+        if (next > goal) {
+            // (512: half a unit for each number made whole on the way; V / 128: 2.4 E of V
+            // masses of 2^-32)
+            const mass_t open = 512 + ps.V / 128 + (mass_t)(kOpen * (float)goal);
             index = j;
             zi = z;
-            return sure;
+            // before the first mass there is nothing to be off
+            return next - goal > open && (goal - at > open || at == 0);
         }
-        part = next;
+        at = next;
     }
     return false;
 }
 
 // A row with something cut off, in its first CTA: n candidates in `list`, sorted.  whole: they
 // are all the row's finite entries.  above: they are all its entries from min_p's key on.
+// firm: Z's error is bounded.
 // Returns the sampled candidate's place, -1 (left open), or -2 - m for m kept ones that are
 // yet to be put in order of their index; the kept mass; in `mass` the running masses.
 template <int NT>
 __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t *list, int n,
-                             mass_t *mass, int V, float M, float Z, bool whole, bool above,
-                             mass_t &kept_mass)
+                             mass_t *mass, int V, float M, float Z, bool firm, bool whole,
+                             bool above, mass_t &kept_mass)
 {
     const int tid = threadIdx.x;
     const Scale &sc = rs.sc;
@@ -231,14 +266,14 @@ __device__ int draw_by_order(SampleShared<NT> &sh, const RowSettings &rs, mass_t
     const bool cut = !open;      // the prefix so far is m entries, known
     if (rs.top_p < 1.0f) {
         // the first place whose running mass reaches the goal
-        if (!cut && rs.top_k > 0 && rs.top_k < V)
+        if (!cut && (!firm || (rs.top_k > 0 && rs.top_k < V)))
             return -1;  // their mass is not known
         if (tid == 0) {  // (fp64 is slow here: one thread)
             const double unit = (double)(1ull << kMassBits);
             sh.goal = cut ? (mass_t)ceil((double)rs.top_p * (double)mass[m - 1])
                           : (mass_t)((double)rs.top_p * (double)Z * unit);
             // (the candidates' masses are exact, Z is not)
-            sh.slack = cut ? 0 : (mass_t)(2.0 * (double)kOpen * (double)Z * unit);
+            sh.slack = cut ? 0 : (mass_t)((double)kSlack * (double)Z * unit);
         }
         __syncthreads();
         const mass_t goal = sh.goal, slack = sh.slack;
@@ -370,36 +405,34 @@ __global__ void __launch_bounds__(NT)
     MaxSumU o = block_exp<NT>(acc, sh.pass.red);  // (its barriers)
     float S1 = two ? block_exp<NT>(raw, sh.pass.red2).s : o.s;
     float bound = cut ? ps.bound_get(sh.pass, r) : -INFINITY;
-    float sum_w = 0.0f;  // the warps' sums, in their own unit
+    float sum_w = 0.0f, sum_p = 0.0f, sum_l = 0.0f;  // the warps' sums, in their own unit
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-        sum_w += sh.pass.red[w].s;
-    float unit = o.s / sum_w, base = 0.0f;
-    float M = o.m, Z = o.s, goal = 0.0f;
-    unsigned has = 0;  // the CTA with the goal
+    for (int w = 0; w < W; ++w) {
+        float e;
+        sum_w += sh.pass.red[w].s;  // (as block_exp adds them: o.s has its roundings)
+        sum_p = two_sum(sum_p, sh.pass.red[w].s, e);
+        sum_l += e;
+    }
+    float unit = sum_w > 0.0f ? o.s / sum_w : 0.0f;
+    float M = o.m, Z = sum_w > 0.0f ? (sum_p + sum_l) * unit : o.s;
     if (cs > 1) {
-        exchange(sh.pass, rank, cs, o.m, bound, o.s, S1);
+        exchange(sh.pass, rank, cs, o.m, bound, Z, S1);
         const auto &part = sh.pass.part;
         for (unsigned c = 0; c < cs; ++c) {
             M = fmaxf(M, part[c][0]);
             bound = fminf(bound, part[c][1]);
         }
         Z = S1 = 0.0f;
+        float lost = 0.0f;
         for (unsigned c = 0; c < cs; ++c) {  // in rank order
-            const float d = part[c][0] - M;
-            Z += part[c][2] * ex2_ftz(d * rs.sc.kappa);
-            S1 += part[c][3] * ex2_ftz(d * kLog2e);
+            float e;
+            Z = two_sum(Z, part[c][2] * share_of(part[c][0], M, rs.sc), e);
+            lost += e;
+            S1 += part[c][3] * ex2_ftz((part[c][0] - M) * kLog2e);
         }
-        goal = rs.u * Z;
-        for (; has < cs - 1; ++has) {
-            const float next = base + part[has][2] * ex2_ftz((part[has][0] - M) * rs.sc.kappa);
-            if (next > goal)
-                break;
-            base = next;
-        }
-        unit *= ex2_ftz((o.m - M) * rs.sc.kappa);
+        Z += lost;
+        unit *= share_of(o.m, M, rs.sc);
     }
-    goal = rs.u * Z;
     if (!(Z > 0.0f && Z < INFINITY) || !(fabsf(M) < INFINITY)) {  // as every CTA finds
         if (rank == 0 && tid == 0) {
             write_row(a, t, -1, NAN, NAN);
@@ -408,7 +441,21 @@ __global__ void __launch_bounds__(NT)
         return;
     }
     const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
+    const bool firm = fabsf(M) < 0.5f * rs.sc.huge;
     if (!cut) {
+        // The CTA with the goal, from the row's nearer end.
+        const bool back = rs.u > 0.5f;
+        const mass_t goal = to_mass((back ? 1.0f - rs.u : rs.u) * Z);
+        unsigned has = back ? cs - 1 : 0;
+        mass_t base = 0;
+        for (unsigned i = 0; i + 1 < cs; ++i) {
+            const auto &part = sh.pass.part[has];
+            const mass_t next = base + to_mass(part[2] * share_of(part[0], M, rs.sc));
+            if (next > goal)
+                break;
+            base = next;
+            has += back ? -1 : 1;
+        }
         if (rank != has)
             return;
         int j;
@@ -417,7 +464,8 @@ __global__ void __launch_bounds__(NT)
         if (tid == 0)
             done = 0;
         __syncthreads();
-        if (draw_by_index<InT, NT, kB>(sh, ps, base, unit, goal, rs.u, M, Z, rs.sc, rank, cs, j, z)) {
+        if (firm && draw_by_index<InT, NT, kB>(sh, ps, base, unit, goal, back, M, rs.sc, rank, cs,
+                                               j, z)) {
             write_row(a, t, j, log_share(z, M, one, S1), log_share(z, M, rs.sc, Z));
             done = 1;
         }
@@ -460,8 +508,8 @@ __global__ void __launch_bounds__(NT)
     int at = 0;
     mass_t kept = (mass_t)1 << kMassBits;
     if (!rs.greedy)
-        at = draw_by_order<NT>(sh, rs, list, n, room, (int)a.V, M, Z, bound == -INFINITY, above,
-                               kept);
+        at = draw_by_order<NT>(sh, rs, list, n, room, (int)a.V, M, Z, firm, bound == -INFINITY,
+                               above, kept);
     mass_t pick = at >= 0 ? list[at] : 0;
     if (at < -2) {
         // more than 64 kept: put in order of the index, with their places
