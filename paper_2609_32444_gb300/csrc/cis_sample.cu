@@ -67,6 +67,13 @@ __device__ __forceinline__ void write_row(const SampleArgs &a, int64_t t, int32_
     if (a.lps_out) a.lps_out[t] = lps;
 }
 
+// A row that cannot be sampled, by one thread.
+__device__ __forceinline__ void refuse_row(const SampleArgs &a, int64_t t)
+{
+    write_row(a, t, -1, NAN, NAN);
+    set_status(a.status, kStatusBadInput);
+}
+
 constexpr int32_t kTodo = -2;   // as a row's id: left to the second kernel
 constexpr int32_t kTaken = -3;  // which has begun with it
 constexpr float kOpen = 8.5f * 0x1p-20f;   // of the goal: a running mass from the nearer end
@@ -362,10 +369,8 @@ __global__ void __launch_bounds__(NT)
     }
     const RowSettings rs = row_settings(a, t);
     if (!rs.ok) {
-        if (rank == 0 && tid == 0) {
-            write_row(a, t, -1, NAN, NAN);
-            set_status(a.status, kStatusBadInput);
-        }
+        if (rank == 0 && tid == 0)
+            refuse_row(a, t);
         return;
     }
     const bool by_k = rs.top_k > 0 && rs.top_k < a.V;
@@ -434,10 +439,8 @@ __global__ void __launch_bounds__(NT)
         unit *= share_of(o.m, M, rs.sc);
     }
     if (!(Z > 0.0f && Z < INFINITY) || !(fabsf(M) < INFINITY)) {  // as every CTA finds
-        if (rank == 0 && tid == 0) {
-            write_row(a, t, -1, NAN, NAN);
-            set_status(a.status, kStatusBadInput);
-        }
+        if (rank == 0 && tid == 0)
+            refuse_row(a, t);
         return;
     }
     const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
@@ -635,8 +638,8 @@ __device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, 
     if (rset.min_p > 0.0f) {
         const uint32_t low = min_p_key(M, rset.tau, rset.min_p);
         if (kept.key < low) {
-            kept = Kept{low - 1, 0};
-            wkey = 0;
+            kept = Kept{low, ~(mass_t)0};  // all entries at it, too
+            wkey = mass(key_value(low));
             parts = false;
         }
     }
@@ -645,6 +648,8 @@ __device__ void exact_row(SelectShared<NT> &sh, const SampleArgs &a, int64_t t, 
     else
         rs.kept_mass(kept.key, mass, gt, eq, gt0, eq0);
     const mass_t Z = gt + min(eq, kept.ties) * wkey;
+    if (Z == 0 && rs.rank == 0 && threadIdx.x == 0)
+        refuse_row(a, t);  // (the maximum is always kept: a mark may not stay in any case)
     target = (mass_t)((double)rset.u * (double)Z);
     // the row's mass at temperature 1: the first kernel's, where it has left the row
     const float S1 = a.lp_out ? a.lp_out[t] : 1.0f;
@@ -1084,6 +1089,8 @@ __global__ void __launch_bounds__(kCountThreads, 1)
             e0 = e;
         }
         if (!here || sw == W) {  // in another CTA's part
+            if (Z == 0 && cl.rank == 0 && tid == 0)
+                refuse_row(a, t);  // (as in exact_row)
             __syncthreads();
             continue;
         }
