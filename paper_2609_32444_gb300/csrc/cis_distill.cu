@@ -90,8 +90,6 @@ struct ListSums {
     float ms, ss;      // (max, sum of e^{(z - ms) / tau}) over the listed
     float qh, ql;      // sum of q (forward, reverse) as a pair
     float am, lq;      // topk: max a and log of sum e^{a - am}
-    float c0;          // reverse: reference of G_k = (z_k - ms) / tau - a_k - c0
-    float A;           //          sum of e^{(z_k - ms) / tau} G_k
     bool any;
 };
 
@@ -110,19 +108,27 @@ __device__ __forceinline__ float warp_max_f(float v)
     return v;
 }
 
-// (z_k - ms) / tau - a_k - c0, rounded about once.
-__device__ __forceinline__ float list_gap(float z, float a, float ms, float c0, const Scale &sc)
+// log p_k = u + ul of a listed token, M the row's maximum, logS + logSl the log of its sum.
+__device__ __forceinline__ float list_log(float z, float M, float logS, float logSl,
+                                          const Scale &sc, float &ul)
 {
-    float l, e1, e2;
-    const float p = scaled_diff(z, ms, sc, l);
-    const float u = two_sum(p, -a, e1), v = two_sum(u, -c0, e2);
-    return v + (e1 + e2 + l);
+    float l, e;
+    const float x = scaled_diff(z, M, sc, l), u = two_sum(x, -logS, e);
+    ul = e + l - logSl;
+    return u;
+}
+// log p_k - a_k, rounded about once.
+__device__ __forceinline__ float list_gap(float u, float ul, float a)
+{
+    float e;
+    const float d = two_sum(u, -a, e);
+    return d + (e + ul);
 }
 
 __device__ __forceinline__ ListSums list_sums(const ListView &li, int K, int kind, const Scale &sc)
 {
     const int lane = threadIdx.x & 31;
-    ListSums r{-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f, false};
+    ListSums r{-INFINITY, 0.0f, 0.0f, 0.0f, -INFINITY, 0.0f, false};
     bool any = false;
     for (int k = lane; k < K; k += 32)
         if (li.id[k] >= 0) {
@@ -164,27 +170,6 @@ __device__ __forceinline__ ListSums list_sums(const ListView &li, int K, int kin
     }
     r.qh = qh;
     r.ql = ql;
-    if (kind == CIS_DISTILL_REVERSE && r.ms != -INFINITY) {
-        // the reference: any listed token's own value, so that the G_k are of the size of
-        // their differences
-        float c0 = 0.0f;
-        bool have = false;
-        for (int k = lane; k < K; k += 32)
-            if (!have && li.id[k] >= 0 && li.z[k] != -INFINITY) {
-                c0 = list_gap(li.z[k], li.a[k], r.ms, 0.0f, sc);
-                have = true;
-            }
-        const unsigned who = __ballot_sync(kAll32, have);
-        r.c0 = who ? __shfl_sync(kAll32, c0, __ffs(who) - 1) : 0.0f;
-        float A = 0.0f;
-        for (int k = lane; k < K; k += 32)
-            if (li.id[k] >= 0 && li.z[k] != -INFINITY) {
-                float l;
-                const float x = scaled_diff(li.z[k], r.ms, sc, l);
-                A = fmaf(expf(x + l), list_gap(li.z[k], li.a[k], r.ms, r.c0, sc), A);
-            }
-        r.A = warp_sum_f(A);
-    }
     return r;
 }
 
@@ -256,8 +241,11 @@ template <typename OutT, int NT> __device__ __forceinline__ void zero_entries(Ou
 // copy and for each other: T=8192, V=151936, K=64 830 us, 6.0 TB/s; T=4096, V=32000 reverse 96 us,
 // 4.8 TB/s; T=4096, V=32003 fp32, K=128 170 us, 5.4 TB/s.  T=256, V=1024: 23 us a call, of which
 // this kernel is 10.
+//
+// Three CTAs an SM asked for in fp32, which is what its slices leave room for: without it the
+// compiler takes 40 registers, for more CTAs, and spills.
 template <typename InT, typename OutT, int NT>
-__global__ void __launch_bounds__(NT + 32)
+__global__ void __launch_bounds__(NT + 32, sizeof(InT) == 4 ? 3 : 0)
     cis_distill_kernel(const __grid_constant__ DistillArgs a, int64_t slice)
 {
     constexpr int NA = NT + 32;  // all threads
@@ -363,7 +351,7 @@ __global__ void __launch_bounds__(NT + 32)
     ListSums ls;
     MaxSum rest{0.0f, 0.0f};
     float M = 0.0f, S = 0.0f, er = 0.0f, es = 0.0f, pr = 0.0f, qr = 0.0f, mean = 0.0f, Q = 1.0f;
-    float sw = 0.0f;
+    float sw = 0.0f, logS = 0.0f, logSl = 0.0f;
     if (!list_warp) {
         landed();
         for (int k = tid; k < K; k += NT) {
@@ -421,6 +409,8 @@ __global__ void __launch_bounds__(NT + 32)
             S = NAN;  // no finite entry, or NaN among the listed
         qr = (1.0f - ls.qh) - ls.ql;
         pr = er / S;
+        logS = logf(S);
+        logSl = log_residual(S, logS);
         // The sum of the rest's gradients; each entry has its share e^{(z - max) / tau} / sum of
         // it, which holds where p_r itself is below fp32's range.
         float mult = 0.0f;
@@ -437,11 +427,20 @@ __global__ void __launch_bounds__(NT + 32)
             if (ls.qh != ls.qh)
                 qr = NAN;
             if (ls.ms != -INFINITY) {  // (else only the rest: its gradient is 0)
-                const float gr = rest.s > 0.0f ? (logf(rest.s) - logf(qr)) +
-                                                     ((scaled_diff(rest.m, ls.ms, a.sc, l) + l) -
-                                                      ls.c0)
-                                               : 0.0f;
-                mean = (ls.A * (es / ls.ss) + er * gr) / S;
+                // L from the outcomes that have a probability: a token that the student masks
+                // (its log p at -1e9, or beyond fp32's range) counts nothing, and neither it nor
+                // one that the teacher all but excludes is what the others are compared with
+                float sum = 0.0f;
+                for (int k = tid - NT; k < K; k += 32)
+                    if (li.id[k] >= 0) {
+                        float ul;
+                        const float u = list_log(li.z[k], M, logS, logSl, a.sc, ul);
+                        const float p = expf(u + ul);
+                        sum = fmaf(p, p == 0.0f ? 0.0f : list_gap(u, ul, li.a[k]), sum);
+                    }
+                const float gr = pr == 0.0f ? 0.0f
+                                            : (logf(rest.s) - logf(qr)) + ((xr + lr) - logS);
+                mean = fmaf(pr, gr, warp_sum_f(sum));
                 mult = pr * (gr - mean);
             }
         }
@@ -455,7 +454,7 @@ __global__ void __launch_bounds__(NT + 32)
     if (list_warp) {
         // The listed entries: log p_k = (z_k - M) / tau - log S = u + ul.
         const bool first = cl.rank == 0;
-        const float c = sw * a.sc.hi, logS = logf(S), logSl = log_residual(S, logS);
+        const float c = sw * a.sc.hi;
         float sum = 0.0f;
 #pragma unroll 2
         for (int k = tid - NT; k < K; k += 32) {
@@ -463,9 +462,8 @@ __global__ void __launch_bounds__(NT + 32)
             const bool mine = grad && e >= 0 && e < sl.n;
             if (li.id[k] < 0 || !(first || mine))
                 continue;
-            float l, e1;
-            const float z = li.z[k], lp = li.a[k], x = scaled_diff(z, M, a.sc, l);
-            const float u = two_sum(x, -logS, e1), ul = e1 + l - logSl;
+            float ul;
+            const float z = li.z[k], lp = li.a[k], u = list_log(z, M, logS, logSl, a.sc, ul);
             const float p = expf(u + ul);
             float lq = lp, lql = 0.0f;
             if (a.kind == CIS_DISTILL_TOPK) {
@@ -478,7 +476,7 @@ __global__ void __launch_bounds__(NT + 32)
             if (mine) {
                 float d;
                 if (a.kind == CIS_DISTILL_REVERSE)
-                    d = p == 0.0f ? 0.0f : p * (list_gap(z, lp, ls.ms, ls.c0, a.sc) - mean);
+                    d = p == 0.0f ? 0.0f : p * (list_gap(u, ul, lp) - mean);
                 else
                     d = fmaf(Q, p, -q);
                 li.value[k] = c * d;
