@@ -229,8 +229,9 @@ cudaError_t launch_bins(const float *key, const uint8_t *mask, int64_t T, const 
     // bins, two values: 18.9 us; one CTA an SM 21.8, 128 threads 22.2, four CTAs
     // of 128 20.4, one of 512 19.4.  T=4,000,000, 64 bins: 156 us; 292, 164, 186,
     // 152.)
+    constexpr size_t kMostBinBytes = 100 * 1024;
     int nt = kBinMaxThreads;
-    while (nt > 32 && bin_smem(a.nbins, NV, nt) > 100 * 1024)
+    while (nt > 32 && bin_smem(a.nbins, NV, nt) > kMostBinBytes)
         nt /= 2;
     const size_t smem = bin_smem(a.nbins, NV, nt);
     // a thread's columns cost it nbins additions at the end: give it some tokens
@@ -238,8 +239,7 @@ cudaError_t launch_bins(const float *key, const uint8_t *mask, int64_t T, const 
     int64_t ctas = std::min({want, (int64_t)2 * sms, bin_ctas(T)});
     ctas = ctas < 1 ? 1 : ctas;
     auto k = cis_binned_sums_kernel<NV>;
-    if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) !=
-        cudaSuccess)
+    if ((e = allow_smem(k, kMostBinBytes)) != cudaSuccess)
         return e;
     k<<<(unsigned)ctas, nt, smem, s>>>(key, mask, T, a, parts);
     if ((e = cudaGetLastError()) != cudaSuccess)

@@ -54,7 +54,7 @@ bool make_plan(int64_t V, int in_bytes, ClusterPlan *p)
         const int64_t per = (V + cs - 1) / cs;
         const int64_t slice = (per + 7) / 8 * 8;
         if (forced || slice * in_bytes <= target || cs == kMaxCluster) {
-            if (slice * in_bytes > 200 * 1024)
+            if (slice * in_bytes > kMostSliceBytes)
                 return false;
             p->cs = cs;
             p->slice = slice;

@@ -34,6 +34,7 @@ namespace cg = cooperative_groups;
 
 namespace cis {
 
+constexpr int64_t kMostSliceBytes = 200 * 1024;
 // Cluster size and slice (entries, a multiple of 8) for a row of V entries.
 struct ClusterPlan {
     int cs;
@@ -618,8 +619,7 @@ cudaError_t launch_cluster_nt(const PassArgs &a, const ClusterPlan &p, cudaStrea
     auto kern = cis_fused_cluster_kernel<InT, OutT, NT, kEnt, kRagged, kOps>;
     // a ragged slice has up to 15 entries of padding
     const size_t smem = p.smem + (kRagged ? 16 * sizeof(InT) : 0);
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem);
+    cudaError_t e = allow_smem(kern, kMostSliceBytes + 128 + 16 * sizeof(InT));
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};

@@ -567,8 +567,9 @@ cudaError_t launch_nt(const DistillArgs &a, const RowPlan &p, cudaStream_t s)
 {
     auto kern = cis_distill_kernel<InT, OutT, NT>;
     const size_t smem = slab_bytes(p.slice, sizeof(InT)) + list_bytes(a.K);
-    const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    constexpr int64_t most = kMostSliceBytes / (int64_t)sizeof(InT);
+    const cudaError_t e =
+        allow_smem(kern, slab_bytes(most, sizeof(InT)) + list_bytes(CIS_MAX_TOPK));
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};

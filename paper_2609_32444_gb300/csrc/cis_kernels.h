@@ -77,6 +77,14 @@ template <typename... P> inline bool aligned4(const P *...p)
     return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0;
 }
 
+// Lets `kern` be launched with up to `most` bytes of dynamic shared memory: the most that any call
+// of it takes.  The setting belongs to the process, so that a call that set its own size could
+// lower it between another thread's setting and launch.
+template <typename K> inline cudaError_t allow_smem(K kern, size_t most)
+{
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 // One launch of the distillation loss (cis_distill.cu).
 struct DistillArgs {
     const void *logits;

@@ -272,6 +272,8 @@ struct PassPlan {
     int cs, nt, kb;
     size_t maxima;  // bytes of the batches' maxima
 };
+// A CTA has at most 65537 vectors, a warp 8193 of them: 65 batches of four a lane.
+constexpr size_t kMostMaxima = 65 * 256 * sizeof(float);
 inline PassPlan pass_plan(int64_t T, int64_t V, int in_bytes)
 {
     const int64_t nvec = V * in_bytes / 16;

@@ -1147,9 +1147,9 @@ template <typename InT, int NT, int kB>
 cudaError_t launch_fast(const SampleArgs &a, const PassPlan &p, cudaStream_t s)
 {
     auto kern = cis_sample_kernel<InT, NT, kB>;
-    const size_t smem = kCap * (2 * sizeof(mass_t) + sizeof(int)) + p.maxima;
-    const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    constexpr size_t lists = kCap * (2 * sizeof(mass_t) + sizeof(int));
+    const size_t smem = lists + p.maxima;
+    const cudaError_t e = allow_smem(kern, lists + kMostMaxima);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -1172,8 +1172,7 @@ template <typename InT>
 cudaError_t launch_exact(const SampleArgs &a, cudaStream_t s)
 {
     constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
-    const cudaError_t e = cudaFuncSetAttribute(
-        cis_sample_exact_kernel<InT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem(cis_sample_exact_kernel<InT>, smem);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -1199,8 +1198,7 @@ cudaError_t launch_exact(const SampleArgs &a, cudaStream_t s)
 inline cudaError_t launch_counts(const SampleArgs &a, cudaStream_t s)
 {
     constexpr size_t smem = sizeof(CountShared);
-    const cudaError_t e = cudaFuncSetAttribute(
-        cis_sample_counts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem(cis_sample_counts_kernel, smem);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};

@@ -113,13 +113,14 @@ struct RowPlan {
     int64_t slice;
     int nt;
 };
+constexpr int64_t kMostSliceBytes = 200 * 1024;
 inline RowPlan row_plan(int64_t V, int in_bytes)
 {
     const int64_t target = (in_bytes == 2 ? 52 : 64) * 1024;
     for (int cs = 1; cs <= kMaxCluster; ++cs) {
         const int64_t slice = ((V + cs - 1) / cs + 7) / 8 * 8;
         if (slice * in_bytes <= target || cs == kMaxCluster) {
-            if (slice * in_bytes > 200 * 1024)
+            if (slice * in_bytes > kMostSliceBytes)
                 return {0, 0, 0};
             return {cs, slice, in_bytes == 4 || slice <= 16384 ? 128 : 256};
         }

@@ -229,8 +229,8 @@ cudaError_t launch_fast(const TopkArgs &a, const PassPlan &p, cudaStream_t s)
     const size_t all = p.cs > 1 ? cap * sizeof(mass_t) : 0;
     const size_t smem =
         cap * (sizeof(mass_t) + sizeof(int)) + (p.maxima < all ? all : p.maxima);
-    const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e =
+        allow_smem(kern, 2048 * (sizeof(mass_t) + sizeof(int)) + kMostMaxima);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -253,8 +253,7 @@ template <typename InT>
 cudaError_t launch_exact(const TopkArgs &a, cudaStream_t s)
 {
     constexpr size_t smem = sizeof(SelectShared<kSelThreads>);
-    const cudaError_t e = cudaFuncSetAttribute(
-        cis_topk_exact_kernel<InT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem(cis_topk_exact_kernel<InT>, smem);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
