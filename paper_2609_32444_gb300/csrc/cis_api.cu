@@ -155,11 +155,18 @@ CIS_API const char *cis_status_string(int32_t status)
     case CIS_ERR_UNSUPPORTED: return "CIS_ERR_UNSUPPORTED: not supported for these arguments";
     case CIS_ERR_CUDA: return "CIS_ERR_CUDA: a CUDA call or launch failed";
     case CIS_ERR_DEVICE_TIMEOUT: return "CIS_ERR_DEVICE_TIMEOUT: a bounded device wait ran out";
-    case CIS_ERR_BAD_TOKEN_ID: return "CIS_ERR_BAD_TOKEN_ID: a valid token id is outside [0, V)";
+    case CIS_ERR_BAD_TOKEN_ID:
+        return "CIS_ERR_BAD_TOKEN_ID: a valid token id is outside [0, V), or twice in a list";
     case CIS_ERR_BAD_INPUT:
         return "CIS_ERR_BAD_INPUT: a row's logits or settings are not what the call documents";
     case CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_TOKEN_ID:
         return "CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_TOKEN_ID";
+    case CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_INPUT:
+        return "CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_INPUT";
+    case CIS_ERR_BAD_TOKEN_ID | CIS_ERR_BAD_INPUT:
+        return "CIS_ERR_BAD_TOKEN_ID | CIS_ERR_BAD_INPUT";
+    case CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_TOKEN_ID | CIS_ERR_BAD_INPUT:
+        return "CIS_ERR_DEVICE_TIMEOUT | CIS_ERR_BAD_TOKEN_ID | CIS_ERR_BAD_INPUT";
     default: return "unknown cis status";
     }
 }
