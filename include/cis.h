@@ -533,8 +533,8 @@ typedef struct {
     int32_t kind;       /* cis_distill_kind_t                                    */
     int32_t agg;        /* cis_agg_t                                             */
     double temperature; /* in [1e-3, 1e3]                                        */
-    double coef;        /* finite: weight of the loss, e.g. temperature^2        */
-    double tail_min;    /* in (0, 0.5]: see the kinds above                      */
+    double coef;        /* in [-1e30, 1e30]: weight of the loss, e.g. temperature^2 */
+    double tail_min;    /* in [1e-30, 0.5]: see the kinds above                  */
     const int64_t *global_counts; /* as in cis_params_t                          */
 } cis_distill_params_t;
 

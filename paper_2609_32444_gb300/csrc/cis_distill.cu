@@ -600,8 +600,8 @@ bool distill_params_ok(const cis_distill_params_t *p)
 {
     return p != nullptr && p->kind >= CIS_DISTILL_FORWARD && p->kind <= CIS_DISTILL_TOPK &&
            (p->agg == CIS_AGG_TOKEN_MEAN || p->agg == CIS_AGG_SEQ_MEAN_TOKEN_MEAN) &&
-           temperature_ok(p->temperature) && isfinite(p->coef) && p->tail_min > 0.0 &&
-           p->tail_min <= 0.5;
+           temperature_ok(p->temperature) && fabs(p->coef) <= 1e30 && p->tail_min >= 1e-30 &&
+           p->tail_min <= 0.5;  // (the kernel has them in fp32)
 }
 
 }  // namespace
