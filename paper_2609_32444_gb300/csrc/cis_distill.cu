@@ -23,6 +23,7 @@
 // common error of the log p_b (that of the row's sum) falls out to first order.
 #include <math.h>
 
+#include "cis_exp.cuh"
 #include "cis_nvtx.h"
 #include "cis_slice.cuh"
 
@@ -125,6 +126,18 @@ __device__ __forceinline__ float list_gap(float u, float ul, float a)
     return d + (e + ul);
 }
 
+// e^a as a pair.  1 less their sum may be 10^-6, so that 2^-42 of each is asked for where they
+// are not below 10^-13 themselves (with 2^-29 that rest was off by 2^-10 of itself).
+__device__ __forceinline__ float list_share(float a, float &lo)
+{
+    if (!(a > -30.0f && a <= 0.5f))
+        return exp_pair(a, 0.0f, lo);
+    int n;
+    const float s = exp_parts(a, 0.0f, lo, n), up = __int_as_float(((n >> 5) + 127) << 23);
+    lo *= up;
+    return s * up;
+}
+
 __device__ __forceinline__ ListSums list_sums(const ListView &li, int K, int kind, const Scale &sc)
 {
     const int lane = threadIdx.x & 31;
@@ -151,7 +164,7 @@ __device__ __forceinline__ ListSums list_sums(const ListView &li, int K, int kin
                 sa += expf(li.a[k] - r.am);
             } else {
                 float e, lo;
-                const float hi = exp_pair(li.a[k], 0.0f, lo);
+                const float hi = list_share(li.a[k], lo);
                 qh = two_sum(qh, hi, e);
                 ql += e + lo;
             }
