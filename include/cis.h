@@ -561,8 +561,9 @@ CIS_API cis_status_t cis_distill_workspace_size(int64_t T, size_t *bytes);
  *   loss_out     device double [1] or NULL.
  *   workspace    device, >= cis_distill_workspace_size(T) bytes, 256-byte aligned;
  *                its first int32 is the device status word, zeroed by this call.
- * A listed token at -inf makes L infinite under FORWARD and TOPK (its gradient
- * stays finite) and counts 0 under REVERSE.  A row with NaN, +inf or no finite
+ * A listed token at -inf, or so far down that (z - max) / temperature leaves
+ * fp32's range, makes L infinite under FORWARD and TOPK (its gradient stays
+ * finite) and counts 0 under REVERSE.  A row with NaN, +inf or no finite
  * logit gives NaN.  Deterministic.  Errors: as cis_loss_fwd_bwd, plus
  * CIS_ERR_INVALID_ARG for K or parameters out of range, ld_top < K or a pointer
  * that is not aligned to its type, and CIS_ERR_UNSUPPORTED for V above 819200

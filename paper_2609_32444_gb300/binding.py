@@ -271,9 +271,9 @@ def cis_count_valid(T: int, mask=None, cu_seqlens=None, out=None) -> torch.Tenso
 
 
 def with_global_counts(params, counts: torch.Tensor):
-    """A copy of params (cis_params_t or cis_distill_params_t) whose normaliser uses the batch-wide {N, G} in
-    `counts` (device int64 [2], kept alive by the caller until the call's
-    kernels have run)."""
+    """A copy of params (cis_params_t or cis_distill_params_t) whose normaliser
+    uses the batch-wide {N, G} in `counts` (device int64 [2], kept alive by the
+    caller until the call's kernels have run)."""
     _need_cuda(counts)
     if counts.dtype != torch.int64 or counts.numel() != 2 or not counts.is_contiguous():
         raise ValueError("counts must be a contiguous device int64 tensor of 2 elements")

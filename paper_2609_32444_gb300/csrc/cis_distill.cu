@@ -16,6 +16,9 @@
 // sum over the rest is formed by itself: p_r = 1 - p_S would lose it where the list holds
 // nearly all.
 //
+// A reverse gradient compares a token's l with L, both of which are formed from the outcomes that
+// have a probability: a listed token at -1e9 has an l of that size and no p.
+//
 // Precision of L: it is a difference of terms far larger than itself.  With
 // phi(d) = e^{-d} - 1 + d >= 0 and d_b = log q_b - log p_b,
 //   sum_b q_b d_b = sum_b q_b phi(d_b) + sum_b q_b - sum_b p_b,

@@ -9,7 +9,8 @@
 // bounds, with r = ceil(K / CTAs), is one that the row's K largest are not below.  The batches
 // that reach the bound are read again (from L2), and their entries that reach it are the
 // candidates: a complete head of the row's order (186 of them for K = 128 in a row of 32,003,
-// 50 for K = 20 in one of 151,936 on eight CTAs).
+// 50 for K = 20 in one of 151,936 on eight CTAs, where likely entries are spread evenly over the
+// row; the least of the warps' and CTAs' bounds is as low as their least likely stretch).
 #pragma once
 
 #include "cis_select.cuh"

@@ -33,8 +33,9 @@
 // Bound: instruction issue in the first kernel (two exponentials an entry where the temperature is
 // not 1; four CTAs of 60 registers an SM, and forcing five into 48 took 126 us a call for 110 at
 // T=1024, V=151936, top-k), and the rows left.  T=1024, V=151936, top-p at temperature 0.7: 118 us
-// and, for the half of the rows that is left, 165; T=256, nothing cut off: 25 us and 31 for 3% of
-// the rows, a row's steps one after another on eight CTAs; T=1, top-k and top-p: 23 us a call.
+// and, for the 36% of the rows that are left, 180; T=256, nothing cut off: 27 us and 50 for the one
+// row in eight that is left, its steps one after another on eight CTAs; T=1, top-k and top-p: 24 us
+// a call.
 #include <math.h>
 
 #include "cis_nvtx.h"

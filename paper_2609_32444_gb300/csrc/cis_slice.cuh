@@ -104,10 +104,10 @@ template <typename InT> struct Slice {
 // them: the smallest cluster whose slices are within 52 KB (bf16, four CTAs an SM) or 64 KB
 // (fp32, three), up to 200 KB with 8 CTAs; cs = 0 where 8 cannot hold the row (over 819,200
 // bf16 or 409,600 fp32 entries).  Measured with the distillation loss: T=8192, V=151936 bf16
-// 830 us on 6 CTAs; in the form before pass 2 took two entries an instruction 856 on 6, 924 on 5, 1020 on 4, 858 to 882 on 7, 898 to 929 on 8; T=4096, V=32003
-// fp32 174 on 2 CTAs, 211 on 3, 180 on 4, 218 on 1.  128 threads for fp32 and for slices of at
-// most 16384 entries, else 256: V=32000 bf16 100 against 110, V=32003 fp32 174 against 177,
-// V=151936 866 against 856.
+// 830 us on 6 CTAs; in the form before pass 2 took two entries an instruction 856 on 6, 924 on 5,
+// 1020 on 4, 858 to 882 on 7, 898 to 929 on 8; T=4096, V=32003 fp32 174 on 2 CTAs, 211 on 3, 180 on
+// 4, 218 on 1.  128 threads for fp32 and for slices of at most 16384 entries, else 256: V=32000 bf16
+// 100 against 110, V=32003 fp32 174 against 177, V=151936 866 against 856.
 struct RowPlan {
     int cs;
     int64_t slice;

@@ -4,13 +4,16 @@
 // A row's order is (z descending, index ascending); lp_k = z_k / tau - log sum e^{z / tau}.
 //
 // The row is read once (cis_rowpass.cuh); the first CTA sorts the row's candidates.  A row
-// with more candidates than fit (long runs of equal entries) is left to the exact kernel,
-// which follows.
+// with more candidates than fit is left to the exact kernel, which follows: long runs of equal
+// entries, a warp or a CTA whose stretch of ids is unlikely as a whole (the bound is the least of
+// theirs), and, for K near 256, rows of a CTA of 64 threads (V=4000 in bf16: every row).
 //
 // Bound: HBM and instruction issue (64%) for many long rows, six CTAs an SM: T=8192, V=151936,
 // K=64 takes 440 us, 5.7 TB/s.  Short rows and few rows wait for a row's last steps (the bound,
 // the candidates, their order), in which a CTA loads next to nothing: T=2048, V=32003 fp32,
-// K=128 65 us, 3.1 TB/s of the rows that are read; T=24, V=151936, K=20 16 us.  Slices of the row
+// K=128 65 us, 3.1 TB/s of the rows that are read; T=24, V=151936, K=20 16 us.  With the rows left
+// it is the exact kernel, 3 us a row: the first of these takes 1.9 ms where the last eighth of the
+// ids is half a deviation lower, and 25 ms where it is a whole one.  Slices of the row
 // in the shared memory of four CTAs, read three times, took 1336 us at the first of these sizes.
 #include <math.h>
 
@@ -224,7 +227,9 @@ template <typename InT, int NT, int kB, int kMin>
 cudaError_t launch_fast(const TopkArgs &a, const PassPlan &p, cudaStream_t s)
 {
     auto kern = cis_topk_kernel<InT, NT, kB, kMin>;
-    // short rows always fit, whatever their entries
+    // Short rows always fit, whatever their entries.  Up to 64 of a list leave some 100 candidates
+    // (at T=8192, V=151936, K=64 room for 512 takes 435 us a call, for 1024 442), longer ones some
+    // 200 to 450, and on uneven rows more (K=128 at V=32003 takes 65 us with either).
     const int cap = a.V <= 1024 ? 1024 : a.V <= 2048 ? 2048 : a.K <= 64 ? 512 : 1024;
     const size_t all = p.cs > 1 ? cap * sizeof(mass_t) : 0;
     const size_t smem =
