@@ -400,6 +400,82 @@ CIS_API cis_status_t cis_lmhead_fused(const void *hidden, const void *weight, in
                                       size_t workspace_bytes, void *stream);
 
 /*
+ * The root-mean-square norm before the LM head, with the residual's addition and an output in
+ * 8 bits.  Per row, in fp32:
+ *   h = x + residual (x without one), y_j = weight_j h_j r, r = (mean_j h_j^2 + eps)^-1/2;
+ *   scale = max(max_j |y_j|, 2^-100) / 448, q_j = e4m3(y_j / scale), so that scale q_j stands for
+ *   y_j (the form that cis_lmhead_logits takes).
+ *   x          device, [T, ld_x] of `dtype` (CIS_BF16 or CIS_F32).
+ *   residual   device, [T, ld_r] of `dtype`, or NULL.
+ *   weight     device, [H] of `weight_dtype` (either type, whatever `dtype` is).
+ *   eps        in [1e-12, 1].
+ *   mask       device uint8 [T] or NULL; masked rows are not read and get zeros, scale too.
+ *   h_out      device, [T, H] of `dtype`, or NULL: h, rounded once; y is formed from h before that.
+ *   y_out      device, [T, H] of `dtype`, or NULL.
+ *   q_out      device e4m3 [T, H], and scale_out device float [T]; both NULL: left out.
+ * NaN and infinities follow the formulas; the squares are summed in fp32, so |h| has to stay
+ * below 1e17.  Rows that start on 16 bytes (and the
+ * weight) are read fastest.  The outputs may not overlap each other or the inputs.  Errors:
+ * CIS_ERR_INVALID_ARG for NULL required pointers, no output at all, q_out without scale_out or the
+ * reverse, T < 0, H <= 0, a stride below H, an unknown type, eps out of range or a pointer that is
+ * not aligned to its type; CIS_ERR_UNSUPPORTED for H above 16384.
+ */
+CIS_API cis_status_t cis_rmsnorm_fwd(const void *x, int32_t dtype, int64_t T, int64_t H,
+                                     int64_t ld_x, const void *residual, int64_t ld_r,
+                                     const void *weight, int32_t weight_dtype, double eps,
+                                     const uint8_t *mask, void *h_out, void *y_out, void *q_out,
+                                     float *scale_out, void *stream);
+
+/* Bytes of device workspace cis_rmsnorm_bwd needs.  Host only.  CIS_ERR_INVALID_ARG if bytes is
+ * NULL, T < 0 or H <= 0; CIS_ERR_UNSUPPORTED for H above 16384. */
+CIS_API cis_status_t cis_rmsnorm_bwd_workspace_size(int64_t T, int64_t H, size_t *bytes);
+
+/*
+ * The norm's gradients.  With r as above, g_j = dy_j weight_j and c = r^2 mean_j g_j h_j:
+ *   dx_j = dh_j + r (g_j - h_j c)   (the gradient of x and of the residual alike),
+ *   dweight_j = sum_t dy_tj h_tj r_t.
+ *   dy         device, [T, ld_dy] of `dtype`: the gradient of y.
+ *   h          device, [T, ld_h] of `dtype`: h_out of the forward call (x without a residual).
+ *   dh         device, [T, ld_dh] of `dtype`, or NULL (0): the gradient that reaches h by the
+ *              residual stream.
+ *   weight, eps, mask: as in the forward call; masked rows are not read, get dx 0 and have no
+ *              part in dweight.
+ *   dx         device, [T, H] of `dtype`;  dweight device float [H], both written.
+ *   workspace  device, >= cis_rmsnorm_bwd_workspace_size(T, H) bytes, 256-byte aligned.
+ * Deterministic.  T == 0: dweight 0.  The outputs may not overlap each other or the inputs.
+ * Errors: as cis_rmsnorm_fwd, and CIS_ERR_INVALID_ARG for a workspace that is too small or
+ * misaligned.
+ */
+CIS_API cis_status_t cis_rmsnorm_bwd(const void *dy, const void *h, int32_t dtype, int64_t T,
+                                     int64_t H, int64_t ld_dy, int64_t ld_h, const void *weight,
+                                     int32_t weight_dtype, const void *dh, int64_t ld_dh,
+                                     double eps, const uint8_t *mask, void *dx, float *dweight,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Logits from 8-bit hidden states and weights, for decoding and scoring:
+ *   logits_tv = hidden_scale_t weight_scale_v sum_h hidden_th weight_vh.
+ *   hidden        device e4m3 [T, H], contiguous rows, 16-byte aligned (q_out of
+ *                 cis_rmsnorm_fwd).
+ *   hidden_scale  device float [T].
+ *   weight        device e4m3 [V, H], contiguous rows, 16-byte aligned.
+ *   weight_scale  device float [V].
+ *   H             a multiple of 16 (else CIS_ERR_UNSUPPORTED).
+ *   logits        device, [T, ld] of `logits_dtype`, any alignment of its rows; j < V is written.
+ *   dev_status    device int32 [1] or NULL: device status bits are OR-ed in (the logits are not
+ *                 complete where CIS_ERR_DEVICE_TIMEOUT is among them).
+ * The products are exact and summed in fp32 on the tensor cores; the scales are applied in fp32,
+ * and the result is rounded once.  NaN in an operand gives NaN.  Deterministic.  The logits may not
+ * overlap the inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, T < 0, V <= 0,
+ * H <= 0, ld < V, an unknown dtype or a misaligned pointer; CIS_ERR_UNSUPPORTED also if the
+ * tensor-map encoder is unavailable.
+ */
+CIS_API cis_status_t cis_lmhead_logits(const void *hidden, const float *hidden_scale,
+                                       const void *weight, const float *weight_scale, int64_t T,
+                                       int64_t H, int64_t V, void *logits, int32_t logits_dtype,
+                                       int64_t ld, int32_t *dev_status, void *stream);
+
+/*
  * Mismatch diagnostics from both engines' full logits (App. A.5; Sec. 4.3,
  * Fig. 5c-d), one row per position.  With p = softmax(logits_train),
  * q = softmax(logits_infer), y the sampled token and f the weight operator of

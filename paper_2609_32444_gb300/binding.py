@@ -166,6 +166,16 @@ def _load():
     L.cis_sample_tokens.restype = ctypes.c_int
     L.cis_topk_logprobs.argtypes = [P, i32, i64, i64, i64, i32, ctypes.c_double, P, P, P, P, P, P]
     L.cis_topk_logprobs.restype = ctypes.c_int
+    L.cis_rmsnorm_fwd.argtypes = [P, i32, i64, i64, i64, P, i64, P, i32, ctypes.c_double, P, P, P,
+                                  P, P, P]
+    L.cis_rmsnorm_fwd.restype = ctypes.c_int
+    L.cis_rmsnorm_bwd_workspace_size.argtypes = [i64, i64, ctypes.POINTER(ctypes.c_size_t)]
+    L.cis_rmsnorm_bwd_workspace_size.restype = ctypes.c_int
+    L.cis_rmsnorm_bwd.argtypes = [P, P, i32, i64, i64, i64, i64, P, i32, P, i64, ctypes.c_double,
+                                  P, P, P, P, ctypes.c_size_t, P]
+    L.cis_rmsnorm_bwd.restype = ctypes.c_int
+    L.cis_lmhead_logits.argtypes = [P, P, P, P, i64, i64, i64, P, i32, i64, P, P]
+    L.cis_lmhead_logits.restype = ctypes.c_int
     _load_native(path)
     return L
 
@@ -654,6 +664,10 @@ def _status(x):
         raise ValueError("dev_status must be an int32 tensor of 1 element")
 
 
+def _bytes(x):
+    return x.numel() * x.element_size()
+
+
 def _list(x, dtype, T, name):
     if x.dtype != dtype or x.dim() != 2 or x.shape[0] != T or (x.shape[1] > 1 and
                                                                x.stride(1) != 1):
@@ -719,6 +733,136 @@ def cis_distill_fwd_bwd(logits: torch.Tensor, top_ids: torch.Tensor, top_lp: tor
             _ptr(workspace), workspace.numel(), _stream())
     _check(rc, "cis_distill_fwd_bwd")
     return {"dlogits": dlogits, "kl": kl, "loss": loss, "workspace": workspace}
+
+
+def _like(x, T, H, dtype, name):
+    """Row stride of an optional [T, H] tensor with contiguous rows."""
+    if x is None:
+        return H
+    if x.dim() != 2 or x.shape != (T, H) or x.dtype != dtype or (H > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name} must be a [{T}, {H}] {dtype} tensor with contiguous rows")
+    return x.stride(0) if T > 1 else H
+
+
+def _norm_weight(weight, H):
+    if weight.dim() != 1 or weight.shape[0] != H or not weight.is_contiguous():
+        raise ValueError(f"weight must be a contiguous [{H}] tensor")
+    return _dtype_code(weight.dtype)
+
+
+def cis_rmsnorm_fwd(x: torch.Tensor, weight: torch.Tensor, residual=None, eps=1e-6, mask=None,
+                    want_y=True, want_q=False):
+    """Root-mean-square norm of h = x + residual ([T, H] bf16 or float), in x's type and / or
+    in 8 bits with a scale a row.  Returns a dict with h (None without a residual), y (None
+    without want_y), q (float8_e4m3fn) and scale (float [T]; None without want_q)."""
+    lib()
+    r = _native.rmsnorm_fwd(x, weight, residual, eps, mask, want_y, want_q)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_rmsnorm_fwd")
+        return r
+    _need_cuda(x, weight, residual, mask)
+    T, ld = _rows(x)
+    H, dev, code = x.shape[1], x.device, _dtype_code(x.dtype)
+    ld_r = _like(residual, T, H, x.dtype, "residual")
+    wcode = _norm_weight(weight, H)
+    _vec(mask, torch.uint8, T, "mask")
+    _on(dev, weight=weight, residual=residual, mask=mask)
+    if not (want_y or want_q or residual is not None):
+        raise ValueError("nothing is asked for: want_y, want_q or a residual")
+    with torch.cuda.device(dev):
+        h = torch.empty((T, H), dtype=x.dtype, device=dev) if residual is not None else None
+        y = torch.empty((T, H), dtype=x.dtype, device=dev) if want_y else None
+        q = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=dev) if want_q else None
+        scale = torch.empty(T, dtype=torch.float32, device=dev) if want_q else None
+        rc = lib().cis_rmsnorm_fwd(
+            _ptr(x), code, T, H, ld, _ptr(residual), ld_r, _ptr(weight), wcode, float(eps),
+            _ptr(mask), _ptr(h), _ptr(y), _ptr(q), _ptr(scale), _stream())
+    _check(rc, "cis_rmsnorm_fwd")
+    return {"h": h, "y": y, "q": q, "scale": scale}
+
+
+def cis_rmsnorm_bwd_workspace_size(T: int, H: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().cis_rmsnorm_bwd_workspace_size(T, H, ctypes.byref(n)),
+           "cis_rmsnorm_bwd_workspace_size")
+    return n.value
+
+
+def cis_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh=None, eps=1e-6,
+                    mask=None, workspace=None):
+    """The norm's gradients from dy and the forward call's h (x where it had no residual), with
+    `dh`, the gradient that reaches h by the residual stream, added.  Returns a dict with dx
+    (in h's type; the residual's gradient too) and dweight (float [H])."""
+    lib()
+    r = _native.rmsnorm_bwd(dy, h, weight, dh, eps, mask, workspace)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_rmsnorm_bwd")
+        return r
+    _need_cuda(dy, h, weight, dh, mask, workspace)
+    T, ld_h = _rows(h)
+    H, dev, code = h.shape[1], h.device, _dtype_code(h.dtype)
+    ld_dy = _like(dy, T, H, h.dtype, "dy")
+    ld_dh = _like(dh, T, H, h.dtype, "dh")
+    wcode = _norm_weight(weight, H)
+    _vec(mask, torch.uint8, T, "mask")
+    _on(dev, dy=dy, weight=weight, dh=dh, mask=mask, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    nws = cis_rmsnorm_bwd_workspace_size(T, H)
+    with torch.cuda.device(dev):
+        dx = torch.empty((T, H), dtype=h.dtype, device=dev)
+        dw = torch.empty(H, dtype=torch.float32, device=dev)
+        if workspace is None or _bytes(workspace) < nws:
+            workspace = torch.empty(nws, dtype=torch.uint8, device=dev)
+        rc = lib().cis_rmsnorm_bwd(
+            _ptr(dy), _ptr(h), code, T, H, ld_dy, ld_h, _ptr(weight), wcode, _ptr(dh), ld_dh,
+            float(eps), _ptr(mask), _ptr(dx), _ptr(dw), _ptr(workspace), _bytes(workspace),
+            _stream())
+    _check(rc, "cis_rmsnorm_bwd")
+    return {"dx": dx, "dweight": dw}
+
+
+def _e4m3_rows(x, scale, name):
+    if x.dim() != 2 or x.dtype != torch.float8_e4m3fn or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous 2-D float8_e4m3fn tensor")
+    _vec(scale, torch.float32, x.shape[0], f"{name}_scale")
+
+
+def cis_lmhead_logits(hidden: torch.Tensor, hidden_scale: torch.Tensor, weight: torch.Tensor,
+                      weight_scale: torch.Tensor, logits_dtype=torch.bfloat16, logits=None,
+                      dev_status=None):
+    """Logits [T, V] from 8-bit rows and their scales: `hidden` float8_e4m3fn [T, H] and
+    `hidden_scale` float [T], as cis_rmsnorm_fwd returns them, `weight` float8_e4m3fn [V, H]
+    and `weight_scale` float [V].  `logits` takes them where given ([T, >= V])."""
+    lib()
+    r = _native.lmhead_logits(hidden, hidden_scale, weight, weight_scale, logits_dtype, logits,
+                              dev_status)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_lmhead_logits")
+        return r
+    _need_cuda(hidden, hidden_scale, weight, weight_scale, logits, dev_status)
+    _e4m3_rows(hidden, hidden_scale, "hidden")
+    _e4m3_rows(weight, weight_scale, "weight")
+    (T, H), V, dev = hidden.shape, weight.shape[0], hidden.device
+    if weight.shape[1] != H:
+        raise ValueError("hidden and weight must have rows of one length")
+    _status(dev_status)
+    _on(dev, hidden_scale=hidden_scale, weight=weight, weight_scale=weight_scale, logits=logits,
+        dev_status=dev_status)
+    with torch.cuda.device(dev):
+        if logits is None:
+            logits = torch.empty((T, V), dtype=logits_dtype, device=dev)
+        To, ld = _rows(logits)
+        if To != T or logits.shape[1] < V:
+            raise ValueError("logits must be [T, >= V]")
+        rc = lib().cis_lmhead_logits(
+            _ptr(hidden), _ptr(hidden_scale), _ptr(weight), _ptr(weight_scale), T, H, V,
+            _ptr(logits), _dtype_code(logits.dtype), ld, _ptr(dev_status), _stream())
+    _check(rc, "cis_lmhead_logits")
+    return logits
 
 
 def cis_binned_sums(key: torch.Tensor, edges, values=(), mask=None):

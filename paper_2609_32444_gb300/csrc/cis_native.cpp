@@ -49,6 +49,10 @@ struct Library {
     decltype(&cis_topk_logprobs) topk = nullptr;
     decltype(&cis_distill_workspace_size) distill_ws = nullptr;
     decltype(&cis_distill_fwd_bwd) distill = nullptr;
+    decltype(&cis_rmsnorm_fwd) norm = nullptr;
+    decltype(&cis_rmsnorm_bwd_workspace_size) norm_bwd_ws = nullptr;
+    decltype(&cis_rmsnorm_bwd) norm_bwd = nullptr;
+    decltype(&cis_lmhead_logits) head = nullptr;
 } lib;
 
 // A tensor argument: None, or a plain tensor (no subclass) with strides.
@@ -566,6 +570,145 @@ PyObject *distill_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// None, or [T, H] rows of `dt` with unit column stride.
+bool like(const Tensor *t, int64_t T, int64_t H, at::ScalarType dt, int64_t &ld)
+{
+    int64_t n;
+    ld = H;
+    return t == nullptr ||
+           (t->scalar_type() == dt && rows(*t, n, ld) && n == T && t->size(1) == H);
+}
+bool norm_weight(const Tensor *w, int64_t H, int32_t &code)
+{
+    return w && w->dim() == 1 && w->size(0) == H && w->is_contiguous() &&
+           dtype_code(w->scalar_type(), code);
+}
+
+// (x, weight, residual, eps, mask, want_y, want_q)
+PyObject *rmsnorm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *w, *r, *mask;
+    bool want_y, want_q;
+    int64_t T, ld, ldr;
+    int32_t code, wcode;
+    if (n != 7 || !take(a[0], x) || !take(a[1], w) || !take(a[2], r) ||
+        !PyFloat_CheckExact(a[3]) || !take(a[4], mask) || !flag(a[5], want_y) ||
+        !flag(a[6], want_q))
+        return none();
+    if (!x || !w || !together(*x, {w, r, mask}) || !rows(*x, T, ld) ||
+        !dtype_code(x->scalar_type(), code))
+        return none();
+    const int64_t H = x->size(1);
+    const at::ScalarType dt = x->scalar_type();
+    if (!like(r, T, H, dt, ldr) || !norm_weight(w, H, wcode) || !vec(mask, at::kByte, T) ||
+        !(want_y || want_q || r))
+        return none();
+    const double eps = PyFloat_AS_DOUBLE(a[3]);
+    const at::Device dev = x->device();
+    const Tensor h = r ? fresh({T, H}, dt, dev) : Tensor();
+    const Tensor y = want_y ? fresh({T, H}, dt, dev) : Tensor();
+    const Tensor q = want_q ? fresh({T, H}, at::kFloat8_e4m3fn, dev) : Tensor();
+    const Tensor sc = fresh_if(want_q, T, at::kFloat, dev);
+    const void *px = ptr(x), *pw = ptr(w), *pr = ptr(r);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    void *ph = ptr(h), *py = ptr(y), *pq = ptr(q);
+    float *psc = ptr<float>(sc);
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.norm(px, code, T, H, ld, pr, ldr, pw, wcode, eps, pmask, ph, py, pq, psc, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return dict({{"h", h}, {"y", y}, {"q", q}, {"scale", sc}});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dy, h, weight, dh, eps, mask, workspace)
+PyObject *rmsnorm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *dy, *h, *w, *dh, *mask, *ws_in;
+    int64_t T, ldh, ldy, lddh;
+    int32_t code, wcode;
+    if (n != 7 || !take(a[0], dy) || !take(a[1], h) || !take(a[2], w) || !take(a[3], dh) ||
+        !PyFloat_CheckExact(a[4]) || !take(a[5], mask) || !take(a[6], ws_in))
+        return none();
+    if (!dy || !h || !w || !together(*h, {dy, w, dh, mask, ws_in}) || !rows(*h, T, ldh) ||
+        !dtype_code(h->scalar_type(), code))
+        return none();
+    const int64_t H = h->size(1);
+    const at::ScalarType dt = h->scalar_type();
+    size_t need = 0;
+    if (!like(dy, T, H, dt, ldy) || !like(dh, T, H, dt, lddh) || !norm_weight(w, H, wcode) ||
+        !vec(mask, at::kByte, T) || (ws_in && !ws_in->is_contiguous()) ||
+        lib.norm_bwd_ws(T, H, &need) != CIS_OK)
+        return none();
+    const double eps = PyFloat_AS_DOUBLE(a[4]);
+    const at::Device dev = h->device();
+    const Tensor dx = fresh({T, H}, dt, dev), dw = fresh({H}, at::kFloat, dev);
+    const Tensor ws = ws_in && ws_in->nbytes() >= need ? *ws_in
+                                                       : fresh({(int64_t)need}, at::kByte, dev);
+    const void *pdy = ptr(dy), *ph = ptr(h), *pw = ptr(w), *pdh = ptr(dh);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    void *pdx = ptr(dx), *pws = ptr(ws);
+    float *pdw = ptr<float>(dw);
+    const size_t nws = ws.nbytes();
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.norm_bwd(pdy, ph, code, T, H, ldy, ldh, pw, wcode, pdh, lddh, eps, pmask, pdx, pdw,
+                      pws, nws, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return dict({{"dx", dx}, {"dweight", dw}});
+    END_HANDLE_TH_ERRORS
+}
+
+// A contiguous matrix of 8-bit numbers, and a scale a row.
+bool e4m3_rows(const Tensor *x, const Tensor *scale)
+{
+    return x && scale && x->dim() == 2 && x->scalar_type() == at::kFloat8_e4m3fn &&
+           x->is_contiguous() && vec(scale, at::kFloat, x->size(0));
+}
+
+// (hidden, hidden_scale, weight, weight_scale, logits_dtype, logits, dev_status)
+PyObject *lmhead_logits(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *xs, *w, *ws, *z_in, *st;
+    if (n != 7 || !take(a[0], x) || !take(a[1], xs) || !take(a[2], w) || !take(a[3], ws) ||
+        !THPDtype_Check(a[4]) || !take(a[5], z_in) || !take(a[6], st))
+        return none();
+    if (!e4m3_rows(x, xs) || !e4m3_rows(w, ws) || !together(*x, {xs, w, ws, z_in, st}) ||
+        x->size(1) != w->size(1) || !status(st))
+        return none();
+    const int64_t T = x->size(0), H = x->size(1), V = w->size(0);
+    at::ScalarType dt = reinterpret_cast<THPDtype *>(a[4])->scalar_type;
+    int64_t To, ld = V;
+    int32_t code;
+    if (z_in && (!rows(*z_in, To, ld) || To != T || z_in->size(1) < V))
+        return none();
+    if (z_in)
+        dt = z_in->scalar_type();
+    if (!dtype_code(dt, code))
+        return none();
+    const Tensor z = z_in ? *z_in : fresh({T, V}, dt, x->device());
+    const void *px = ptr(x), *pw = ptr(w);
+    const float *pxs = ptr<float>(xs), *pws = ptr<float>(ws);
+    void *pz = ptr(z);
+    int32_t *pst = ptr<int32_t>(st);
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.head(px, pxs, pw, pws, T, H, V, pz, code, ld, pst, s);
+    Py_END_ALLOW_THREADS
+    return rc != CIS_OK ? PyLong_FromLong(rc) : wrap(z);
+    END_HANDLE_TH_ERRORS
+}
+
 // init(path, params type, distillation's params type): the library's entry points, and the
 // types of `params`.
 PyObject *init(PyObject *, PyObject *args)
@@ -593,6 +736,10 @@ PyObject *init(PyObject *, PyObject *args)
     get(lib.topk, "cis_topk_logprobs");
     get(lib.distill_ws, "cis_distill_workspace_size");
     get(lib.distill, "cis_distill_fwd_bwd");
+    get(lib.norm, "cis_rmsnorm_fwd");
+    get(lib.norm_bwd_ws, "cis_rmsnorm_bwd_workspace_size");
+    get(lib.norm_bwd, "cis_rmsnorm_bwd");
+    get(lib.head, "cis_lmhead_logits");
     if (!ok)
         return PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path);
     Py_INCREF(type);
@@ -615,6 +762,9 @@ PyMethodDef methods[] = {
     {"mismatch_diagnostics", fast(mismatch_diagnostics), METH_FASTCALL, nullptr},
     {"sample_tokens", fast(sample_tokens), METH_FASTCALL, nullptr},
     {"topk_logprobs", fast(topk_logprobs), METH_FASTCALL, nullptr},
+    {"rmsnorm_fwd", fast(rmsnorm_fwd), METH_FASTCALL, nullptr},
+    {"rmsnorm_bwd", fast(rmsnorm_bwd), METH_FASTCALL, nullptr},
+    {"lmhead_logits", fast(lmhead_logits), METH_FASTCALL, nullptr},
     {"distill_fwd_bwd", fast(distill_fwd_bwd), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cis_native", nullptr, -1, methods,
