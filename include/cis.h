@@ -577,6 +577,68 @@ CIS_API cis_status_t cis_topk_logprobs(const void *logits, int32_t dtype, int64_
                                        const uint8_t *mask, int32_t *ids_out, float *lp_out,
                                        float *lse_out, int32_t *dev_status, void *stream);
 
+/* Most drafted tokens of a request that cis_verify_tokens takes. */
+#define CIS_MAX_DRAFTS 64
+
+/* Bytes of device workspace cis_verify_tokens needs.  Host only.  CIS_ERR_INVALID_ARG if bytes is
+ * NULL or a size is out of cis_verify_tokens' range. */
+CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, int32_t max_drafts,
+                                               size_t *bytes);
+
+/*
+ * Verifies drafted tokens against the target's probabilities, from given uniform numbers (the
+ * rejection step of speculative decoding): the tokens that a step of B requests ends with, drawn
+ * as if from the target alone.  Request b has n_b = cu_drafts[b + 1] - cu_drafts[b] drafts and
+ * n_b + 1 rows of logits, the row before each draft and the one behind the last.  With
+ * p_i = softmax(z_i / temperature) and q_i the distribution that draft x_i was drawn from, in order:
+ *   x_i is kept where u_i q_i(x_i) < p_i(x_i);
+ *   at the first i that is not, the last token is drawn from max(p_i - q_i, 0) (from p_i where
+ *   that is 0 throughout);
+ *   if all are kept, it is drawn from p_{n_b}.
+ * It is the first entry, by index, whose running mass is above u_last times the mass.  At
+ * temperature 0 p is 1 on the row's first largest entry.
+ *   logits          device, [N + B, ld] of `dtype`, any alignment of its rows: request b's rows
+ *                   from cu_drafts[b] + b on.
+ *   draft_ids       device int32 [N], u device float [N], each in [0, 1): the requests' drafts,
+ *                   one after another.  Both may be NULL where N is 0.
+ *   cu_drafts       device int32 [B + 1], cu_drafts[0] >= 0, non-decreasing, at most N.
+ *   max_drafts      0 .. CIS_MAX_DRAFTS: the most that a request has.
+ *   draft_logits    device, [N, ld_draft] of `dtype`: the rows that the drafts were drawn from, with
+ *                   draft_temperature.  NULL: q_i is 1 on the draft (tokens that were looked up).
+ *   u_last          device float [B], each in [0, 1).
+ *   temperature, draft_temperature
+ *                   device float [B], each 0 or in [1e-3, 1e3]; NULL: 1.  A draft_temperature of 0
+ *                   is a q that is 1 on the draft.
+ *   mask            device uint8 [B] or NULL; requests with 0 are not read: tokens and kept -1,
+ *                   log-probabilities 0.
+ *   tokens_out      device int32 [B, max_drafts + 1]: the kept drafts, the last token, then -1.
+ *   kept_out        device int32 [B]: how many drafts are kept.
+ *   lp_out          device float [B, max_drafts + 1] or NULL: the tokens' log-probabilities at
+ *                   temperature 1, the raw values that cis_loss_fwd_bwd takes as lp_infer; 0 behind
+ *                   the last token.
+ *   lp_sampled_out  device float [B, max_drafts + 1] or NULL: those at the request's temperature
+ *                   (0 at temperature 0).
+ *   dev_status      device int32 [1] or NULL: device status bits are OR-ed in.
+ *   workspace       device, >= cis_verify_workspace_size(B, V, max_drafts) bytes, 256-byte aligned.
+ * Rows are looked at in order up to the last token's.  Where one that is reached has NaN, +inf or
+ * no finite logit, where a number that is reached or a request's setting or range of cu_drafts is
+ * out of its range (CIS_ERR_BAD_INPUT), or a draft that is reached is not in [0, V)
+ * (CIS_ERR_BAD_TOKEN_ID), the request's tokens and kept are -1 and its log-probabilities NaN.
+ * Logits at -inf have probability 0, in either row.  The decisions are taken on masses that are
+ * right to 2^-42 of each and 2^-59 of the row's.  Deterministic.  The outputs may not overlap each
+ * other or the inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, B < 0 or above
+ * 2^20, N < 0 or above B max_drafts, V <= 0, a stride below V, max_drafts out of range, an unknown
+ * dtype, a pointer that is not aligned to its type, or a workspace that is too small or
+ * misaligned; CIS_ERR_UNSUPPORTED for V above 2^20.
+ */
+CIS_API cis_status_t cis_verify_tokens(
+    const void *logits, int32_t dtype, int64_t B, int64_t N, int64_t V, int64_t ld,
+    const int32_t *draft_ids, const int32_t *cu_drafts, int32_t max_drafts,
+    const void *draft_logits, int64_t ld_draft, const float *u, const float *u_last,
+    const float *temperature, const float *draft_temperature, const uint8_t *mask,
+    int32_t *tokens_out, int32_t *kept_out, float *lp_out, float *lp_sampled_out,
+    int32_t *dev_status, void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Distillation from a teacher's lists: per row t the teacher's most likely
  * tokens j_k and their log-probabilities a_k (cis_topk_logprobs writes such

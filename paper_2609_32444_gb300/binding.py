@@ -34,6 +34,7 @@ CIS_DISTILL_FORWARD, CIS_DISTILL_REVERSE, CIS_DISTILL_TOPK = 0, 1, 2
 DISTILL_KINDS = {"forward": CIS_DISTILL_FORWARD, "reverse": CIS_DISTILL_REVERSE,
                  "topk": CIS_DISTILL_TOPK}
 CIS_MAX_TOPK = 256
+CIS_MAX_DRAFTS = 64
 
 
 class cis_params_t(ctypes.Structure):
@@ -176,6 +177,11 @@ def _load():
     L.cis_rmsnorm_bwd.restype = ctypes.c_int
     L.cis_lmhead_logits.argtypes = [P, P, P, P, i64, i64, i64, P, i32, i64, P, P]
     L.cis_lmhead_logits.restype = ctypes.c_int
+    L.cis_verify_workspace_size.argtypes = [i64, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+    L.cis_verify_workspace_size.restype = ctypes.c_int
+    L.cis_verify_tokens.argtypes = [P, i32, i64, i64, i64, i64, P, P, i32, P, i64, P, P, P, P, P,
+                                    P, P, P, P, P, P, ctypes.c_size_t, P]
+    L.cis_verify_tokens.restype = ctypes.c_int
     _load_native(path)
     return L
 
@@ -863,6 +869,82 @@ def cis_lmhead_logits(hidden: torch.Tensor, hidden_scale: torch.Tensor, weight: 
             _ptr(logits), _dtype_code(logits.dtype), ld, _ptr(dev_status), _stream())
     _check(rc, "cis_lmhead_logits")
     return logits
+
+
+def cis_verify_workspace_size(B: int, V: int, max_drafts: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().cis_verify_workspace_size(B, V, max_drafts, ctypes.byref(n)),
+           "cis_verify_workspace_size")
+    return n.value
+
+
+def cis_verify_tokens(logits: torch.Tensor, draft_ids: torch.Tensor, cu_drafts: torch.Tensor,
+                      u: torch.Tensor, u_last: torch.Tensor, max_drafts: int, draft_logits=None,
+                      temperature=None, draft_temperature=None, mask=None, V=None, want_lp=True,
+                      want_lp_sampled=False, dev_status=None, workspace=None):
+    """Verification of drafted tokens (speculative decoding): request b's drafts are
+    draft_ids[cu_drafts[b]:cu_drafts[b + 1]], and logits has n_b + 1 rows for it, in order.
+    Returns (tokens int32 [B, max_drafts + 1], kept int32 [B], lp, lp_sampled): the kept drafts,
+    the token after them and -1 behind it, with their log-probabilities at temperature 1 and at
+    the request's (None without want_lp, want_lp_sampled)."""
+    lib()
+    r = _native.verify_tokens(logits, draft_ids, cu_drafts, u, u_last, max_drafts, draft_logits,
+                              temperature, draft_temperature, mask, V, want_lp, want_lp_sampled,
+                              dev_status, workspace)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "cis_verify_tokens")
+        return r
+    _need_cuda(logits, draft_ids, cu_drafts, u, u_last, draft_logits, temperature,
+               draft_temperature, mask, dev_status, workspace)
+    T, ld = _rows(logits)
+    V = logits.shape[1] if V is None else V
+    if V > logits.shape[1]:
+        raise ValueError("V is larger than the logits' rows")
+    max_drafts = operator.index(max_drafts)
+    if not 0 <= max_drafts <= CIS_MAX_DRAFTS:
+        raise ValueError(f"max_drafts must be between 0 and {CIS_MAX_DRAFTS}")
+    if cu_drafts.dtype != torch.int32 or cu_drafts.dim() != 1 or cu_drafts.shape[0] < 1 or \
+            not cu_drafts.is_contiguous():
+        raise ValueError("cu_drafts must be contiguous int32 [B + 1]")
+    B, N, dev = cu_drafts.shape[0] - 1, draft_ids.numel(), logits.device
+    if T != N + B:
+        raise ValueError("logits must have a row for each draft and one more for each request")
+    if N > B * max_drafts:
+        raise ValueError("there are more drafts than max_drafts for each request")
+    for x, dt, n, nm in ((draft_ids, torch.int32, N, "draft_ids"), (u, torch.float32, N, "u"),
+                         (u_last, torch.float32, B, "u_last"),
+                         (temperature, torch.float32, B, "temperature"),
+                         (draft_temperature, torch.float32, B, "draft_temperature"),
+                         (mask, torch.uint8, B, "mask")):
+        _vec(x, dt, n, nm)
+    ld_draft = V
+    if draft_logits is not None:
+        Td, ld_draft = _rows(draft_logits)
+        if Td != N or draft_logits.shape[1] < V or draft_logits.dtype != logits.dtype:
+            raise ValueError(f"draft_logits must be [{N}, >= V] rows in the logits' type")
+    _status(dev_status)
+    _on(dev, draft_ids=draft_ids, cu_drafts=cu_drafts, u=u, u_last=u_last,
+        draft_logits=draft_logits, temperature=temperature, draft_temperature=draft_temperature,
+        mask=mask, dev_status=dev_status, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    nws = cis_verify_workspace_size(B, V, max_drafts)
+    with torch.cuda.device(dev):
+        shape = (B, max_drafts + 1)
+        tokens = torch.empty(shape, dtype=torch.int32, device=dev)
+        kept = torch.empty(B, dtype=torch.int32, device=dev)
+        lp = torch.empty(shape, dtype=torch.float32, device=dev) if want_lp else None
+        lps = torch.empty(shape, dtype=torch.float32, device=dev) if want_lp_sampled else None
+        if workspace is None or _bytes(workspace) < nws:
+            workspace = torch.empty(nws, dtype=torch.uint8, device=dev)
+        rc = lib().cis_verify_tokens(
+            _ptr(logits), _dtype_code(logits.dtype), B, N, V, ld, _ptr(draft_ids), _ptr(cu_drafts),
+            max_drafts, _ptr(draft_logits), ld_draft, _ptr(u), _ptr(u_last), _ptr(temperature),
+            _ptr(draft_temperature), _ptr(mask), _ptr(tokens), _ptr(kept), _ptr(lp), _ptr(lps),
+            _ptr(dev_status), _ptr(workspace), _bytes(workspace), _stream())
+    _check(rc, "cis_verify_tokens")
+    return tokens, kept, lp, lps
 
 
 def cis_binned_sums(key: torch.Tensor, edges, values=(), mask=None):

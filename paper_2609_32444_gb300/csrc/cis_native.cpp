@@ -53,6 +53,8 @@ struct Library {
     decltype(&cis_rmsnorm_bwd_workspace_size) norm_bwd_ws = nullptr;
     decltype(&cis_rmsnorm_bwd) norm_bwd = nullptr;
     decltype(&cis_lmhead_logits) head = nullptr;
+    decltype(&cis_verify_workspace_size) verify_ws = nullptr;
+    decltype(&cis_verify_tokens) verify = nullptr;
 } lib;
 
 // A tensor argument: None, or a plain tensor (no subclass) with strides.
@@ -709,6 +711,64 @@ PyObject *lmhead_logits(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// (logits, draft_ids, cu_drafts, u, u_last, max_drafts, draft_logits, temperature,
+//  draft_temperature, mask, V, want_lp, want_lp_sampled, dev_status, workspace)
+PyObject *verify_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *z, *ids, *cu, *u, *ul, *zd, *tau, *taud, *mask, *st, *ws_in;
+    bool want_lp, want_lps;
+    int64_t D, T, ld, V, Td, ldd;
+    int32_t code;
+    if (n != 15 || !take(a[0], z) || !take(a[1], ids) || !take(a[2], cu) || !take(a[3], u) ||
+        !take(a[4], ul) || !integer(a[5], D) || !take(a[6], zd) || !take(a[7], tau) ||
+        !take(a[8], taud) || !take(a[9], mask) || !flag(a[11], want_lp) ||
+        !flag(a[12], want_lps) || !take(a[13], st) || !take(a[14], ws_in))
+        return none();
+    if (!z || !ids || !cu || !u || !ul ||
+        !together(*z, {ids, cu, u, ul, zd, tau, taud, mask, st, ws_in}) || !rows(*z, T, ld) ||
+        !dtype_code(z->scalar_type(), code) || !vocabulary(a[10], *z, V) || D < 0 ||
+        D > CIS_MAX_DRAFTS || cu->dim() != 1 || cu->size(0) < 1)
+        return none();
+    const int64_t B = cu->size(0) - 1, N = ids->numel();
+    size_t need = 0;
+    if (T != N + B || N > B * D || !vec(cu, at::kInt, B + 1) || !vec(ids, at::kInt, N) ||
+        !vec(u, at::kFloat, N) || !vec(ul, at::kFloat, B) || !vec(tau, at::kFloat, B) ||
+        !vec(taud, at::kFloat, B) || !vec(mask, at::kByte, B) || !status(st) ||
+        (ws_in && !ws_in->is_contiguous()) ||
+        lib.verify_ws(B, V, (int32_t)D, &need) != CIS_OK)
+        return none();
+    ldd = V;
+    if (zd && (zd->scalar_type() != z->scalar_type() || !rows(*zd, Td, ldd) || Td != N ||
+               zd->size(1) < V))
+        return none();
+    const at::Device dev = z->device();
+    const Tensor tok = fresh({B, D + 1}, at::kInt, dev), kept = fresh({B}, at::kInt, dev);
+    const Tensor lp = want_lp ? fresh({B, D + 1}, at::kFloat, dev) : Tensor();
+    const Tensor lps = want_lps ? fresh({B, D + 1}, at::kFloat, dev) : Tensor();
+    const Tensor ws = ws_in && ws_in->nbytes() >= need ? *ws_in
+                                                       : fresh({(int64_t)need}, at::kByte, dev);
+    const void *pz = ptr(z), *pzd = ptr(zd);
+    const int32_t *pids = ptr<int32_t>(ids), *pcu = ptr<int32_t>(cu);
+    const float *pu = ptr<float>(u), *pul = ptr<float>(ul), *ptau = ptr<float>(tau);
+    const float *ptaud = ptr<float>(taud);
+    const uint8_t *pmask = ptr<uint8_t>(mask);
+    int32_t *ptok = ptr<int32_t>(tok), *pkept = ptr<int32_t>(kept), *pst = ptr<int32_t>(st);
+    float *plp = ptr<float>(lp), *plps = ptr<float>(lps);
+    void *pws = ptr(ws);
+    const size_t nws = ws.nbytes();
+    int rc;
+    void *s = stream();
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.verify(pz, code, B, N, V, ld, pids, pcu, (int32_t)D, pzd, ldd, pu, pul, ptau, ptaud,
+                    pmask, ptok, pkept, plp, plps, pst, pws, nws, s);
+    Py_END_ALLOW_THREADS
+    if (rc != CIS_OK)
+        return PyLong_FromLong(rc);
+    return Py_BuildValue("NNNN", wrap(tok), wrap(kept), wrap(lp), wrap(lps));
+    END_HANDLE_TH_ERRORS
+}
+
 // init(path, params type, distillation's params type): the library's entry points, and the
 // types of `params`.
 PyObject *init(PyObject *, PyObject *args)
@@ -740,6 +800,8 @@ PyObject *init(PyObject *, PyObject *args)
     get(lib.norm_bwd_ws, "cis_rmsnorm_bwd_workspace_size");
     get(lib.norm_bwd, "cis_rmsnorm_bwd");
     get(lib.head, "cis_lmhead_logits");
+    get(lib.verify_ws, "cis_verify_workspace_size");
+    get(lib.verify, "cis_verify_tokens");
     if (!ok)
         return PyErr_Format(PyExc_ImportError, "%s lacks an entry point", path);
     Py_INCREF(type);
@@ -765,6 +827,7 @@ PyMethodDef methods[] = {
     {"rmsnorm_fwd", fast(rmsnorm_fwd), METH_FASTCALL, nullptr},
     {"rmsnorm_bwd", fast(rmsnorm_bwd), METH_FASTCALL, nullptr},
     {"lmhead_logits", fast(lmhead_logits), METH_FASTCALL, nullptr},
+    {"verify_tokens", fast(verify_tokens), METH_FASTCALL, nullptr},
     {"distill_fwd_bwd", fast(distill_fwd_bwd), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cis_native", nullptr, -1, methods,

@@ -81,10 +81,39 @@ def test_logits_refusals(binding, over, rc):
     assert _call(binding.lib().cis_lmhead_logits, HEAD, HEAD_OK, **over) == rc
 
 
+VER = ("z", "dtype", "B", "N", "V", "ld", "ids", "cu", "D", "zd", "ldd", "u", "ul", "tau", "taud",
+       "mask", "tok", "kept", "lp", "lps", "status", "ws", "nws", "stream")
+VER_OK = (P, 1, 2, 6, 100, 100, P, P, 3, P, 100, P, P, None, None, None, P, P, None, None, None, P,
+          1 << 20, None)
+
+
+@pytest.mark.parametrize("over,rc", [
+    (dict(z=None), 1), (dict(ids=None), 1), (dict(cu=None), 1), (dict(u=None), 1),
+    (dict(ul=None), 1), (dict(tok=None), 1), (dict(kept=None), 1), (dict(ws=None), 1),
+    (dict(ws=P + 128), 1), (dict(nws=255), 1), (dict(B=-1), 1), (dict(B=(1 << 20) + 1), 1),
+    (dict(N=-1), 1), (dict(N=7), 1), (dict(V=0), 1), (dict(ld=99), 1), (dict(ldd=99), 1),
+    (dict(D=-1), 1), (dict(D=65), 1), (dict(dtype=7), 1), (dict(z=P + 1), 1), (dict(zd=P + 1), 1),
+    (dict(u=P + 2), 1), (dict(kept=P + 1), 1), (dict(lp=P, lps=P), 1),
+    (dict(V=(1 << 20) + 1, ld=1 << 21, ldd=1 << 21), 2), (dict(B=0, N=0, z=None, ids=None), 0)])
+def test_verification_refusals(binding, over, rc):
+    assert _call(binding.lib().cis_verify_tokens, VER, VER_OK, **over) == rc
+
+
+def test_verification_workspace(binding):
+    n = ctypes.c_size_t()
+    f = binding.lib().cis_verify_workspace_size
+    assert f(1, 100, 4, None) == 1 and f(-1, 100, 4, ctypes.byref(n)) == 1
+    assert f(1, 0, 4, ctypes.byref(n)) == 1 and f(1, 100, 65, ctypes.byref(n)) == 1
+    # 32 bytes for each row and stretch at least
+    for B, V, D in ((0, 10, 0), (1, 151936, 4), (64, 151936, 4), (256, 1000, 16), (3, 1 << 20, 64)):
+        assert binding.cis_verify_workspace_size(B, V, D) >= 32 * B * (D + 1)
+
+
 def test_host_tensors_are_refused(binding):
     x, w = torch.zeros(2, 64), torch.ones(64)
     q = x.to(torch.float8_e4m3fn)
     for call in (lambda: binding.cis_rmsnorm_fwd(x, w), lambda: binding.cis_rmsnorm_bwd(x, x, w),
-                 lambda: binding.cis_lmhead_logits(q, w[:2], q, w[:2])):
+                 lambda: binding.cis_lmhead_logits(q, w[:2], q, w[:2]),
+                 lambda: binding.cis_verify_tokens(x, w[:1].int(), w[:2].int(), w[:1], w[:1], 1)):
         with pytest.raises(ValueError, match="CUDA"):
             call()
