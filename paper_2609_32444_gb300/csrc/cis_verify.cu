@@ -7,14 +7,19 @@
 // from the target's next row.  At temperature 0 p is all on the row's first largest entry.
 //
 // Two kernels.  The first reads every row once, a row's stretches on CTAs of their own: maximum
-// and sums of exponentials at tau and at 1.  In the second a cluster has a request: it puts the
-// stretches together, goes through the drafts, and draws the last token.  Sums of fp32
-// exponentials decide a draft only where their error cannot matter: with E = 2^-20 a sum is off by
-// less than 6 E of itself (cis_sample.cu), so that p and u q farther apart than 16 E of the larger
-// are in the order they seem.  Else the draft, and in any case the last token, is decided by whole
-// numbers, masses e^{(z - M) / tau} / S in units of 2^-60 right to 2^-42 of each, S the sum that
-// the first kernel found: what S is off by is common to a row, and the exact sums of both rows'
-// masses take it out again.  Sums of whole numbers depend on no order.
+// and sums of exponentials at tau and at 1.  In the second, CTAs that each have a few segments of
+// a request's row put the stretches together, go through the drafts, and add up the row's masses; the
+// last of them to finish draws the token.  Sums of fp32 exponentials decide a draft only where
+// their error cannot matter: with E = 2^-20 a sum is off by less than 6 E of itself (cis_sample.cu),
+// so that p and u q farther apart than 16 E of the larger are in the order they seem.  Else the
+// draft, and in any case the last token, is decided by whole numbers: masses e^{(z - M) / tau} / S
+// in units of 2^-60, right to 2^-35 of each, S the first kernel's sum.  What S is off by is common
+// to a row; the sums of both rows' masses, SP and SQ, take it out again: q's share in p's unit is
+// Q (1 + delta), delta = SP / SQ - 1, below 2^-16.  So that one pass does, a segment keeps SP, SQ
+// and, of the entries where P is above Q, the sums of P - Q and of Q, from which max(p - q, 0)
+// follows once delta is known; entries whose sign delta could turn are put in a list instead (a
+// few of a row; some hundreds where bf16 logits and drafts differ by the same step in many).
+// Sums of whole numbers depend on no order.
 #include <math.h>
 
 #include "cis_nvtx.h"
@@ -45,6 +50,10 @@ struct VerifyArgs {
     int32_t *status;
     Part *parts;  // [D + 1][B][chunks]
     int chunks;
+    struct Segment *segs;  // [B][groups][8]
+    int32_t *undecided;    // [B][groups][8][kListed]
+    uint32_t *tickets;     // [B]: the second kernel's CTAs that have finished
+    int groups;
 };
 
 constexpr int kVerifyThreads = 256;
@@ -143,6 +152,8 @@ __global__ void __launch_bounds__(kVerifyThreads)
         allow_next_grid();
     const int c = blockIdx.x % g.chunks, item = blockIdx.x / g.chunks;
     const int i = item / g.B, b = item % g.B;
+    if (item < g.B && c == 0 && threadIdx.x == 0)
+        g.tickets[item] = 0;
     const Request r = request(g, b);
     if (!r.on || !r.ok || i > r.n)
         return;
@@ -191,152 +202,317 @@ __global__ void __launch_bounds__(kVerifyThreads)
 // ------------------------------------------------------------------ the request
 enum : int { kAccept = 0, kReject = 1, kOpen = 2, kBadRow = 3, kBadDraft = 4 };
 struct Level {
-    double px, qx;  // p and q at the draft, by the first kernel's sums
-    float m, s, s1, md, sd, zx;
+    float m, s, s1, md, sd, zx, dx;
     int arg, id, state;
 };
 
-// e^{(z - M) / tau - L} in units of 2^-60: right to 2^-42 of itself, 0 below e^-41.
 constexpr int kUnitBits = 60;
-struct ShareMass {
-    Scale sc;
-    float M, hi, lo;  // L = hi + lo
-    __device__ __forceinline__ mass_t operator()(float z) const
+constexpr int kSteps = 2048;  // the table's, from 1 to 2
+constexpr int kWarps = kVerifyThreads / 32;
+
+// A row's masses, e^{(z - M) / tau} / S in units of 2^-60.  With Y = 2048 log2 of it, n + f,
+// |f| <= 1: 2^{n >> 11} T[n & 2047] e^{f ln2 / 2048}, T[i] = 2^{i / 2048} in 62 bits, the exponential
+// by three terms.  z K and the row's own n are whole numbers taken off by one FMA, whose rest is
+// exact for bf16 entries and else right to 2^-25; f and f ln2 / 2048 are rounded to 2^-24 of
+// themselves: 2^-35 of the mass in all.  Entries below e^-42 are 0.  (No fp64: two lanes a cycle.)
+struct RowShare {
+    float khi, klo;  // K = 2048 log2e / tau
+    float magic;     // 1.5 2^23 less the row's n
+    float f0;        // its fraction
+    float base;      // 0, or M where z K would leave the range: the entries that count are next to
+                     // M then, and z - M is exact
+    float low;       // of z - base: a mass of 0
+    float unit;      // 2048 log2 S as it was taken
+    __device__ void set(float M, float tau, const Scale &sc, float S)
     {
-        float dl, e, r;
-        const float d = sum_pair(z, -M, dl), x = d * sc.hi;
-        const float y = sum_pair(x, -hi, e);
-        if (!(y > -41.0f))
-            return 0;
-        const float yl = fmaf(d, sc.hi, -x) + fmaf(d, sc.lo, dl * sc.hi) + (e - lo);
-        int n;
-        const float s = exp_parts(y, yl, r, n);
-        const long long v = ((long long)__float2uint_rn(s * 0x1p24f) << 24) +
-                            (long long)__float2int_rn(r * 0x1p48f);
-        const int up = kUnitBits - 48 + (n >> 5);  // 13 .. -48
-        return up >= 0 ? (mass_t)v << up : (mass_t)((v + (1ll << (-up - 1))) >> -up);
+        constexpr float log2e_lo = (float)(1.4426950408889634074 - (double)kLog2e);
+        khi = kSteps * kLog2e * sc.hi;
+        klo = fmaf(kSteps * kLog2e, sc.hi, -khi) +
+              kSteps * fmaf(kLog2e, sc.lo, log2e_lo * sc.hi);
+        base = fabsf(M) < 1250.0f * tau ? 0.0f : M;
+        unit = kSteps * log2f(S);
+        const float x = M - base, h = x * khi, n = rintf(h), m = rintf(unit);
+        const float f = ((h - n) + (unit - m)) + (fmaf(x, khi, -h) + x * klo), r = rintf(f);
+        magic = 12582912.0f - (n + m + r);
+        f0 = f - r;
+        low = x - (41.93f - 0.6931472f / kSteps * unit) * tau;
     }
+    // Y: its whole part (as its place in t's bits) and fraction
+    __device__ __forceinline__ float split(float z, float &t) const
+    {
+        const float x = fmaxf(z - base, low);
+        t = fmaf(x, khi, magic);
+        const float w = t - magic;
+        return fmaf(x, khi, -w) + fmaf(x, klo, -f0);
+    }
+    __device__ __forceinline__ static mass_t mass(const mass_t *table, float t, float f)
+    {
+        constexpr float c1 = (float)(0.693147180559945309417 / kSteps);
+        constexpr float c2 = (float)(0.5 * 0.693147180559945309417 / kSteps *
+                                     0.693147180559945309417 / kSteps);
+        constexpr float c3 = c1 * c2 / 3.0f;
+        const int n = __float_as_int(t) - __float_as_int(12582912.0f);
+        const mass_t T = table[n & (kSteps - 1)];
+        const float u = f * fmaf(f, fmaf(f, c3, c2), c1);
+        const long long add = (long long)(int)(T >> 32) * __float2int_rn(u * 0x1p42f);
+        return (T + (mass_t)(add >> 10)) >> (62 - kUnitBits - (n >> 11));
+    }
+    __device__ __forceinline__ mass_t operator()(const mass_t *table, float z) const
+    {
+        float t;
+        const float f = split(z, t);
+        return mass(table, t, f);
+    }
+};
+
+// The table: T[32 .. 64 steps] from 2^{i / 32} and 2^{j / 2048}, j < 64.
+__device__ inline void fill_table(mass_t *table, mass_t *parts)
+{
+    const int tid = threadIdx.x;
+    auto whole = [](float s, float lo) {  // s + lo in [1, 2), in units of 2^-62
+        return ((mass_t)__float2uint_rn(s * 0x1p24f) << 38) +
+               (mass_t)((long long)__float2int_rn(lo * 0x1p48f) << 14);
+    };
+    if (tid < 64) {
+        constexpr double step = 0.693147180559945309417 / kSteps;
+        constexpr float c = (float)step, cl = (float)(step - (double)c);
+        const float i = (float)tid, x = i * c;
+        float lo;
+        int n;
+        const float s = exp_parts(x, fmaf(i, c, -x) + i * cl, lo, n);
+        parts[tid] = whole(s, lo);
+    } else if (tid < 96) {
+        const float2 T = kExp2Table[tid - 64];
+        parts[tid] = whole(T.x, T.y);
+    }
+    __syncthreads();
+    for (int i = tid; i < kSteps; i += kVerifyThreads)
+        table[i] = __umul64hi(parts[64 + (i >> 6)], parts[i & 63]) << 2;
+}
+
+// A segment's sums: of both rows' masses, of what is left of the first (P - Q, or P), and of Q
+// where something is left; and the number of entries that are not in the last two, as their sign
+// is not settled.  kListed of them are listed; with more, all are looked at again.
+constexpr int kListed = 32;
+struct Segment {
+    mass_t p, q, left, q_left;
+    mass_t undecided;
 };
 
 struct RequestShared {
     Level level[CIS_MAX_DRAFTS + 1];
-    ShareMass p, q;
-    mass_t sums[2][kMaxCluster][2];        // the CTAs' sums, in turn
-    mass_t warps[2][kVerifyThreads / 32];  // this CTA's warps'
-    mass_t scan_w[kVerifyThreads / 32];
-    mass_t goal, delta;
-    int minus, state;
+    mass_t table[kSteps];
+    mass_t parts[96];
+    mass_t warps[2][kWarps];
+    RowShare p, q;
+    mass_t goal, rest, delta;
+    mass_t more[kVerifyThreads];  // the undecided entries' part of each segment
+    int undecided[kWarps];
+    int minus, seg, found, end, last;
 };
 
-template <typename InT> struct RequestRow {
-    const InT *p, *q;  // q: null where the draft's distribution is all on it
-    int id;            // -1: no draft (nothing is taken off)
-};
+// The rows that a token is drawn from.
+template <typename InT> struct DrawRow {
+    const InT *p, *q;  // q: null without a draft's row
+    int V, id;         // the draft, or -1
+    bool residual;     // something is taken off: q, or the draft itself
+    int head, nvec;    // p's 16-byte vectors
+    int segs;
+    bool same;         // q's are the same
 
-// Entries [j0, j1), every `step`-th from j0 on: f(entry, target's value, draft's value).
-template <typename InT, typename F>
-__device__ __forceinline__ void entries(const RequestRow<InT> &r, int j0, int j1, int step, F f)
-{
-    constexpr int kAhead = 4;
-#pragma unroll 1
-    for (int j = j0; j < j1; j += kAhead * step) {
-        float z[kAhead], d[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const bool in = j + k * step < j1;
-            z[k] = in ? to_f32(r.p[j + k * step]) : -INFINITY;
-            d[k] = in && r.q ? to_f32(r.q[j + k * step]) : -INFINITY;
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (j + k * step < j1)
-                f(j + k * step, z[k], d[k]);
+    __device__ __forceinline__ void enter(const InT *p_, const InT *q_, int V_, int id_, int segs_)
+    {
+        p = p_;
+        q = q_;
+        V = V_;
+        id = id_;
+        residual = id >= 0;
+        segs = segs_;
+        head = row_head(p, V);
+        nvec = (V - head) / Vec<InT>::kN;
+        same = q == nullptr ||
+               ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) == 0;
     }
-}
+    // Segment s has the entries [start(s), start(s + 1)).
+    __device__ __forceinline__ int start(int s) const
+    {
+        return s == 0 ? 0 : s >= segs ? V
+                                      : head + (int)((int64_t)nvec * s / segs) * Vec<InT>::kN;
+    }
+};
 
-// The sums of two numbers a thread over the cluster, in every thread; sh.sums[turn] has the CTAs',
-// sh.warps this CTA's warps'.  The two buffers in turn: whoever writes one for the next time but
-// one has passed the barrier before which the others read it.
-__device__ inline void cluster_sums(RequestShared &sh, unsigned rank, unsigned cs, int &turn,
-                                    mass_t a, mass_t b, mass_t &A, mass_t &Bs)
+// One segment's sums, by one warp; every lane gets them.
+template <typename InT, bool kPair>
+__device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const RowShare &mp,
+                                               const RowShare &mq, const mass_t *table, int s,
+                                               int *count, int32_t *list)
 {
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    turn ^= 1;
+    constexpr int EV = Vec<InT>::kN;
+    const int lane = threadIdx.x & 31, j0 = row.start(s), j1 = row.start(s + 1);
+    Segment a = {};
+    if (kPair) {
+        if (lane == 0)
+            *count = 0;
+        __syncwarp();
+    }
+    auto add = [&](int j, float z, float d) {
+        float tp, tq;
+        const float fp = mp.split(z, tp);
+        const mass_t P = RowShare::mass(table, tp, fp);
+        a.p += P;
+        if constexpr (kPair) {
+            const float fq = mq.split(d, tq);
+            const mass_t Q = RowShare::mass(table, tq, fq);
+            a.q += Q;
+            // Y's difference: settled beyond 0.05 / 2048 of log2, 2^-15.8 (delta is below 12 E)
+            const float gap = (tp - tq) + (fp - fq);
+            if (gap > 0.05f) {
+                a.left += P - Q;
+                a.q_left += Q;
+            } else if (gap >= -0.05f && P != 0) {
+                const int at = atomicAdd(count, 1);
+                if (at < kListed)
+                    list[at] = j;
+            }
+        }
+    };
+    int from = j0, to = j0;  // the vectors' entries
+    if (row.same) {
+        from = s == 0 ? row.head : j0;
+        to = s == row.segs - 1 ? row.head + row.nvec * EV : j1;
+        const uint4 *vp = reinterpret_cast<const uint4 *>(row.p + from);
+        const uint4 *vq = reinterpret_cast<const uint4 *>(row.q + (kPair ? from : 0));
+        const int n = (to - from) / EV;
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        Vec<InT> x, y;
+        uint4 nx = lane < n ? __ldg(vp + lane) : none, ny = none;
+        if constexpr (kPair)
+            ny = lane < n ? __ldg(vq + lane) : none;
+#pragma unroll 1
+        for (int v = lane; v < n; v += 32) {
+            x.q = nx;
+            y.q = ny;
+            if (v + 32 < n) {
+                nx = __ldg(vp + v + 32);
+                if constexpr (kPair)
+                    ny = __ldg(vq + v + 32);
+            }
+#pragma unroll
+            for (int e = 0; e < EV; ++e)
+                add(from + v * EV + e, x.entry(e), kPair ? y.entry(e) : 0.0f);
+        }
+    }
+    // the entries before and after them
+    const int edge = (from - j0) + (j1 - to);
+#pragma unroll 1
+    for (int i = lane; i < edge; i += 32) {
+        const int j = i < from - j0 ? j0 + i : to + (i - (from - j0));
+        add(j, to_f32(row.p[j]), kPair ? to_f32(row.q[j]) : 0.0f);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
-    }
-    __syncthreads();
-    if (lane == 0) {
-        sh.warps[0][w] = a;
-        sh.warps[1][w] = b;
-    }
-    __syncthreads();
-    if (threadIdx.x < cs) {
-        mass_t s0 = 0, s1 = 0;
-        for (int i = 0; i < kVerifyThreads / 32; ++i) {
-            s0 += sh.warps[0][i];
-            s1 += sh.warps[1][i];
+        a.p += __shfl_xor_sync(0xffffffffu, a.p, o);
+        if constexpr (kPair) {
+            a.q += __shfl_xor_sync(0xffffffffu, a.q, o);
+            a.left += __shfl_xor_sync(0xffffffffu, a.left, o);
+            a.q_left += __shfl_xor_sync(0xffffffffu, a.q_left, o);
         }
-        mass_t *to = cg::this_cluster().map_shared_rank(&sh.sums[turn][rank][0], (int)threadIdx.x);
-        to[0] = s0;
-        to[1] = s1;
     }
-    cluster_sync_data();
-    A = Bs = 0;
-    for (unsigned c = 0; c < cs; ++c) {
-        A += sh.sums[turn][c][0];
-        Bs += sh.sums[turn][c][1];
+    if constexpr (kPair) {
+        __syncwarp();
+        a.undecided = *count;
+    } else {
+        a.left = a.p;
+        if (row.residual && row.id >= j0 && row.id < j1)  // all but the draft
+            a.left -= mp(table, to_f32(row.p[row.id]));
     }
+    return a;
+}
+
+// The sum of a number a thread over the CTA, in every thread.
+__device__ __forceinline__ mass_t cta_sum(mass_t x, mass_t *warps)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        x += __shfl_xor_sync(0xffffffffu, x, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0)
+        warps[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i)
+        x += warps[i];
+    return x;
+}
+// The sum of the threads before this one.
+__device__ __forceinline__ mass_t cta_before(mass_t x, mass_t *warps)
+{
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    mass_t run = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const mass_t y = __shfl_up_sync(0xffffffffu, run, o);
+        run += lane >= o ? y : 0;
+    }
+    __syncthreads();
+    if (lane == 31)
+        warps[w] = run;
+    __syncthreads();
+    run -= x;
+    for (int i = 0; i < w; ++i)
+        run += warps[i];
+    return run;
 }
 
 template <typename InT>
-__global__ void __launch_bounds__(kVerifyThreads)
-    cis_verify_requests_kernel(const __grid_constant__ VerifyArgs g, unsigned cs)
+__global__ void __launch_bounds__(kVerifyThreads, 4)
+    cis_verify_requests_kernel(const __grid_constant__ VerifyArgs g)
 {
-    constexpr int NT = kVerifyThreads, W = NT / 32;
+    constexpr int NT = kVerifyThreads;
     __shared__ RequestShared sh;
-    const int b = blockIdx.x / cs, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const unsigned rank = blockIdx.x - b * cs;
+    const int b = blockIdx.x / g.groups, rank = blockIdx.x - b * g.groups;
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const Request r = request(g, b);
     const int64_t out = (int64_t)b * (g.D + 1);
     auto fill = [&](int from, int32_t id, float v) {  // slots from `from` on
-        if (rank == 0)
-            for (int i = from + tid; i <= g.D; i += NT) {
-                g.tokens[out + i] = id;
-                if (g.lp) g.lp[out + i] = v;
-                if (g.lps) g.lps[out + i] = v;
-            }
+        for (int i = from + tid; i <= g.D; i += NT) {
+            g.tokens[out + i] = id;
+            if (g.lp) g.lp[out + i] = v;
+            if (g.lps) g.lps[out + i] = v;
+        }
     };
     auto refuse = [&](int32_t bits) {
         fill(0, -1, NAN);
-        if (rank == 0 && tid == 0) {
+        if (tid == 0) {
             g.kept[b] = -1;
             set_status(g.status, bits);
         }
     };
+    if (r.on && r.ok && !r.greedy)
+        fill_table(sh.table, sh.parts);
     grid_wait();
-    if (!r.on || !r.ok) {  // as every CTA of the cluster finds
-        if (r.on) {
-            refuse(kStatusBadInput);
-        } else {
-            fill(0, -1, 0.0f);
-            if (rank == 0 && tid == 0)
-                g.kept[b] = -1;
+    if (!r.on || !r.ok) {  // as every CTA of the request finds
+        if (rank == 0) {
+            if (r.on) {
+                refuse(kStatusBadInput);
+            } else {
+                fill(0, -1, 0.0f);
+                if (tid == 0)
+                    g.kept[b] = -1;
+            }
         }
         return;
     }
-    cluster_sync_data();  // every CTA of the cluster has started
     const Scale sc = device_scale(r.greedy ? 1.0f : r.tau);
-    const Scale sd = device_scale(r.model ? r.tau_d : 1.0f);
     const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
     const InT *z0 = static_cast<const InT *>(g.z) + ((int64_t)r.a + b) * g.ld;
     const InT *d0 = g.zd ? static_cast<const InT *>(g.zd) + (int64_t)r.a * g.ldd : nullptr;
 
     // Every row's stretches together, a warp a row.
-    for (int i = w; i <= r.n; i += W) {
+    for (int i = w; i <= r.n; i += kWarps) {
         const bool in = lane < g.chunks, draft = r.model && i < r.n;
+        const Scale sd = device_scale(draft ? r.tau_d : 1.0f);
         Part p = {};
         p.m = p.md = -INFINITY;
         if (in)
@@ -359,7 +535,7 @@ __global__ void __launch_bounds__(kVerifyThreads)
             arg = min(arg, __shfl_xor_sync(0xffffffffu, arg, o));
         }
         if (lane == 0) {
-            Level v = {0.0, 1.0, M, s, s1, Md, sq, 0.0f, arg, -1, kAccept};
+            Level v = {M, s, s1, Md, sq, 0.0f, 0.0f, arg, -1, kAccept};
             const float u = i < r.n ? g.u[r.a + i] : 0.0f;
             if (!(s > 0.0f && s < INFINITY) || !(fabsf(M) < INFINITY) ||
                 !(u >= 0.0f && u < 1.0f) ||
@@ -374,14 +550,18 @@ __global__ void __launch_bounds__(kVerifyThreads)
                     if (r.greedy) {
                         v.state = v.id == arg ? kAccept : kReject;
                     } else {
-                        v.px = exp(((double)v.zx - (double)M) / (double)r.tau) / (double)s;
-                        if (draft)
-                            v.qx = exp(((double)to_f32(d0[i * g.ldd + v.id]) - (double)Md) /
-                                       (double)r.tau_d) / (double)sq;
-                        const double uq = (double)u * v.qx;
-                        v.state = fabs(v.px - uq) > 0x1p-16 * fmax(v.px, uq)
-                                      ? (uq < v.px ? kAccept : kReject)
-                                      : (v.px > 0.0 ? kOpen : kReject);
+                        // (2^-21 more than the sums; where fp32 has no such number the draft is
+                        // left open too)
+                        const float px = share_of(v.zx, M, sc) / s;
+                        float uq = u;
+                        if (draft) {
+                            v.dx = to_f32(d0[i * g.ldd + v.id]);
+                            uq *= share_of(v.dx, Md, sd) / sq;
+                        }
+                        const float most = fmaxf(px, uq);
+                        v.state = fabsf(px - uq) > 0x1p-16f * most && most > 1e-30f
+                                      ? (uq < px ? kAccept : kReject)
+                                      : kOpen;
                     }
                 }
             }
@@ -390,171 +570,219 @@ __global__ void __launch_bounds__(kVerifyThreads)
     }
     __syncthreads();
 
-    RequestRow<InT> row = {z0, nullptr, -1};
-    const int j0 = (int)((int64_t)g.V * (rank * W + w) / (cs * W));
-    const int j1 = (int)((int64_t)g.V * (rank * W + w + 1) / (cs * W));
-    int turn = 0;
-    // Level i's rows, and their masses.
-    auto enter = [&](int i) {
-        const Level &v = sh.level[i];
-        row.p = z0 + i * g.ld;
-        row.id = v.id;
-        row.q = v.id >= 0 && r.model ? d0 + i * g.ldd : nullptr;
-        __syncthreads();
-        if (tid == 0 || tid == 32) {
-            const double L = log((double)(tid == 0 ? v.s : row.q ? v.sd : 1.0f));
-            const float hi = (float)L;
-            ShareMass m = {sc, v.m, hi, (float)(L - (double)hi)};
-            if (tid == 0) {
-                sh.p = m;
-            } else {
-                m.sc = sd;
-                m.M = v.md;
-                sh.q = m;
-            }
-        }
-        __syncthreads();
+    int k = 0;
+    auto advance = [&] {  // to the next row that decides something
+        while (sh.level[k].state == kAccept && k < r.n)
+            ++k;
+        return sh.level[k].state;
     };
-    // The sums of both rows' masses, in every thread (without a draft's row the second is 2^60).
-    auto both_sums = [&](mass_t &sp, mass_t &sq) {
-        mass_t a = 0, c = 0;
-        const ShareMass mp = sh.p, mq = sh.q;
-        entries(row, j0 + lane, j1, 32, [&](int, float z, float d) {
-            a += mp(z);
-            if (row.q)
-                c += mq(d);
-        });
-        cluster_sums(sh, rank, cs, turn, a, c, sp, sq);
-        if (!row.q)
-            sq = 1ull << kUnitBits;
-    };
-
-    int k = 0, state = kAccept, summed = -1;
-    mass_t sp = 0, sq = 0;
-    for (;; ++k) {
-        state = sh.level[k].state;
-        if (state == kOpen) {
-            enter(k);
-            both_sums(sp, sq);
-            summed = k;
-            if (tid == 0) {
-                const Level &v = sh.level[k];
-                sh.state = (double)g.u[r.a + k] * v.qx * (double)sp < v.px * (double)sq ? kAccept
-                                                                                       : kReject;
-            }
-            __syncthreads();
-            state = sh.state;
+    int state = advance();
+    auto finish = [&](int32_t token, float z) {  // every thread
+        if (state == kBadRow || state == kBadDraft) {
+            refuse(state == kBadRow ? kStatusBadInput : kStatusBadId);
+            return;
         }
-        if (state != kAccept || k == r.n)
-            break;
-    }
-    if (state == kBadRow || state == kBadDraft) {
-        refuse(state == kBadRow ? kStatusBadInput : kStatusBadId);
-        cluster_sync_data();  // no CTA leaves while a peer writes its shared memory
-        return;
-    }
-    if (rank == 0) {
-        for (int i = tid; i < k; i += NT) {
+        for (int i = tid; i <= k; i += NT) {
             const Level &v = sh.level[i];
-            g.tokens[out + i] = v.id;
-            if (g.lp) g.lp[out + i] = log_prob(v.zx, v.m, one, v.s1);
-            if (g.lps) g.lps[out + i] = r.greedy ? 0.0f : log_prob(v.zx, v.m, sc, v.s);
+            const float x = i < k ? v.zx : z;
+            g.tokens[out + i] = i < k ? v.id : token;
+            if (g.lp) g.lp[out + i] = log_prob(x, v.m, one, v.s1);
+            if (g.lps) g.lps[out + i] = r.greedy ? 0.0f : log_prob(x, v.m, sc, v.s);
         }
+        fill(k + 1, -1, 0.0f);
         if (tid == 0)
             g.kept[b] = k;
-    }
-    fill(k + 1, -1, 0.0f);
-    auto last = [&](int j, float z) {
-        const Level &v = sh.level[k];
-        g.tokens[out + k] = j;
-        if (g.lp) g.lp[out + k] = log_prob(z, v.m, one, v.s1);
-        if (g.lps) g.lps[out + k] = r.greedy ? 0.0f : log_prob(z, v.m, sc, v.s);
     };
-    if (r.greedy) {
-        if (rank == 0 && tid == 0)
-            last(sh.level[k].arg, sh.level[k].m);
-        cluster_sync_data();
+    if (r.greedy || state == kBadRow || state == kBadDraft) {
+        if (rank == 0)
+            finish(sh.level[k].arg, sh.level[k].m);
         return;
     }
 
-    // The last token: what is left of p.
-    enter(k);
-    if (row.q && summed != k)
-        both_sums(sp, sq);
-    if (tid == 0 && row.q) {  // sp / sq - 1 in units of 2^-64
-        const double x = ((double)(long long)(sp - sq)) / (double)sq;
-        sh.minus = x < 0.0;
-        sh.delta = (mass_t)(fabs(x) * 0x1p64);
+    // The row's masses, a warp a segment.
+    const int segs = g.groups * kWarps;
+    Segment *mine = g.segs + (int64_t)b * segs;
+    int32_t *undecided = g.undecided + (int64_t)b * segs * kListed;
+    DrawRow<InT> row;
+    auto enter = [&] {
+        const Level &v = sh.level[k];
+        row.enter(z0 + k * g.ld, v.id >= 0 && r.model ? d0 + k * g.ldd : nullptr, g.V, v.id, segs);
+        __syncthreads();
+        if (tid == 0)
+            sh.p.set(v.m, r.tau, sc, v.s);
+        if (tid == 32 && row.q)
+            sh.q.set(v.md, r.tau_d, device_scale(r.tau_d), v.sd);
+        __syncthreads();
+    };
+    auto sums = [&](int from, int to) {
+        const RowShare mp = sh.p, mq = sh.q;
+        for (int s = from + w; s < to; s += kWarps) {
+            int32_t *list = undecided + (int64_t)s * kListed;
+            int *count = &sh.undecided[w];
+            const Segment a =
+                row.q && row.residual
+                    ? add_segment<InT, true>(row, mp, mq, sh.table, s, count, list)
+                    : add_segment<InT, false>(row, mp, mp, sh.table, s, count, list);
+            __syncwarp();
+            if (lane == 0)
+                mine[s] = a;
+        }
+    };
+    enter();
+    sums(rank * kWarps, rank * kWarps + kWarps);
+    if (g.groups > 1) {  // the request's last CTA goes on
+        __threadfence();
+        __syncthreads();
+        if (tid == 0)
+            sh.last = atomicAdd(&g.tickets[b], 1u) == (unsigned)g.groups - 1;
+        __syncthreads();
+        if (!sh.last)
+            return;
+        __threadfence();
+    } else {
+        __syncthreads();
     }
-    __syncthreads();
-    const ShareMass mp = sh.p, mq = sh.q;
-    const mass_t delta = sh.delta;
-    const bool minus = sh.minus;
-    bool residual = row.id >= 0;
-    auto mass = [&](int j, float z, float d) -> mass_t {
-        const mass_t P = mp(z);
-        if (!residual)
+    const RowShare *mp = &sh.p, *mq = &sh.q;
+    bool minus = false;
+    mass_t delta = 0, left = 0;
+    auto off = [&](mass_t Q) {  // Q (1 + delta)
+        const mass_t x = __umul64hi(Q, delta);
+        return minus ? Q - x : Q + x;
+    };
+    auto mass = [&](int j) -> mass_t {
+        const mass_t P = (*mp)(sh.table, to_f32(row.p[j]));
+        if (!row.residual)
             return P;
         if (!row.q)
             return j == row.id ? 0 : P;
-        mass_t Q = mq(d);
-        const mass_t off = __umul64hi(Q, delta);
-        Q = minus ? Q - off : Q + off;
+        const mass_t Q = off((*mq)(sh.table, to_f32(row.q[j])));
         return P > Q ? P - Q : 0;
     };
-    mass_t R = 0, none;
     for (;;) {
-        mass_t own = 0;
-        entries(row, j0 + lane, j1, 32,
-                [&](int j, float z, float d) { own += mass(j, z, d); });
-        cluster_sums(sh, rank, cs, turn, own, 0, R, none);
-        if (R > 0 || !residual)
-            break;
-        residual = false;  // p is q as far as can be told: the whole of p
-    }
-    if (tid == 0)
-        sh.goal = min((mass_t)((double)g.u_last[b] * (double)R), R - 1);
-    __syncthreads();
-    // the CTA, the warp's stretch, and in it a thread's part
-    const mass_t goal = sh.goal;
-    mass_t base = 0;
-    unsigned has = 0;
-    while (has + 1 < cs && base + sh.sums[turn][has][0] <= goal)
-        base += sh.sums[turn][has++][0];
-    if (has == rank) {
-        int ws = 0;
-        while (ws + 1 < W && base + sh.warps[0][ws] <= goal)
-            base += sh.warps[0][ws++];
-        const int s0 = (int)((int64_t)g.V * (rank * W + ws) / (cs * W));
-        const int s1 = (int)((int64_t)g.V * (rank * W + ws + 1) / (cs * W));
-        const int per = (s1 - s0 + NT - 1) / NT;
-        const int a0 = min(s1, s0 + tid * per), a1 = min(s1, a0 + per);
-        mass_t own = 0;
-        entries(row, a0, a1, 1, [&](int j, float z, float d) { own += mass(j, z, d); });
-        mass_t run = own;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const mass_t x = __shfl_up_sync(0xffffffffu, run, o);
-            run += lane >= o ? x : 0;
-        }
-        if (lane == 31)
-            sh.scan_w[w] = run;
-        __syncthreads();
-        mass_t at = base + run - own;
-        for (int i = 0; i < w; ++i)
-            at += sh.scan_w[i];
-        if (at <= goal && goal < at + own) {
-            for (int j = a0; j < a1; ++j) {
-                const float z = to_f32(row.p[j]);
-                at += mass(j, z, row.q ? to_f32(row.q[j]) : 0.0f);
-                if (at > goal) {
-                    last(j, z);
-                    break;
-                }
+        Segment a = {};
+        for (int s = tid; s < segs; s += NT)  // (segs <= NT)
+            a = Segment{__ldcg(&mine[s].p), __ldcg(&mine[s].q), __ldcg(&mine[s].left),
+                        __ldcg(&mine[s].q_left), __ldcg(&mine[s].undecided)};
+        const mass_t sp = cta_sum(a.p, sh.warps[0]);
+        const mass_t sq = row.q && row.residual ? cta_sum(a.q, sh.warps[1]) : 1ull << kUnitBits;
+        if (state == kOpen) {  // (rare: what follows is left to this CTA)
+            if (tid == 0) {
+                // p(x) = e^{(z - M) / tau} 2^-{unit / 2048} 2^60 / SP, and q's likewise
+                Level &v = sh.level[k];
+                auto share = [](float z, float M, float tau, float unit, mass_t sum) {
+                    return exp(((double)z - (double)M) / (double)tau -
+                               (double)unit * (0.693147180559945309417 / kSteps)) / (double)sum;
+                };
+                const double P = share(v.zx, v.m, r.tau, sh.p.unit, sp);
+                const double Q = row.q ? share(v.dx, v.md, r.tau_d, sh.q.unit, sq)
+                                       : 1.0 / (double)(1ull << kUnitBits);
+                v.state = (double)g.u[r.a + k] * Q < P ? kAccept : kReject;
+            }
+            __syncthreads();
+            const int was = k;
+            state = advance();
+            if (state == kBadRow || state == kBadDraft) {
+                finish(-1, 0.0f);
+                return;
+            }
+            if (k != was) {
+                enter();
+                sums(0, segs);
+                __syncthreads();
+                continue;
             }
         }
+        left = a.left;
+        if (row.q && row.residual) {
+            if (tid == 0) {
+                // SP / SQ - 1 in units of 2^-64: to fp32, and then what that leaves
+                sh.minus = sp < sq;
+                const mass_t d = sp < sq ? sq - sp : sp - sq;
+                const mass_t x = __float2ull_rz((float)d / (float)sq * 0x1p64f);
+                const long long rest = (long long)(d - __umul64hi(x, sq));
+                sh.delta = x + (mass_t)__float2ll_rn((float)rest / (float)sq * 0x1p64f);
+            }
+            __syncthreads();
+            minus = sh.minus;
+            delta = sh.delta;
+            const mass_t x = __umul64hi(a.q_left, delta);
+            left = minus ? left + x : left - x;
+            // the entries that were undecided: a warp a segment
+            sh.more[tid] = a.undecided;
+            __syncthreads();
+            for (int s = w; s < segs; s += kWarps) {
+                const int n = (int)sh.more[s];
+                if (n == 0)
+                    continue;
+                mass_t own = 0;
+                if (n <= kListed) {
+                    if (lane < n)
+                        own = mass(__ldcg(undecided + (int64_t)s * kListed + lane));
+                } else {
+                    for (int j = row.start(s) + lane; j < row.start(s + 1); j += 32)
+                        own += mass(j);
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    own += __shfl_xor_sync(0xffffffffu, own, o);
+                __syncwarp();
+                if (lane == 0)
+                    sh.more[s] = own;
+            }
+            __syncthreads();
+            if (a.undecided)
+                left = sh.more[tid] + (a.undecided > kListed ? 0 : left);
+            __syncthreads();
+        }
+        const mass_t R = cta_sum(left, sh.warps[0]);
+        if (R > 0) {
+            // The segment, and in it a thread's part.
+            if (tid == 0)
+                sh.goal = __umul64hi(R, __float2ull_rz(g.u_last[b] * 0x1p64f));  // (below R)
+            const mass_t before = cta_before(left, sh.warps[1]);  // (its barriers)
+            const mass_t goal = sh.goal;
+            if (before <= goal && goal < before + left) {
+                sh.seg = tid;
+                sh.rest = goal - before;
+            }
+            if (tid == 0)
+                sh.end = sh.found = -1;
+            __syncthreads();
+            const mass_t rest = sh.rest;
+            const int s0 = row.start(sh.seg), s1 = row.start(sh.seg + 1);
+            const int per = (s1 - s0 + NT - 1) / NT;
+            const int a0 = min(s1, s0 + tid * per), a1 = min(s1, a0 + per);
+            mass_t own = 0;
+            int end = -1;  // the last entry with a mass
+#pragma unroll 4
+            for (int j = a0; j < a1; ++j) {
+                const mass_t m = mass(j);
+                own += m;
+                end = m ? j : end;
+            }
+            atomicMax(&sh.end, end);
+            mass_t at = cta_before(own, sh.warps[0]);
+            if (at <= rest && rest < at + own) {
+                int j = a0;
+                while ((at += mass(j)) <= rest)
+                    ++j;
+                sh.found = j;
+            }
+            __syncthreads();
+            // (a segment's sum and its entries' are off from each other by their roundings, a unit
+            // each: beyond the last entry it is that one)
+            const int j = sh.found >= 0 ? sh.found : sh.end;
+            if (j >= 0) {
+                finish(j, to_f32(row.p[j]));
+                return;
+            }
+        }
+        // p is q as far as can be told: the whole of p
+        row.residual = false;
+        __syncthreads();
+        sums(0, segs);
+        __syncthreads();
     }
-    cluster_sync_data();
 }
 
 // A row's stretches: as many CTAs as fill the SMs four times, 512 vectors at least each.
@@ -567,6 +795,30 @@ int chunks_of(int64_t B, int64_t D, int64_t V, int in_bytes)
     return c < 1 ? 1 : (int)c;
 }
 
+// The second kernel's CTAs a request: as many again, 256 entries a segment at least, and no more
+// segments than a CTA has threads.
+int groups_of(int64_t B, int64_t V)
+{
+    int64_t c = (608 + B - 1) / B;
+    c = c < V / (256 * kWarps) ? c : V / (256 * kWarps);
+    c = c < kVerifyThreads / kWarps ? c : kVerifyThreads / kWarps;
+    return c < 1 ? 1 : (int)c;
+}
+
+struct VerifyLayout {
+    size_t segs, undecided, tickets, total;
+};
+VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D, int chunks)
+{
+    VerifyLayout l;
+    l.segs = ws_round_up((size_t)B * (size_t)(D + 1) * (size_t)chunks * sizeof(Part));
+    const size_t n = (size_t)B * groups_of(B, V) * kWarps;
+    l.undecided = l.segs + ws_round_up(n * sizeof(Segment));
+    l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(int32_t));
+    l.total = l.tickets + ws_round_up((size_t)B * sizeof(uint32_t));
+    return l;
+}
+
 template <typename InT> cudaError_t launch_verify(const VerifyArgs &g, cudaStream_t s)
 {
     const unsigned grid = (unsigned)((int64_t)g.B * (g.D + 1) * g.chunks);
@@ -577,23 +829,16 @@ template <typename InT> cudaError_t launch_verify(const VerifyArgs &g, cudaStrea
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess)
         return e;
-    unsigned cs = 1;
-    while (cs < kMaxCluster && (int64_t)g.B * cs * 2 <= 608 && g.V / (2 * cs) >= 2048)
-        cs *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)g.B * cs);
+    cfg.gridDim = dim3((unsigned)(g.B * g.groups));
     cfg.blockDim = dim3(kVerifyThreads);
     cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cs;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, cis_verify_requests_kernel<InT>, g, cs);
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, cis_verify_requests_kernel<InT>, g);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -615,7 +860,7 @@ extern "C" CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, 
         return CIS_ERR_INVALID_ARG;
     const int64_t n = B > 0 ? B : 1;
     const int c = chunks_of(n, max_drafts, V, 4);  // (bf16 rows have no more)
-    *bytes = ws_round_up((size_t)n * (size_t)(max_drafts + 1) * (size_t)c * sizeof(Part));
+    *bytes = verify_layout(n, V, max_drafts, c).total;
     return CIS_OK;
 }
 
@@ -665,8 +910,14 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     g.lp = lp_out;
     g.lps = lp_sampled_out;
     g.status = dev_status;
-    g.parts = static_cast<Part *>(workspace);
     g.chunks = chunks_of(B, max_drafts, V, dtype == CIS_BF16 ? 2 : 4);
+    g.groups = groups_of(B, V);
+    const VerifyLayout l = verify_layout(B, V, max_drafts, g.chunks);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    g.parts = reinterpret_cast<Part *>(ws);
+    g.segs = reinterpret_cast<Segment *>(ws + l.segs);
+    g.undecided = reinterpret_cast<int32_t *>(ws + l.undecided);
+    g.tickets = reinterpret_cast<uint32_t *>(ws + l.tickets);
     const cudaError_t e = dtype == CIS_BF16 ? launch_verify<__nv_bfloat16>(g, (cudaStream_t)stream)
                                             : launch_verify<float>(g, (cudaStream_t)stream);
     return e == cudaSuccess ? CIS_OK : CIS_ERR_CUDA;
