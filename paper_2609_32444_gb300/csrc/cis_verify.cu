@@ -48,16 +48,16 @@ struct VerifyArgs {
     int32_t *tokens, *kept;
     float *lp, *lps;
     int32_t *status;
-    Part *parts;  // [D + 1][B][chunks]
-    int chunks;
-    struct Segment *segs;  // [B][groups][8]
-    int32_t *undecided;    // [B][groups][8][kListed]
+    Part *parts;  // [D + 1][B][stretches]
+    int stretches;
+    struct Segment *segs;  // [B][segments]
+    int32_t *undecided;    // [B][segments][kListed]
     uint32_t *tickets;     // [B]: the second kernel's CTAs that have finished
-    int groups;
+    int groups, segments;  // of a request
 };
 
-constexpr int kVerifyThreads = 256;
-constexpr int kMaxChunks = 32;  // a lane each
+constexpr int kVerifyThreads = 256, kWarps = kVerifyThreads / 32;
+constexpr int kMaxStretches = 64;  // two a lane
 
 // A request, checked.
 struct Request {
@@ -98,6 +98,38 @@ __device__ __forceinline__ float share_of(float m, float M, const Scale &sc)
     const float e = expf(scaled_diff(m, M, sc, lo));
     return fmaf(e, lo, e);
 }
+// The lanes' sums together, as sums of e^{z - m}, in every lane: each at its own whole offset, so
+// that they move to the largest's by powers of two (where the maximum is too large for that, by
+// the exponential).
+template <bool kScaled> __device__ __forceinline__ MaxSumU warp_exp(const ExpAcc<false, kScaled> &acc)
+{
+    float M = acc.m;  // (a NaN is kept by its lane's sum)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    ExpAcc<false, kScaled> all = acc;
+    all.m = M;
+    all.c = M == -INFINITY ? 0.0f : ceilf(M * acc.kappa());
+    float s = acc.S, d;
+    if constexpr (kScaled)
+        s += acc.lost;
+    if (all.fast()) {
+        d = acc.fast() ? acc.c - all.c : fmaf(acc.m, acc.kappa(), -all.c);
+    } else {
+        s = acc.result().s;
+        d = acc.m == -INFINITY ? -INFINITY : (acc.m - M) * acc.kappa();
+    }
+    s *= ex2_ftz(d);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (M == -INFINITY)
+        return {M, s, 0.0f};
+    all.S = s;
+    if constexpr (kScaled)
+        all.lost = 0.0f;
+    return all.result();
+}
 // The log-probability of z: (z - M) / tau - log of the row's mass; at most 0, whatever the mass's
 // roundings.
 __device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, float mass)
@@ -108,113 +140,144 @@ __device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, flo
     return fminf(u + (e + l - log_residual(mass, ls)), 0.0f);
 }
 
-template <typename InT, int kB> using Pass = RowPass<InT, kVerifyThreads, kB>;
-
-// One row's stretch: its maximum and sum at sc, and with `two` that at 1.
-template <typename InT, int kB>
-__device__ __forceinline__ MaxSumU stretch(PassShared<kVerifyThreads> &sh, Pass<InT, kB> &ps,
-                                           const Scale &sc, bool two, float &s1)
+// A stretch of one row, of the target's or (the items behind theirs) a draft's, by a warp of its
+// own: no barrier holds a warp whose loads have come.  Four vectors a lane at a time, with the next
+// four on their way.
+template <typename InT>
+__global__ void __launch_bounds__(kVerifyThreads, 3)
+    cis_verify_rows_kernel(const __grid_constant__ VerifyArgs g)
 {
+    constexpr int EV = Vec<InT>::kN, kB = 4;
+    if (threadIdx.x == 0)
+        allow_next_grid();
+    const int lane = threadIdx.x & 31, rows = g.B * (g.D + 1);
+    const int id = (int)blockIdx.x * kWarps + (int)(threadIdx.x >> 5);
+    int item = id / g.stretches;
+    const int st = id - item * g.stretches;
+    if (item < g.B && st == 0 && lane == 0)
+        g.tickets[item] = 0;
+    const bool draft = item >= rows;
+    item -= draft ? rows : 0;
+    const int i = item / g.B, b = item - i * g.B;
+    if (i > g.D)
+        return;
+    const Request r = request(g, b);
+    if (!r.on || !r.ok || i > r.n || (draft && (!r.model || i == r.n)))
+        return;
+    const InT *row = draft ? static_cast<const InT *>(g.zd) + ((int64_t)r.a + i) * g.ldd
+                           : static_cast<const InT *>(g.z) + ((int64_t)r.a + b + i) * g.ld;
+    const int head = row_head(row, g.V), nvec = (g.V - head) / EV;
+    const int v0 = nvec * st / g.stretches, v1 = nvec * (st + 1) / g.stretches;
+    const uint4 *rv = reinterpret_cast<const uint4 *>(row + head), *at = rv + v0 + lane;
+    const int full = (v1 - v0) / (32 * kB);
+    Vec<InT> x[kB];
+    uint4 next[kB];
+    if (full > 0) {
+#pragma unroll
+        for (int k = 0; k < kB; ++k)
+            next[k] = __ldg(at + 32 * k);
+    }
+    const float tau = draft ? r.tau_d : r.greedy ? 1.0f : r.tau;
+    const Scale sc = device_scale(tau);
+    const bool two = !draft && g.lp && tau != 1.0f;
     ExpAcc<false, true> acc;
     acc.k = sc.kappa;
     acc.h = sc.huge;
     ExpAcc<false> raw;
-    auto entry = [&](auto &e, float z) {
-        e.raise(z);
-        if (e.m != -INFINITY)
-            e.add_entry(z);
+    auto batch = [&] {
+        const float mx = vec_max<kB>(x);
+        take<false, kB>(acc, x, mx);
+        if (two)
+            take<false, kB>(raw, x, mx);
     };
-    ps.stream(
-        false,
-        [&](const Vec<InT> (&x)[kB], float mx) {
-            take<false, kB>(acc, x, mx);
-            if (two)
-                take<false, kB>(raw, x, mx);
-        },
-        [&](float z) {
-            entry(acc, z);
-            if (two)
-                entry(raw, z);
-        });
-    const MaxSumU o = block_exp<kVerifyThreads>(acc, sh.red);
-    s1 = two ? block_exp<kVerifyThreads>(raw, sh.red2).s : o.s;
-    return o;
-}
-
-template <typename InT, int kB>
-__global__ void __launch_bounds__(kVerifyThreads)
-    cis_verify_rows_kernel(const __grid_constant__ VerifyArgs g)
-{
-    constexpr int NT = kVerifyThreads, EV = Vec<InT>::kN;
-    __shared__ PassShared<NT> sh;
-    __shared__ int first;
-    if (threadIdx.x == 0)
-        allow_next_grid();
-    const int c = blockIdx.x % g.chunks, item = blockIdx.x / g.chunks;
-    const int i = item / g.B, b = item % g.B;
-    if (item < g.B && c == 0 && threadIdx.x == 0)
-        g.tickets[item] = 0;
-    const Request r = request(g, b);
-    if (!r.on || !r.ok || i > r.n)
+#pragma unroll 1
+    for (int k0 = 1; k0 <= full; ++k0) {
+#pragma unroll
+        for (int k = 0; k < kB; ++k)
+            x[k].q = next[k];
+        at += 32 * kB;
+        if (k0 < full) {
+#pragma unroll
+            for (int k = 0; k < kB; ++k)
+                next[k] = __ldg(at + 32 * k);
+        }
+        batch();
+    }
+    const int left = v1 - v0 - full * 32 * kB;
+    if (left > 0) {
+        const uint4 none = make_uint4(Vec<InT>::kNone, Vec<InT>::kNone, Vec<InT>::kNone,
+                                      Vec<InT>::kNone);
+#pragma unroll
+        for (int k = 0; k < kB; ++k)
+            x[k].q = lane + 32 * k < left ? __ldg(at + 32 * k) : none;
+        batch();
+    }
+    // the ragged ends, fewer than EV entries each: to the first and the last stretch
+    const int tail = head + nvec * EV;
+    int end = -1;
+    if (st == 0 && lane < head)
+        end = lane;
+    if (st == g.stretches - 1 && lane >= 16 && lane - 16 < g.V - tail)
+        end = tail + lane - 16;
+    float zend = -INFINITY;
+    if (end >= 0) {
+        zend = to_f32(row[end]);
+        acc.raise(zend);
+        if (acc.m != -INFINITY)
+            acc.add_entry(zend);
+        if (two) {
+            raw.raise(zend);
+            if (raw.m != -INFINITY)
+                raw.add_entry(zend);
+        }
+    }
+    const MaxSumU o = warp_exp(acc);
+    Part &out = g.parts[((int64_t)i * g.B + b) * g.stretches + st];
+    if (draft) {
+        if (lane == 0) {
+            out.md = o.m;
+            out.sd = o.s;
+        }
         return;
-    const InT *row = static_cast<const InT *>(g.z) + ((int64_t)r.a + b + i) * g.ld;
-    const Scale sc = device_scale(r.greedy ? 1.0f : r.tau);
-    Part out = {};
-    Pass<InT, kB> ps(row, g.V, c, g.chunks, nullptr);
-    const MaxSumU o = stretch<InT, kB>(sh, ps, sc, g.lp && sc.hi != 1.0f, out.s1);
-    out.m = o.m;
-    out.s = o.s;
+    }
+    const float s1 = two ? warp_exp(raw).s : o.s;
+    int first = 0x7fffffff;
     if (r.greedy) {  // (read again, from L2)
-        if (threadIdx.x == 0)
-            first = 0x7fffffff;
-        __syncthreads();
-        int at = 0x7fffffff;
-        for (int v = ps.v0 + threadIdx.x; v < ps.v1; v += NT) {
-            Vec<InT> x[1];
-            x[0].q = __ldg(ps.rv + v);
-            if (vec_max<1>(x) == o.m) {
+        for (int v = v0 + lane; v < v1; v += 32) {
+            Vec<InT> y[1];
+            y[0].q = __ldg(rv + v);
+            if (vec_max<1>(y) == o.m) {
 #pragma unroll
                 for (int e = EV - 1; e >= 0; --e)
-                    at = x[0].entry(e) == o.m ? ps.head + v * EV + e : at;
+                    first = y[0].entry(e) == o.m ? head + v * EV + e : first;
                 break;
             }
         }
-        if (ps.end >= 0 && ps.zend == o.m)
-            at = min(at, ps.end);
-        if (at != 0x7fffffff)
-            atomicMin(&first, at);
-        __syncthreads();
+        if (end >= 0 && zend == o.m)
+            first = min(first, end);
+        first = __reduce_min_sync(0xffffffffu, first);
+    }
+    if (lane == 0) {
+        out.m = o.m;
+        out.s = o.s;
+        out.s1 = s1;
         out.arg = first;
     }
-    if (r.model && i < r.n) {
-        __syncthreads();
-        Pass<InT, kB> pd(static_cast<const InT *>(g.zd) + ((int64_t)r.a + i) * g.ldd, g.V, c,
-                         g.chunks, nullptr);
-        float unused;
-        const MaxSumU d = stretch<InT, kB>(sh, pd, device_scale(r.tau_d), false, unused);
-        out.md = d.m;
-        out.sd = d.s;
-    }
-    if (threadIdx.x == 0)
-        g.parts[((int64_t)i * g.B + b) * g.chunks + c] = out;
 }
 
 // ------------------------------------------------------------------ the request
 enum : int { kAccept = 0, kReject = 1, kOpen = 2, kBadRow = 3, kBadDraft = 4 };
-struct Level {
-    float m, s, s1, md, sd, zx, dx;
-    int arg, id, state;
-};
+struct Level;
 
 constexpr int kUnitBits = 60;
 constexpr int kSteps = 2048;  // the table's, from 1 to 2
-constexpr int kWarps = kVerifyThreads / 32;
 
 // A row's masses, e^{(z - M) / tau} / S in units of 2^-60.  With Y = 2048 log2 of it, n + f,
 // |f| <= 1: 2^{n >> 11} T[n & 2047] e^{f ln2 / 2048}, T[i] = 2^{i / 2048} in 62 bits, the exponential
 // by three terms.  z K and the row's own n are whole numbers taken off by one FMA, whose rest is
 // exact for bf16 entries and else right to 2^-25; f and f ln2 / 2048 are rounded to 2^-24 of
-// themselves: 2^-35 of the mass in all.  Entries below e^-42 are 0.  (No fp64: two lanes a cycle.)
+// themselves, and their product with T to 2^-36: 2^-35 of the mass in all.  Entries below e^-42
+// are 0.  (No fp64: two lanes a cycle.)
 struct RowShare {
     float khi, klo;  // K = 2048 log2e / tau
     float magic;     // 1.5 2^23 less the row's n
@@ -223,7 +286,10 @@ struct RowShare {
                      // M then, and z - M is exact
     float low;       // of z - base: a mass of 0
     float unit;      // 2048 log2 S as it was taken
-    __device__ void set(float M, float tau, const Scale &sc, float S)
+    // depth: from where on entries are 0, in units of e.  A draft's row has 0.2 more than the
+    // target's: entries that both forbid are then as far apart as any.
+    static constexpr float kDepth = 41.75f;  // (a shift of 63 bits, below 42.28)
+    __device__ void set(float M, float tau, const Scale &sc, float S, float depth)
     {
         constexpr float log2e_lo = (float)(1.4426950408889634074 - (double)kLog2e);
         khi = kSteps * kLog2e * sc.hi;
@@ -235,33 +301,61 @@ struct RowShare {
         const float f = ((h - n) + (unit - m)) + (fmaf(x, khi, -h) + x * klo), r = rintf(f);
         magic = 12582912.0f - (n + m + r);
         f0 = f - r;
-        low = x - (41.93f - 0.6931472f / kSteps * unit) * tau;
+        low = x - (depth - 0.6931472f / kSteps * unit) * tau;
     }
     // Y: its whole part (as its place in t's bits) and fraction
     __device__ __forceinline__ float split(float z, float &t) const
     {
         const float x = fmaxf(z - base, low);
         t = fmaf(x, khi, magic);
-        const float w = t - magic;
-        return fmaf(x, khi, -w) + fmaf(x, klo, -f0);
-    }
-    __device__ __forceinline__ static mass_t mass(const mass_t *table, float t, float f)
-    {
-        constexpr float c1 = (float)(0.693147180559945309417 / kSteps);
-        constexpr float c2 = (float)(0.5 * 0.693147180559945309417 / kSteps *
-                                     0.693147180559945309417 / kSteps);
-        constexpr float c3 = c1 * c2 / 3.0f;
-        const int n = __float_as_int(t) - __float_as_int(12582912.0f);
-        const mass_t T = table[n & (kSteps - 1)];
-        const float u = f * fmaf(f, fmaf(f, c3, c2), c1);
-        const long long add = (long long)(int)(T >> 32) * __float2int_rn(u * 0x1p42f);
-        return (T + (mass_t)(add >> 10)) >> (62 - kUnitBits - (n >> 11));
+        return fmaf(x, khi, magic - t) + fmaf(x, klo, -f0);
     }
     __device__ __forceinline__ mass_t operator()(const mass_t *table, float z) const
     {
         float t;
         const float f = split(z, t);
-        return mass(table, t, f);
+        return mass(table, t, f * fmaf(f, fmaf(f, kC3, kC2), kC1));
+    }
+    // e^{f ln2 / 2048} - 1 in units of 2^-36
+    static constexpr double kStep = 0.693147180559945309417 / kSteps;
+    static constexpr float kC1 = (float)(kStep * 0x1p36), kC2 = (float)(kStep * kStep / 2 * 0x1p36),
+                           kC3 = (float)(kStep * kStep * kStep / 6 * 0x1p36);
+    __device__ __forceinline__ static mass_t mass(const mass_t *table, float t, float u)
+    {
+        const int n = __float_as_int(t);  // and 1.5 2^23, whose low 11 bits are 0
+        const mass_t T = table[n & (kSteps - 1)];
+        const mass_t m = T + (mass_t)((long long)(int)(T >> 36) * __float2int_rn(u));
+        return m >> (62 - kUnitBits + (0x4b400000 >> 11) - (n >> 11));
+    }
+};
+
+// Two entries' masses, of two rows or of one, with packed instructions: the same as RowShare's.
+struct TwoShares {
+    float2 khi, klo, magic, nf0, nbase, low;
+    __device__ __forceinline__ TwoShares(const RowShare &a, const RowShare &b)
+        : khi(make_float2(a.khi, b.khi)), klo(make_float2(a.klo, b.klo)),
+          magic(make_float2(a.magic, b.magic)), nf0(make_float2(-a.f0, -b.f0)),
+          nbase(make_float2(-a.base, -b.base)), low(make_float2(a.low, b.low))
+    {
+    }
+    __device__ __forceinline__ float2 split(float2 z, float2 &t) const
+    {
+        float2 x = __fadd2_rn(z, nbase);
+        x.x = fmaxf(x.x, low.x);
+        x.y = fmaxf(x.y, low.y);
+        t = __ffma2_rn(x, khi, magic);
+        const float2 nw = __ffma2_rn(t, make_float2(-1.0f, -1.0f), magic);
+        return __fadd2_rn(__ffma2_rn(x, khi, nw), __ffma2_rn(x, klo, nf0));
+    }
+    __device__ __forceinline__ static void masses(const mass_t *table, float2 t, float2 f,
+                                                  mass_t &a, mass_t &b)
+    {
+        float2 u = __ffma2_rn(f, make_float2(RowShare::kC3, RowShare::kC3),
+                              make_float2(RowShare::kC2, RowShare::kC2));
+        u = __ffma2_rn(f, u, make_float2(RowShare::kC1, RowShare::kC1));
+        u = __fmul2_rn(f, u);
+        a = RowShare::mass(table, t.x, u.x);
+        b = RowShare::mass(table, t.y, u.y);
     }
 };
 
@@ -299,14 +393,20 @@ struct Segment {
     mass_t undecided;
 };
 
+// A row of the request, its draft and what they come to.
+struct Level {
+    float m, s, s1, md, sd;
+    float u, zx, dx;  // the draft's number and logits
+    int arg, id, state;
+    RowShare p, q;
+};
+
 struct RequestShared {
     Level level[CIS_MAX_DRAFTS + 1];
     mass_t table[kSteps];
     mass_t parts[96];
     mass_t warps[2][kWarps];
-    RowShare p, q;
     mass_t goal, rest, delta;
-    mass_t more[kVerifyThreads];  // the undecided entries' part of each segment
     int undecided[kWarps];
     int minus, seg, found, end, last;
 };
@@ -349,31 +449,41 @@ __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const Ro
 {
     constexpr int EV = Vec<InT>::kN;
     const int lane = threadIdx.x & 31, j0 = row.start(s), j1 = row.start(s + 1);
-    Segment a = {};
+    const TwoShares two(mp, mq);
+    mass_t sp = 0, sq = 0, left = 0, q_left = 0;
+    float least = INFINITY;  // the least distance of a sign from its border
     if (kPair) {
         if (lane == 0)
             *count = 0;
         __syncwarp();
     }
-    auto add = [&](int j, float z, float d) {
-        float tp, tq;
-        const float fp = mp.split(z, tp);
-        const mass_t P = RowShare::mass(table, tp, fp);
-        a.p += P;
+    // kPair: an entry of both rows; else two entries of one
+    auto add = [&](float a, float b) {
+        float2 t;
+        const float2 f = two.split(make_float2(a, b), t);
+        mass_t P, Q;
+        TwoShares::masses(table, t, f, P, Q);
         if constexpr (kPair) {
-            const float fq = mq.split(d, tq);
-            const mass_t Q = RowShare::mass(table, tq, fq);
-            a.q += Q;
+            sp += P;
+            sq += Q;
             // Y's difference: settled beyond 0.05 / 2048 of log2, 2^-15.8 (delta is below 12 E)
-            const float gap = (tp - tq) + (fp - fq);
+            const float gap = (t.x - t.y) + (f.x - f.y);
             if (gap > 0.05f) {
-                a.left += P - Q;
-                a.q_left += Q;
-            } else if (gap >= -0.05f && P != 0) {
-                const int at = atomicAdd(count, 1);
-                if (at < kListed)
-                    list[at] = j;
+                left += P;
+                q_left += Q;
             }
+            least = fminf(least, fabsf(gap));
+        } else {
+            sp += P + Q;
+        }
+    };
+    auto check = [&](int j) {  // lists entry j where its sign is not settled
+        float2 t;
+        const float2 f = two.split(make_float2(to_f32(row.p[j]), to_f32(row.q[j])), t);
+        if (fabsf((t.x - t.y) + (f.x - f.y)) <= 0.05f && mp(table, to_f32(row.p[j])) != 0) {
+            const int at = atomicAdd(count, 1);
+            if (at < kListed)
+                list[at] = j;
         }
     };
     int from = j0, to = j0;  // the vectors' entries
@@ -397,9 +507,21 @@ __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const Ro
                 if constexpr (kPair)
                     ny = __ldg(vq + v + 32);
             }
+            if constexpr (kPair) {
 #pragma unroll
-            for (int e = 0; e < EV; ++e)
-                add(from + v * EV + e, x.entry(e), kPair ? y.entry(e) : 0.0f);
+                for (int e = 0; e < EV; ++e)
+                    add(x.entry(e), y.entry(e));
+                if (least <= 0.05f) {
+                    least = INFINITY;
+#pragma unroll 1
+                    for (int e = 0; e < EV; ++e)
+                        check(from + v * EV + e);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < EV; e += 2)
+                    add(x.entry(e), x.entry(e + 1));
+            }
         }
     }
     // the entries before and after them
@@ -407,26 +529,30 @@ __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const Ro
 #pragma unroll 1
     for (int i = lane; i < edge; i += 32) {
         const int j = i < from - j0 ? j0 + i : to + (i - (from - j0));
-        add(j, to_f32(row.p[j]), kPair ? to_f32(row.q[j]) : 0.0f);
+        add(to_f32(row.p[j]), kPair ? to_f32(row.q[j]) : -INFINITY);
+        if (kPair && least <= 0.05f) {
+            least = INFINITY;
+            check(j);
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        a.p += __shfl_xor_sync(0xffffffffu, a.p, o);
+        sp += __shfl_xor_sync(0xffffffffu, sp, o);
         if constexpr (kPair) {
-            a.q += __shfl_xor_sync(0xffffffffu, a.q, o);
-            a.left += __shfl_xor_sync(0xffffffffu, a.left, o);
-            a.q_left += __shfl_xor_sync(0xffffffffu, a.q_left, o);
+            sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            left += __shfl_xor_sync(0xffffffffu, left, o);
+            q_left += __shfl_xor_sync(0xffffffffu, q_left, o);
         }
     }
     if constexpr (kPair) {
         __syncwarp();
-        a.undecided = *count;
+        return {sp, sq, left - q_left, q_left, (mass_t)*count};
     } else {
-        a.left = a.p;
+        left = sp;
         if (row.residual && row.id >= j0 && row.id < j1)  // all but the draft
-            a.left -= mp(table, to_f32(row.p[row.id]));
+            left -= mp(table, to_f32(row.p[row.id]));
+        return {sp, 0, left, 0, 0};
     }
-    return a;
 }
 
 // The sum of a number a thread over the CTA, in every thread.
@@ -489,8 +615,22 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             set_status(g.status, bits);
         }
     };
-    if (r.on && r.ok && !r.greedy)
-        fill_table(sh.table, sh.parts);
+    const InT *z0 = static_cast<const InT *>(g.z) + ((int64_t)r.a + b) * g.ld;
+    const InT *d0 = g.zd ? static_cast<const InT *>(g.zd) + (int64_t)r.a * g.ldd : nullptr;
+    // what the first kernel does not change
+    if (r.on && r.ok) {
+        for (int i = tid; i <= r.n; i += NT) {
+            Level &v = sh.level[i];
+            v.id = i < r.n ? g.ids[r.a + i] : -1;
+            v.u = i < r.n ? g.u[r.a + i] : 0.0f;
+            const bool in = v.id >= 0 && v.id < g.V;
+            v.zx = in ? to_f32(z0[i * g.ld + v.id]) : 0.0f;
+            v.dx = in && r.model ? to_f32(d0[i * g.ldd + v.id]) : 0.0f;
+        }
+        if (!r.greedy)
+            fill_table(sh.table, sh.parts);
+    }
+    __syncthreads();
     grid_wait();
     if (!r.on || !r.ok) {  // as every CTA of the request finds
         if (rank == 0) {
@@ -506,27 +646,38 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     }
     const Scale sc = device_scale(r.greedy ? 1.0f : r.tau);
     const Scale one{1.0f, 0.0f, kLog2e, kHugeLogit};
-    const InT *z0 = static_cast<const InT *>(g.z) + ((int64_t)r.a + b) * g.ld;
-    const InT *d0 = g.zd ? static_cast<const InT *>(g.zd) + (int64_t)r.a * g.ldd : nullptr;
 
     // Every row's stretches together, a warp a row.
     for (int i = w; i <= r.n; i += kWarps) {
-        const bool in = lane < g.chunks, draft = r.model && i < r.n;
+        const bool draft = r.model && i < r.n;
         const Scale sd = device_scale(draft ? r.tau_d : 1.0f);
-        Part p = {};
-        p.m = p.md = -INFINITY;
-        if (in)
-            p = g.parts[((int64_t)i * g.B + b) * g.chunks + lane];
-        float M = p.m, Md = p.md;
+        const Part *parts = g.parts + ((int64_t)i * g.B + b) * g.stretches;
+        Part p[kMaxStretches / 32];
+        float M = -INFINITY, Md = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < kMaxStretches / 32; ++c) {
+            p[c] = Part{-INFINITY, 0.0f, 0.0f, 0x7fffffff, -INFINITY, 0.0f, {0, 0}};
+            if (lane + 32 * c < g.stretches)
+                p[c] = parts[lane + 32 * c];
+            M = fmaxf(M, p[c].m);
+            Md = draft ? fmaxf(Md, p[c].md) : Md;
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
             Md = fmaxf(Md, __shfl_xor_sync(0xffffffffu, Md, o));
         }
-        float s = in ? p.s * share_of(p.m, M, sc) : 0.0f;
-        float s1 = in ? p.s1 * share_of(p.m, M, one) : 0.0f;
-        float sq = in && draft ? p.sd * share_of(p.md, Md, sd) : 0.0f;
-        int arg = in && p.m == M ? p.arg : 0x7fffffff;
+        float s = 0.0f, s1 = 0.0f, sq = 0.0f;
+        int arg = 0x7fffffff;
+#pragma unroll
+        for (int c = 0; c < kMaxStretches / 32; ++c)
+            if (lane + 32 * c < g.stretches) {
+                s += p[c].s * share_of(p[c].m, M, sc);
+                s1 += p[c].s1 * share_of(p[c].m, M, one);
+                if (draft)
+                    sq += p[c].sd * share_of(p[c].md, Md, sd);
+                arg = p[c].m == M ? min(arg, p[c].arg) : arg;
+            }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -535,37 +686,38 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             arg = min(arg, __shfl_xor_sync(0xffffffffu, arg, o));
         }
         if (lane == 0) {
-            Level v = {M, s, s1, Md, sq, 0.0f, 0.0f, arg, -1, kAccept};
-            const float u = i < r.n ? g.u[r.a + i] : 0.0f;
+            Level &v = sh.level[i];
+            v.m = M;
+            v.s = s;
+            v.s1 = s1;
+            v.md = Md;
+            v.sd = sq;
+            v.arg = arg;
+            v.state = kAccept;
             if (!(s > 0.0f && s < INFINITY) || !(fabsf(M) < INFINITY) ||
-                !(u >= 0.0f && u < 1.0f) ||
+                !(v.u >= 0.0f && v.u < 1.0f) ||
                 (draft && (!(sq > 0.0f && sq < INFINITY) || !(fabsf(Md) < INFINITY)))) {
                 v.state = kBadRow;
-            } else if (i < r.n) {
-                v.id = g.ids[r.a + i];
-                if (v.id < 0 || v.id >= g.V) {
-                    v.state = kBadDraft;
-                } else {
-                    v.zx = to_f32(z0[i * g.ld + v.id]);
-                    if (r.greedy) {
-                        v.state = v.id == arg ? kAccept : kReject;
-                    } else {
-                        // (2^-21 more than the sums; where fp32 has no such number the draft is
-                        // left open too)
-                        const float px = share_of(v.zx, M, sc) / s;
-                        float uq = u;
-                        if (draft) {
-                            v.dx = to_f32(d0[i * g.ldd + v.id]);
-                            uq *= share_of(v.dx, Md, sd) / sq;
-                        }
-                        const float most = fmaxf(px, uq);
-                        v.state = fabsf(px - uq) > 0x1p-16f * most && most > 1e-30f
-                                      ? (uq < px ? kAccept : kReject)
-                                      : kOpen;
-                    }
+            } else if (i < r.n && (v.id < 0 || v.id >= g.V)) {
+                v.state = kBadDraft;
+            } else if (r.greedy) {
+                if (i < r.n)
+                    v.state = v.id == arg ? kAccept : kReject;
+            } else {
+                v.p.set(M, r.tau, sc, s, RowShare::kDepth);
+                if (draft)
+                    v.q.set(Md, r.tau_d, sd, sq, RowShare::kDepth + 0.2f);
+                if (i < r.n) {
+                    // (2^-21 more than the sums; where fp32 has no such number the draft is left
+                    // open too)
+                    const float px = share_of(v.zx, M, sc) / s;
+                    const float uq = draft ? v.u * (share_of(v.dx, Md, sd) / sq) : v.u;
+                    const float most = fmaxf(px, uq);
+                    v.state = fabsf(px - uq) > 0x1p-16f * most && most > 1e-30f
+                                  ? (uq < px ? kAccept : kReject)
+                                  : kOpen;
                 }
             }
-            sh.level[i] = v;
         }
     }
     __syncthreads();
@@ -600,22 +752,16 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     }
 
     // The row's masses, a warp a segment.
-    const int segs = g.groups * kWarps;
+    const int segs = g.segments, own_segs = segs / g.groups;
     Segment *mine = g.segs + (int64_t)b * segs;
     int32_t *undecided = g.undecided + (int64_t)b * segs * kListed;
     DrawRow<InT> row;
     auto enter = [&] {
         const Level &v = sh.level[k];
         row.enter(z0 + k * g.ld, v.id >= 0 && r.model ? d0 + k * g.ldd : nullptr, g.V, v.id, segs);
-        __syncthreads();
-        if (tid == 0)
-            sh.p.set(v.m, r.tau, sc, v.s);
-        if (tid == 32 && row.q)
-            sh.q.set(v.md, r.tau_d, device_scale(r.tau_d), v.sd);
-        __syncthreads();
     };
     auto sums = [&](int from, int to) {
-        const RowShare mp = sh.p, mq = sh.q;
+        const RowShare mp = sh.level[k].p, mq = sh.level[k].q;
         for (int s = from + w; s < to; s += kWarps) {
             int32_t *list = undecided + (int64_t)s * kListed;
             int *count = &sh.undecided[w];
@@ -629,7 +775,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
         }
     };
     enter();
-    sums(rank * kWarps, rank * kWarps + kWarps);
+    sums(rank * own_segs, (rank + 1) * own_segs);
     if (g.groups > 1) {  // the request's last CTA goes on
         __threadfence();
         __syncthreads();
@@ -642,21 +788,24 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     } else {
         __syncthreads();
     }
-    const RowShare *mp = &sh.p, *mq = &sh.q;
     bool minus = false;
     mass_t delta = 0, left = 0;
     auto off = [&](mass_t Q) {  // Q (1 + delta)
         const mass_t x = __umul64hi(Q, delta);
         return minus ? Q - x : Q + x;
     };
-    auto mass = [&](int j) -> mass_t {
-        const mass_t P = (*mp)(sh.table, to_f32(row.p[j]));
+    auto mass_of = [&](int j, float z, float d) -> mass_t {
+        const Level &v = sh.level[k];
+        const mass_t P = v.p(sh.table, z);
         if (!row.residual)
             return P;
         if (!row.q)
             return j == row.id ? 0 : P;
-        const mass_t Q = off((*mq)(sh.table, to_f32(row.q[j])));
+        const mass_t Q = off(v.q(sh.table, d));
         return P > Q ? P - Q : 0;
+    };
+    auto mass = [&](int j) {
+        return mass_of(j, to_f32(row.p[j]), row.q ? to_f32(row.q[j]) : 0.0f);
     };
     for (;;) {
         Segment a = {};
@@ -673,10 +822,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                     return exp(((double)z - (double)M) / (double)tau -
                                (double)unit * (0.693147180559945309417 / kSteps)) / (double)sum;
                 };
-                const double P = share(v.zx, v.m, r.tau, sh.p.unit, sp);
-                const double Q = row.q ? share(v.dx, v.md, r.tau_d, sh.q.unit, sq)
+                const double P = share(v.zx, v.m, r.tau, v.p.unit, sp);
+                const double Q = row.q ? share(v.dx, v.md, r.tau_d, v.q.unit, sq)
                                        : 1.0 / (double)(1ull << kUnitBits);
-                v.state = (double)g.u[r.a + k] * Q < P ? kAccept : kReject;
+                v.state = (double)v.u * Q < P ? kAccept : kReject;
             }
             __syncthreads();
             const int was = k;
@@ -707,32 +856,23 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             delta = sh.delta;
             const mass_t x = __umul64hi(a.q_left, delta);
             left = minus ? left + x : left - x;
-            // the entries that were undecided: a warp a segment
-            sh.more[tid] = a.undecided;
-            __syncthreads();
-            for (int s = w; s < segs; s += kWarps) {
-                const int n = (int)sh.more[s];
-                if (n == 0)
-                    continue;
+            // the entries that were undecided, a thread a segment; where there were too many, all
+            const int n = (int)a.undecided;
+            if (n <= kListed)
+                for (int i = 0; i < n; ++i)
+                    left += mass(__ldcg(undecided + (int64_t)tid * kListed + i));
+            const unsigned many = __ballot_sync(0xffffffffu, n > kListed);
+            for (unsigned bits = many; bits; bits &= bits - 1) {
+                const int s = 32 * w + __ffs(bits) - 1;
                 mass_t own = 0;
-                if (n <= kListed) {
-                    if (lane < n)
-                        own = mass(__ldcg(undecided + (int64_t)s * kListed + lane));
-                } else {
-                    for (int j = row.start(s) + lane; j < row.start(s + 1); j += 32)
-                        own += mass(j);
-                }
+                for (int j = row.start(s) + lane; j < row.start(s + 1); j += 32)
+                    own += mass(j);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1)
                     own += __shfl_xor_sync(0xffffffffu, own, o);
-                __syncwarp();
-                if (lane == 0)
-                    sh.more[s] = own;
+                if (tid == s)
+                    left = own;
             }
-            __syncthreads();
-            if (a.undecided)
-                left = sh.more[tid] + (a.undecided > kListed ? 0 : left);
-            __syncthreads();
         }
         const mass_t R = cta_sum(left, sh.warps[0]);
         if (R > 0) {
@@ -754,19 +894,45 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             const int a0 = min(s1, s0 + tid * per), a1 = min(s1, a0 + per);
             mass_t own = 0;
             int end = -1;  // the last entry with a mass
-#pragma unroll 4
-            for (int j = a0; j < a1; ++j) {
-                const mass_t m = mass(j);
-                own += m;
-                end = m ? j : end;
+            for (int j = a0; j < a1; j += 4) {
+                float z[4], d[4];
+                mass_t m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[i] = j + i < a1 ? to_f32(row.p[j + i]) : -INFINITY;
+                    d[i] = j + i < a1 && row.q ? to_f32(row.q[j + i]) : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    m[i] = mass_of(j + i, z[i], d[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    own += m[i];
+                    end = m[i] ? j + i : end;
+                }
             }
             atomicMax(&sh.end, end);
             mass_t at = cta_before(own, sh.warps[0]);
-            if (at <= rest && rest < at + own) {
-                int j = a0;
-                while ((at += mass(j)) <= rest)
-                    ++j;
-                sh.found = j;
+            const unsigned hit = __ballot_sync(0xffffffffu, at <= rest && rest < at + own);
+            if (hit) {  // the thread's entries, over its warp
+                const int src = __ffs(hit) - 1, e = __shfl_sync(0xffffffffu, a1, src);
+                int j = __shfl_sync(0xffffffffu, a0, src);
+                mass_t passed = __shfl_sync(0xffffffffu, at, src);
+                for (;; j += 32) {
+                    mass_t run = j + lane < e ? mass(j + lane) : 0;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const mass_t y = __shfl_up_sync(0xffffffffu, run, o);
+                        run += lane >= o ? y : 0;
+                    }
+                    const unsigned over = __ballot_sync(0xffffffffu, passed + run > rest);
+                    if (over) {
+                        if (lane == 0)
+                            sh.found = j + __ffs(over) - 1;
+                        break;
+                    }
+                    passed += __shfl_sync(0xffffffffu, run, 31);
+                }
             }
             __syncthreads();
             // (a segment's sum and its entries' are off from each other by their roundings, a unit
@@ -785,34 +951,43 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     }
 }
 
-// A row's stretches: as many CTAs as fill the SMs four times, 512 vectors at least each.
-int chunks_of(int64_t B, int64_t D, int64_t V, int in_bytes)
+// A row's stretches: as many warps as the SMs hold at a time (24 each), or 256 vectors at least.
+int stretches_of(int64_t B, int64_t D, int64_t V, int in_bytes)
 {
-    const int64_t nvec = V * in_bytes / 16, items = B * (D + 1);
-    int64_t c = (608 + items - 1) / items;
-    c = c < nvec / 512 ? c : nvec / 512;
-    c = c < kMaxChunks ? c : kMaxChunks;
+    const int64_t nvec = V * in_bytes / 16;
+    int64_t c = 24 * 152 / (B * (2 * D + 1));
+    c = c < nvec / 256 ? c : nvec / 256;
+    c = c < kMaxStretches ? c : kMaxStretches;
     return c < 1 ? 1 : (int)c;
 }
 
-// The second kernel's CTAs a request: as many again, 256 entries a segment at least, and no more
-// segments than a CTA has threads.
+// The second kernel's CTAs a request: four an SM in all, 256 entries a segment at least, and no
+// more segments than a CTA has threads.
 int groups_of(int64_t B, int64_t V)
 {
-    int64_t c = (608 + B - 1) / B;
+    int64_t c = 608 / B;
     c = c < V / (256 * kWarps) ? c : V / (256 * kWarps);
     c = c < kVerifyThreads / kWarps ? c : kVerifyThreads / kWarps;
     return c < 1 ? 1 : (int)c;
 }
 
+// Their segments: a multiple of the groups' warps, of 1024 entries at most where that many fit a
+// CTA's threads.
+int segments_of(int64_t V, int groups)
+{
+    const int step = groups * kWarps, most = kVerifyThreads / step * step;
+    const int64_t want = (V + 1023) / 1024, up = (want + step - 1) / step * step;
+    return (int)(up < most ? up : most);
+}
+
 struct VerifyLayout {
     size_t segs, undecided, tickets, total;
 };
-VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D, int chunks)
+VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D, int stretches)
 {
     VerifyLayout l;
-    l.segs = ws_round_up((size_t)B * (size_t)(D + 1) * (size_t)chunks * sizeof(Part));
-    const size_t n = (size_t)B * groups_of(B, V) * kWarps;
+    l.segs = ws_round_up((size_t)B * (size_t)(D + 1) * (size_t)stretches * sizeof(Part));
+    const size_t n = (size_t)B * segments_of(V, groups_of(B, V));
     l.undecided = l.segs + ws_round_up(n * sizeof(Segment));
     l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(int32_t));
     l.total = l.tickets + ws_round_up((size_t)B * sizeof(uint32_t));
@@ -821,12 +996,17 @@ VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D, int chunks)
 
 template <typename InT> cudaError_t launch_verify(const VerifyArgs &g, cudaStream_t s)
 {
-    const unsigned grid = (unsigned)((int64_t)g.B * (g.D + 1) * g.chunks);
-    if ((int64_t)g.V * (int)sizeof(InT) / 16 <= 4096 * (int64_t)g.chunks)
-        cis_verify_rows_kernel<InT, 1><<<grid, kVerifyThreads, 0, s>>>(g);
-    else
-        cis_verify_rows_kernel<InT, 4><<<grid, kVerifyThreads, 0, s>>>(g);
-    cudaError_t e = cudaGetLastError();
+    const int64_t rows = (int64_t)g.B * (g.zd ? 2 * g.D + 1 : g.D + 1);
+    // The second kernel's CTAs start beside the first one's: they need the shared memory that an SM
+    // would else have given to its L1 (on the few SMs that were free they took 20,000 cycles for a
+    // request of V=151936, for 7,500).
+    cudaError_t e = cudaFuncSetAttribute(cis_verify_rows_kernel<InT>,
+                                         cudaFuncAttributePreferredSharedMemoryCarveout, 60);
+    if (e != cudaSuccess)
+        return e;
+    cis_verify_rows_kernel<InT>
+        <<<(unsigned)((rows * g.stretches + kWarps - 1) / kWarps), kVerifyThreads, 0, s>>>(g);
+    e = cudaGetLastError();
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
@@ -859,7 +1039,7 @@ extern "C" CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, 
     if (bytes == nullptr || !verify_sizes_ok(B, V, max_drafts))
         return CIS_ERR_INVALID_ARG;
     const int64_t n = B > 0 ? B : 1;
-    const int c = chunks_of(n, max_drafts, V, 4);  // (bf16 rows have no more)
+    const int c = stretches_of(n, max_drafts, V, 4);  // (bf16 rows have no more)
     *bytes = verify_layout(n, V, max_drafts, c).total;
     return CIS_OK;
 }
@@ -910,9 +1090,10 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     g.lp = lp_out;
     g.lps = lp_sampled_out;
     g.status = dev_status;
-    g.chunks = chunks_of(B, max_drafts, V, dtype == CIS_BF16 ? 2 : 4);
+    g.stretches = stretches_of(B, max_drafts, V, dtype == CIS_BF16 ? 2 : 4);
     g.groups = groups_of(B, V);
-    const VerifyLayout l = verify_layout(B, V, max_drafts, g.chunks);
+    g.segments = segments_of(V, g.groups);
+    const VerifyLayout l = verify_layout(B, V, max_drafts, g.stretches);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     g.parts = reinterpret_cast<Part *>(ws);
     g.segs = reinterpret_cast<Segment *>(ws + l.segs);
