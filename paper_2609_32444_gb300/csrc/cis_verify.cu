@@ -48,7 +48,7 @@ struct VerifyArgs {
     int32_t *tokens, *kept;
     float *lp, *lps;
     int32_t *status;
-    Part *parts;  // [D + 1][B][stretches]
+    Part *parts;  // [N + B][stretches]
     int stretches;
     struct Segment *segs;  // [B][segments]
     int32_t *undecided;    // [B][segments][kListed]
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3)
         }
     }
     const MaxSumU o = warp_exp(acc);
-    Part &out = g.parts[((int64_t)i * g.B + b) * g.stretches + st];
+    Part &out = g.parts[((int64_t)r.a + b + i) * g.stretches + st];
     if (draft) {
         if (lane == 0) {
             out.md = o.m;
@@ -243,14 +243,20 @@ __global__ void __launch_bounds__(kVerifyThreads, 3)
     const float s1 = two ? warp_exp(raw).s : o.s;
     int first = 0x7fffffff;
     if (r.greedy) {  // (read again, from L2)
-        for (int v = v0 + lane; v < v1; v += 32) {
-            Vec<InT> y[1];
-            y[0].q = __ldg(rv + v);
-            if (vec_max<1>(y) == o.m) {
+#pragma unroll 1
+        for (int v = v0 + lane; v < v1 && first == 0x7fffffff; v += 32 * kB) {
 #pragma unroll
-                for (int e = EV - 1; e >= 0; --e)
-                    first = y[0].entry(e) == o.m ? head + v * EV + e : first;
-                break;
+            for (int k = 0; k < kB; ++k)
+                x[k].q = __ldg(rv + min(v + 32 * k, v1 - 1));
+#pragma unroll
+            for (int k = kB - 1; k >= 0; --k) {
+                const Vec<InT> y[1] = {x[k]};
+                if (vec_max<1>(y) == o.m) {
+#pragma unroll
+                    for (int e = EV - 1; e >= 0; --e)
+                        first = y[0].entry(e) == o.m ? head + min(v + 32 * k, v1 - 1) * EV + e
+                                                     : first;
+                }
             }
         }
         if (end >= 0 && zend == o.m)
@@ -407,6 +413,8 @@ struct RequestShared {
     mass_t parts[96];
     mass_t warps[2][kWarps];
     mass_t goal, rest, delta;
+    unsigned many[kWarps];        // segments with too many undecided entries, and
+    mass_t more[kVerifyThreads];  // what is left in them
     int undecided[kWarps];
     int minus, seg, found, end, last;
 };
@@ -651,7 +659,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     for (int i = w; i <= r.n; i += kWarps) {
         const bool draft = r.model && i < r.n;
         const Scale sd = device_scale(draft ? r.tau_d : 1.0f);
-        const Part *parts = g.parts + ((int64_t)i * g.B + b) * g.stretches;
+        const Part *parts = g.parts + ((int64_t)r.a + b + i) * g.stretches;
         Part p[kMaxStretches / 32];
         float M = -INFINITY, Md = -INFINITY;
 #pragma unroll
@@ -807,6 +815,19 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     auto mass = [&](int j) {
         return mass_of(j, to_f32(row.p[j]), row.q ? to_f32(row.q[j]) : 0.0f);
     };
+    auto four = [&](const int (&j)[4]) {  // the masses of four entries (-1: none)
+        float z[4], d[4];
+        mass_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            z[i] = j[i] >= 0 ? to_f32(row.p[j[i]]) : -INFINITY;
+            d[i] = j[i] >= 0 && row.q ? to_f32(row.q[j[i]]) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sum += mass_of(j[i], z[i], d[i]);
+        return sum;
+    };
     for (;;) {
         Segment a = {};
         for (int s = tid; s < segs; s += NT)  // (segs <= NT)
@@ -857,22 +878,41 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             const mass_t x = __umul64hi(a.q_left, delta);
             left = minus ? left + x : left - x;
             // the entries that were undecided, a thread a segment; where there were too many, all
+            // of them, a warp a segment
             const int n = (int)a.undecided;
-            if (n <= kListed)
-                for (int i = 0; i < n; ++i)
-                    left += mass(__ldcg(undecided + (int64_t)tid * kListed + i));
             const unsigned many = __ballot_sync(0xffffffffu, n > kListed);
-            for (unsigned bits = many; bits; bits &= bits - 1) {
-                const int s = 32 * w + __ffs(bits) - 1;
-                mass_t own = 0;
-                for (int j = row.start(s) + lane; j < row.start(s + 1); j += 32)
-                    own += mass(j);
+            if (n <= kListed)
+                for (int i = 0; i < n; i += 4) {
+                    const int4 q = __ldcg(reinterpret_cast<const int4 *>(
+                        undecided + (int64_t)tid * kListed + i));
+                    const int j[4] = {q.x, i + 1 < n ? q.y : -1, i + 2 < n ? q.z : -1,
+                                      i + 3 < n ? q.w : -1};
+                    left += four(j);
+                }
+            if (lane == 0)
+                sh.many[w] = many;
+            __syncthreads();
+            for (int i = 0; i < kWarps; ++i)
+                for (unsigned bits = sh.many[i]; bits; bits &= bits - 1) {
+                    const int s = 32 * i + __ffs(bits) - 1;
+                    if (s % kWarps != w)
+                        continue;
+                    mass_t own = 0;
+                    const int e = row.start(s + 1);
+                    for (int j0 = row.start(s) + lane; j0 < e; j0 += 128) {
+                        const int j[4] = {j0, j0 + 32 < e ? j0 + 32 : -1, j0 + 64 < e ? j0 + 64 : -1,
+                                          j0 + 96 < e ? j0 + 96 : -1};
+                        own += four(j);
+                    }
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    own += __shfl_xor_sync(0xffffffffu, own, o);
-                if (tid == s)
-                    left = own;
-            }
+                    for (int o = 16; o > 0; o >>= 1)
+                        own += __shfl_xor_sync(0xffffffffu, own, o);
+                    if (lane == 0)
+                        sh.more[s] = own;
+                }
+            __syncthreads();
+            if (n > kListed)
+                left = sh.more[tid];
         }
         const mass_t R = cta_sum(left, sh.warps[0]);
         if (R > 0) {
@@ -951,11 +991,13 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     }
 }
 
-// A row's stretches: as many warps as the SMs hold at a time (24 each), or 256 vectors at least.
-int stretches_of(int64_t B, int64_t D, int64_t V, int in_bytes)
+// A row's stretches: as many warps in all as the SMs hold at a time (24 each), 256 vectors each at
+// least.
+constexpr int64_t kRowWarps = 24 * 152;
+int stretches_of(int64_t rows, int64_t V, int in_bytes)
 {
     const int64_t nvec = V * in_bytes / 16;
-    int64_t c = 24 * 152 / (B * (2 * D + 1));
+    int64_t c = kRowWarps / rows;
     c = c < nvec / 256 ? c : nvec / 256;
     c = c < kMaxStretches ? c : kMaxStretches;
     return c < 1 ? 1 : (int)c;
@@ -983,10 +1025,11 @@ int segments_of(int64_t V, int groups)
 struct VerifyLayout {
     size_t segs, undecided, tickets, total;
 };
-VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D, int stretches)
+VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D)
 {
     VerifyLayout l;
-    l.segs = ws_round_up((size_t)B * (size_t)(D + 1) * (size_t)stretches * sizeof(Part));
+    // (rows times their stretches: no more than the warps, or the rows)
+    l.segs = ws_round_up((size_t)(B * (D + 1) + kRowWarps) * sizeof(Part));
     const size_t n = (size_t)B * segments_of(V, groups_of(B, V));
     l.undecided = l.segs + ws_round_up(n * sizeof(Segment));
     l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(int32_t));
@@ -1039,8 +1082,7 @@ extern "C" CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, 
     if (bytes == nullptr || !verify_sizes_ok(B, V, max_drafts))
         return CIS_ERR_INVALID_ARG;
     const int64_t n = B > 0 ? B : 1;
-    const int c = stretches_of(n, max_drafts, V, 4);  // (bf16 rows have no more)
-    *bytes = verify_layout(n, V, max_drafts, c).total;
+    *bytes = verify_layout(n, V, max_drafts).total;
     return CIS_OK;
 }
 
@@ -1090,10 +1132,10 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     g.lp = lp_out;
     g.lps = lp_sampled_out;
     g.status = dev_status;
-    g.stretches = stretches_of(B, max_drafts, V, dtype == CIS_BF16 ? 2 : 4);
+    g.stretches = stretches_of(N * (draft_logits ? 2 : 1) + B, V, dtype == CIS_BF16 ? 2 : 4);
     g.groups = groups_of(B, V);
     g.segments = segments_of(V, g.groups);
-    const VerifyLayout l = verify_layout(B, V, max_drafts, g.stretches);
+    const VerifyLayout l = verify_layout(B, V, max_drafts);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     g.parts = reinterpret_cast<Part *>(ws);
     g.segs = reinterpret_cast<Segment *>(ws + l.segs);
