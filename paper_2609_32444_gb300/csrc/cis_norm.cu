@@ -12,6 +12,7 @@
 // every row starts on 16 bytes and else an element at a time; each tensor is read once.  In the
 // backward kernel a thread has the same columns in every row that it takes, so that dweight's sum
 // stays in its registers (16 of them); the CTAs' sums meet in the workspace, in a fixed order.
+// Its threads are few for their registers, so that rows are copied ahead to shared memory.
 //
 // Bound: HBM for many rows; for few, the latency of a load, a reduction and a store.
 #include <cuda_fp8.h>
@@ -50,6 +51,13 @@ template <> struct Pack<__nv_bfloat16, 8> {
     {
         q = __ldg(reinterpret_cast<const uint4 *>(p));
     }
+    __device__ __forceinline__ void shared(uint32_t a)
+    {
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
+                     : "r"(a)
+                     : "memory");
+    }
     __device__ __forceinline__ void get(float (&f)[8]) const
     {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -66,6 +74,13 @@ template <> struct Pack<float, 4> {
     {
         q = __ldg(reinterpret_cast<const float4 *>(p));
     }
+    __device__ __forceinline__ void shared(uint32_t a)
+    {
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w)
+                     : "r"(a)
+                     : "memory");
+    }
     __device__ __forceinline__ void get(float (&f)[4]) const
     {
         f[0] = q.x;
@@ -77,6 +92,11 @@ template <> struct Pack<float, 4> {
 template <typename T> struct Pack<T, 1> {
     T q;
     __device__ __forceinline__ void load(const T *p) { q = __ldg(p); }
+    __device__ __forceinline__ void shared(uint32_t a)
+    {
+        if constexpr (sizeof(T) == 4)
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(q) : "r"(a) : "memory");
+    }
     __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(q); }
 };
 
@@ -182,7 +202,121 @@ __device__ __forceinline__ void row_reduce(float &s, float &m, float2 (*slots)[3
 
 template <int TPR> constexpr int kCta = TPR < 128 ? 128 : TPR;
 
-// The forward kernel: TPR threads a row, V vectors of E elements each.
+// The rows of a group of threads, t = first, first + step, ..., and which of the next ones count
+// (bit i: row t + i step): the mask is read before the loads that it decides about, and what was
+// read is looked at a row later.
+struct RowWalk {
+    static constexpr int kKnown = 8;
+    const uint8_t *mask;
+    int64_t T, step, t;
+    unsigned bits, more;
+    __device__ __forceinline__ RowWalk(const uint8_t *m, int64_t T_, int64_t first, int64_t step_)
+        : mask(m), T(T_), step(step_), t(first), bits(0)
+    {
+        unsigned v[kKnown];
+#pragma unroll
+        for (int i = 0; i < kKnown; ++i)
+            v[i] = valid(t + i * step);
+#pragma unroll
+        for (int i = 0; i < kKnown; ++i)
+            bits |= (unsigned)(v[i] != 0) << i;
+        more = valid(t + kKnown * step);
+    }
+    __device__ __forceinline__ unsigned valid(int64_t r) const
+    {
+        return r < T ? (mask ? (unsigned)__ldg(mask + r) : 1u) : 0u;
+    }
+    __device__ __forceinline__ bool on(int i) const { return bits >> i & 1; }
+    __device__ __forceinline__ void advance()
+    {
+        bits = bits >> 1 | (unsigned)(more != 0) << (kKnown - 1);
+        t += step;
+        more = valid(t + kKnown * step);
+    }
+};
+
+// K tensors' rows on their way: a thread copies what it will use itself, V vectors of E elements of
+// each, into places of its own in shared memory, S - 1 rows ahead, and waits for nobody else.
+// Elements of 2 bytes by themselves cannot be copied so: they are loaded when they are used.
+template <typename T, int E, int NT, int V, int K, int S> struct Rows {
+    static constexpr bool kAsync = sizeof(Pack<T, E>) >= 4;
+    static constexpr size_t kBytes = kAsync ? sizeof(Pack<T, E>) * NT * V * K * S : 0;
+    const T *base[K];  // this thread's first element of row 0 (null: no such tensor)
+    int64_t ld[K];
+    int left, stride;  // elements from this thread's first on, and between its vectors
+    uint32_t place;
+    int stage = 0;
+
+    __device__ __forceinline__ void copy(int64_t t, int s)
+    {
+        if constexpr (kAsync) {
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+                if (base[i]) {
+                    const T *row = base[i] + t * ld[i];
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k * stride < left) {
+                            const uint32_t to =
+                                place + (uint32_t)(((s * K + i) * V + k) * NT *
+                                                   sizeof(Pack<T, E>));
+                            if constexpr (sizeof(Pack<T, E>) == 16)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to),
+                                             "l"(row + k * stride)
+                                             : "memory");
+                            else
+                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to),
+                                             "l"(row + k * stride)
+                                             : "memory");
+                        }
+                }
+        }
+    }
+    // The first S - 1 rows.
+    __device__ __forceinline__ void start(const RowWalk &w)
+    {
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) {
+            if (w.on(i))
+                copy(w.t + i * w.step, i);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    }
+    // The current row, and one more on its way.
+    __device__ __forceinline__ void take(const RowWalk &w, Pack<T, E> (&p)[K][V])
+    {
+        if constexpr (kAsync) {
+            const int next = stage == 0 ? S - 1 : stage - 1;
+            if (w.on(S - 1))
+                copy(w.t + (S - 1) * w.step, next);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            if (w.on(0)) {
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    if (base[i])
+#pragma unroll
+                        for (int k = 0; k < V; ++k)
+                            if (k * stride < left)
+                                p[i][k].shared(place + (uint32_t)(((stage * K + i) * V + k) * NT *
+                                                                  sizeof(Pack<T, E>)));
+            }
+            stage = stage + 1 == S ? 0 : stage + 1;
+        } else if (w.on(0)) {
+#pragma unroll
+            for (int i = 0; i < K; ++i)
+                if (base[i])
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k * stride < left)
+                            p[i][k].load(base[i] + w.t * ld[i] + k * stride);
+        }
+    }
+};
+
+// The forward kernel: TPR threads a row, V vectors of E elements each.  Enough CTAs hide one
+// another's latencies (rows copied ahead, as in the backward kernel, took 41 us for 38 at T=16384,
+// H=2048, 40% padding; weights kept in registers, or packed instructions, 43).
 template <typename T, int E, int TPR, int V>
 __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormArgs a)
 {
@@ -280,54 +414,67 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
     }
 }
 
-// The backward kernel.
-template <typename T, int E, int TPR, int V>
-__global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_bwd_kernel(const NormArgs a)
+// The backward kernel's threads an SM, whose rows on their way have kRowBytes of its shared memory
+// (640 threads spill; 8 elements a thread and 768 took 49 us for 42 at T=16384, H=2048, 40% padding).
+constexpr int kBwdThreads = 512, kRowBytes = 200 * 1024;
+constexpr int kMaxSms = 256;
+// CTAs of TPR threads (128 at least) an SM.
+constexpr int ctas_of(int tpr, int threads)
 {
-    constexpr int R = kCta<TPR> / TPR;
+    return threads > tpr && threads > 128 ? threads / (tpr < 128 ? 128 : tpr) : 1;
+}
+// The backward kernel.
+template <typename T, int E, int TPR, int V, int S>
+__global__ void __launch_bounds__(kCta<TPR>, ctas_of(TPR, kBwdThreads))
+    cis_rmsnorm_bwd_kernel(const NormArgs a)
+{
+    constexpr int R = kCta<TPR> / TPR, kStep = TPR * E;
+    extern __shared__ __align__(16) uint8_t dyn_smem[];
     __shared__ float2 slots[2][32];
-    const int at = TPR > 32 ? threadIdx.x : threadIdx.x & 31;
+    if (threadIdx.x == 0)
+        allow_next_grid();
+    const int at = (TPR > 32 ? threadIdx.x : threadIdx.x & 31) * E;
     const int group = TPR > 32 ? 0 : threadIdx.x >> 5;
     int turn = 0;
     float acc[V][E] = {};
-    for (int64_t t = (int64_t)blockIdx.x * R + group; t < a.T; t += (int64_t)gridDim.x * R) {
-        T *dx = static_cast<T *>(a.y_out) + t * a.H;
-        if (a.mask && !a.mask[t]) {
+    RowWalk row(a.mask, a.T, (int64_t)blockIdx.x * R + group, (int64_t)gridDim.x * R);
+    using In = Rows<T, E, kCta<TPR>, V, 3, S>;
+    In in{{static_cast<const T *>(a.dy) + at, static_cast<const T *>(a.x) + at,
+           a.residual ? static_cast<const T *>(a.residual) + at : nullptr},
+          {a.ld_dy, a.ld_x, a.ld_r}, a.H - at, kStep,
+          (uint32_t)__cvta_generic_to_shared(dyn_smem) +
+              (uint32_t)(threadIdx.x * sizeof(Pack<T, E>))};
+    in.start(row);
+    float w[V][E];
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (at + k * kStep < a.H)
+            weights_of(a, at + k * kStep, w[k]);
+    for (; row.t < a.T; row.advance()) {
+        T *dx = static_cast<T *>(a.y_out) + row.t * a.H;
+        Pack<T, E> now[3][V];
+        in.take(row, now);
+        if (!row.on(0)) {
             float z[E] = {};
             for (int k = 0; k < V; ++k) {
-                const int j = (at + k * TPR) * E;
+                const int j = at + k * kStep;
                 if (j < a.H)
                     put(dx + j, z);
             }
             continue;
         }
-        const T *dy = static_cast<const T *>(a.dy) + t * a.ld_dy;
-        const T *h = static_cast<const T *>(a.x) + t * a.ld_x;
-        const T *dh = a.residual ? static_cast<const T *>(a.residual) + t * a.ld_r : nullptr;
-        Pack<T, E> py[V], ph[V], pr[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int j = (at + k * TPR) * E;
-            if (j < a.H) {
-                py[k].load(dy + j);
-                ph[k].load(h + j);
-                if (dh)
-                    pr[k].load(dh + j);
-            }
-        }
         float s = 0.0f, gh = 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int j = (at + k * TPR) * E;
+            const int j = at + k * kStep;
             if (j < a.H) {
-                float w[E], y[E], x[E];
-                weights_of(a, j, w);
-                py[k].get(y);
-                ph[k].get(x);
+                float y[E], x[E];
+                now[0][k].get(y);
+                now[1][k].get(x);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     s = fmaf(x[i], x[i], s);
-                    gh = fmaf(y[i] * w[i], x[i], gh);
+                    gh = fmaf(y[i] * w[k][i], x[i], gh);
                 }
             }
         }
@@ -336,17 +483,16 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_bwd_kernel(const NormAr
         const float c = rstd * rstd * (gh / H);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int j = (at + k * TPR) * E;
+            const int j = at + k * kStep;
             if (j < a.H) {
-                float w[E], y[E], x[E], d[E] = {};
-                weights_of(a, j, w);
-                py[k].get(y);
-                ph[k].get(x);
-                if (dh)
-                    pr[k].get(d);
+                float y[E], x[E], d[E] = {};
+                now[0][k].get(y);
+                now[1][k].get(x);
+                if (a.residual)
+                    now[2][k].get(d);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    d[i] = fmaf(rstd, fmaf(-x[i], c, y[i] * w[i]), d[i]);
+                    d[i] = fmaf(rstd, fmaf(-x[i], c, y[i] * w[k][i]), d[i]);
                     acc[k][i] = fmaf(y[i], x[i] * rstd, acc[k][i]);
                 }
                 put(dx + j, d);
@@ -360,7 +506,7 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_bwd_kernel(const NormAr
         for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                part[group][(at + k * 32) * E + i] = acc[k][i];
+                part[group][at + k * kStep + i] = acc[k][i];
         __syncthreads();
         for (int j = threadIdx.x; j < a.H; j += kCta<TPR>) {
             float v = 0.0f;
@@ -374,7 +520,7 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_bwd_kernel(const NormAr
         for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const int j = (at + k * TPR) * E + i;
+                const int j = at + k * kStep + i;
                 if (j < a.H)
                     out[j] = acc[k][i];
             }
@@ -386,6 +532,7 @@ __global__ void __launch_bounds__(1024) cis_rmsnorm_dweight_kernel(const float *
                                                                    float *dw)
 {
     __shared__ float sh[32][33];
+    grid_wait();
     const int c = threadIdx.x & 31, w = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
     float s = 0.0f;
     if (j < H) {
@@ -411,42 +558,63 @@ cudaError_t sm_count(int *n)
 }
 
 // Backward CTAs: as many as the registers of an SM hold, whose sums the workspace keeps.
-constexpr int kBwdThreads = 512;  // a SM's, at most 128 registers each
-constexpr int kMaxSms = 256;
+// Backward CTAs: as many as run at a time, whose sums the workspace keeps.
 int64_t bwd_ctas(int64_t T, int tpr, int sms)
 {
     const int cta = tpr < 128 ? 128 : tpr, rows = cta / tpr;
-    const int64_t most = (int64_t)sms * (kBwdThreads > cta ? kBwdThreads / cta : 1);
+    const int64_t most = (int64_t)sms * ctas_of(tpr, kBwdThreads);
     const int64_t need = (T + rows - 1) / rows;
     return need < most ? need : most;
 }
-int64_t most_sums(int64_t T) { return T < kMaxSms * 4 ? T : kMaxSms * 4; }
+constexpr int64_t kMaxSums = kMaxSms * (kBwdThreads / 128);
+int64_t most_sums(int64_t T) { return T < kMaxSums ? T : kMaxSums; }
+
+// Rows on their way: four, or as many as fit.
+template <typename T, int E, int NT, int V, int K> constexpr int stages_of(int ctas)
+{
+    return Rows<T, E, NT, V, K, 4>::kBytes * ctas <= kRowBytes   ? 4
+           : Rows<T, E, NT, V, K, 2>::kBytes * ctas <= kRowBytes ? 2
+                                                                 : 1;
+}
 
 template <typename T, int E, int TPR, int V>
 cudaError_t launch(const NormArgs &a, bool bwd, void *workspace, cudaStream_t s)
 {
+    constexpr int NT = kCta<TPR>, R = NT / TPR;
     int sms = 0;
     cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess)
         return e;
     if (!bwd) {
-        constexpr int R = kCta<TPR> / TPR;
-        const int64_t need = (a.T + R - 1) / R, most = (int64_t)sms * (2048 / kCta<TPR>);
+        const int64_t need = (a.T + R - 1) / R, most = (int64_t)sms * (2048 / NT);
         cis_rmsnorm_fwd_kernel<T, E, TPR, V>
-            <<<(unsigned)(need < most ? need : most), kCta<TPR>, 0, s>>>(a);
+            <<<(unsigned)(need < most ? need : most), NT, 0, s>>>(a);
         return cudaGetLastError();
     }
+    constexpr int S = stages_of<T, E, NT, V, 3>(ctas_of(TPR, kBwdThreads));
+    constexpr size_t smem = Rows<T, E, NT, V, 3, S>::kBytes;
+    auto kern = cis_rmsnorm_bwd_kernel<T, E, TPR, V, S>;
+    if (smem > 32 * 1024 && (e = allow_smem(kern, smem)) != cudaSuccess)
+        return e;
     NormArgs b = a;
     const int64_t n = bwd_ctas(a.T, TPR, sms < kMaxSms ? sms : kMaxSms);
     if (n > 1)
         b.dw = static_cast<float *>(workspace);
-    cis_rmsnorm_bwd_kernel<T, E, TPR, V><<<(unsigned)n, kCta<TPR>, 0, s>>>(b);
+    kern<<<(unsigned)n, NT, smem, s>>>(b);
     e = cudaGetLastError();
     if (e != cudaSuccess || n <= 1)
         return e;
-    cis_rmsnorm_dweight_kernel<<<(unsigned)((a.H + 31) / 32), 1024, 0, s>>>(b.dw, (int)n, a.H,
-                                                                            a.dw);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.H + 31) / 32));
+    cfg.blockDim = dim3(1024);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, cis_rmsnorm_dweight_kernel, (const float *)b.dw, (int)n, a.H, a.dw);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 // By the row's length: 16 elements a thread (8 in the shortest rows, 32 in the longest).
