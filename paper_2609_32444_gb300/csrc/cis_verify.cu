@@ -366,7 +366,7 @@ struct TwoShares {
 };
 
 // The table: T[32 .. 64 steps] from 2^{i / 32} and 2^{j / 2048}, j < 64.
-__device__ inline void fill_table(mass_t *table, mass_t *parts)
+__device__ inline void fill_parts(mass_t *parts)
 {
     const int tid = threadIdx.x;
     auto whole = [](float s, float lo) {  // s + lo in [1, 2), in units of 2^-62
@@ -385,8 +385,11 @@ __device__ inline void fill_table(mass_t *table, mass_t *parts)
         const float2 T = kExp2Table[tid - 64];
         parts[tid] = whole(T.x, T.y);
     }
-    __syncthreads();
-    for (int i = tid; i < kSteps; i += kVerifyThreads)
+}
+__device__ inline void fill_table(mass_t *table, const mass_t *parts)
+{
+#pragma unroll
+    for (int i = threadIdx.x; i < kSteps; i += kVerifyThreads)
         table[i] = __umul64hi(parts[64 + (i >> 6)], parts[i & 63]) << 2;
 }
 
@@ -412,11 +415,11 @@ struct RequestShared {
     mass_t table[kSteps];
     mass_t parts[96];
     mass_t warps[2][kWarps];
-    mass_t goal, rest, delta;
+    mass_t rest;
     unsigned many[kWarps];        // segments with too many undecided entries, and
     mass_t more[kVerifyThreads];  // what is left in them
     int undecided[kWarps];
-    int minus, seg, found, end, last;
+    int seg, found, end, last;
 };
 
 // The rows that a token is drawn from.
@@ -563,24 +566,29 @@ __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const Ro
     }
 }
 
-// The sum of a number a thread over the CTA, in every thread.
-__device__ __forceinline__ mass_t cta_sum(mass_t x, mass_t *warps)
+// The sums of two numbers a thread over the CTA, in every thread.
+__device__ __forceinline__ void cta_sums(mass_t &x, mass_t &y, mass_t (*warps)[kWarps])
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = 16; o > 0; o >>= 1) {
         x += __shfl_xor_sync(0xffffffffu, x, o);
+        y += __shfl_xor_sync(0xffffffffu, y, o);
+    }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        warps[threadIdx.x >> 5] = x;
+    if ((threadIdx.x & 31) == 0) {
+        warps[0][threadIdx.x >> 5] = x;
+        warps[1][threadIdx.x >> 5] = y;
+    }
     __syncthreads();
-    x = 0;
+    x = y = 0;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i)
-        x += warps[i];
-    return x;
+    for (int i = 0; i < kWarps; ++i) {
+        x += warps[0][i];
+        y += warps[1][i];
+    }
 }
-// The sum of the threads before this one.
-__device__ __forceinline__ mass_t cta_before(mass_t x, mass_t *warps)
+// The sum of the threads before this one, and of all.
+__device__ __forceinline__ mass_t cta_before(mass_t x, mass_t *warps, mass_t &all)
 {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     mass_t run = x;
@@ -594,8 +602,12 @@ __device__ __forceinline__ mass_t cta_before(mass_t x, mass_t *warps)
         warps[w] = run;
     __syncthreads();
     run -= x;
-    for (int i = 0; i < w; ++i)
-        run += warps[i];
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        run += i < w ? warps[i] : 0;
+        all += warps[i];
+    }
     return run;
 }
 
@@ -625,18 +637,27 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     };
     const InT *z0 = static_cast<const InT *>(g.z) + ((int64_t)r.a + b) * g.ld;
     const InT *d0 = g.zd ? static_cast<const InT *>(g.zd) + (int64_t)r.a * g.ldd : nullptr;
-    // what the first kernel does not change
+    // what the first kernel does not change (a draft's logits are on their way while the table is
+    // filled)
+    static_assert(CIS_MAX_DRAFTS < NT, "a thread a level");
     if (r.on && r.ok) {
-        for (int i = tid; i <= r.n; i += NT) {
-            Level &v = sh.level[i];
-            v.id = i < r.n ? g.ids[r.a + i] : -1;
-            v.u = i < r.n ? g.u[r.a + i] : 0.0f;
-            const bool in = v.id >= 0 && v.id < g.V;
-            v.zx = in ? to_f32(z0[i * g.ld + v.id]) : 0.0f;
-            v.dx = in && r.model ? to_f32(d0[i * g.ldd + v.id]) : 0.0f;
-        }
+        const int id = tid < r.n ? g.ids[r.a + tid] : -1;
+        const float u = tid < r.n ? g.u[r.a + tid] : 0.0f;
+        if (!r.greedy)
+            fill_parts(sh.parts);
+        const bool in = id >= 0 && id < g.V;
+        const float zx = in ? to_f32(z0[tid * g.ld + id]) : 0.0f;
+        const float dx = in && r.model ? to_f32(d0[tid * g.ldd + id]) : 0.0f;
+        __syncthreads();
         if (!r.greedy)
             fill_table(sh.table, sh.parts);
+        if (tid <= r.n) {
+            Level &v = sh.level[tid];
+            v.id = id;
+            v.u = u;
+            v.zx = zx;
+            v.dx = dx;
+        }
     }
     __syncthreads();
     grid_wait();
@@ -815,6 +836,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     auto mass = [&](int j) {
         return mass_of(j, to_f32(row.p[j]), row.q ? to_f32(row.q[j]) : 0.0f);
     };
+    const float u_last = g.u_last[b];
     auto four = [&](const int (&j)[4]) {  // the masses of four entries (-1: none)
         float z[4], d[4];
         mass_t sum = 0;
@@ -833,8 +855,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
         for (int s = tid; s < segs; s += NT)  // (segs <= NT)
             a = Segment{__ldcg(&mine[s].p), __ldcg(&mine[s].q), __ldcg(&mine[s].left),
                         __ldcg(&mine[s].q_left), __ldcg(&mine[s].undecided)};
-        const mass_t sp = cta_sum(a.p, sh.warps[0]);
-        const mass_t sq = row.q && row.residual ? cta_sum(a.q, sh.warps[1]) : 1ull << kUnitBits;
+        mass_t sp = a.p, sq = a.q;
+        cta_sums(sp, sq, sh.warps);
+        if (!(row.q && row.residual))
+            sq = 1ull << kUnitBits;
         if (state == kOpen) {  // (rare: what follows is left to this CTA)
             if (tid == 0) {
                 // p(x) = e^{(z - M) / tau} 2^-{unit / 2048} 2^60 / SP, and q's likewise
@@ -848,7 +872,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                                        : 1.0 / (double)(1ull << kUnitBits);
                 v.state = (double)v.u * Q < P ? kAccept : kReject;
             }
-            __syncthreads();
+            __syncthreads();  // (of sh.level)
             const int was = k;
             state = advance();
             if (state == kBadRow || state == kBadDraft) {
@@ -864,17 +888,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
         }
         left = a.left;
         if (row.q && row.residual) {
-            if (tid == 0) {
-                // SP / SQ - 1 in units of 2^-64: to fp32, and then what that leaves
-                sh.minus = sp < sq;
-                const mass_t d = sp < sq ? sq - sp : sp - sq;
-                const mass_t x = __float2ull_rz((float)d / (float)sq * 0x1p64f);
-                const long long rest = (long long)(d - __umul64hi(x, sq));
-                sh.delta = x + (mass_t)__float2ll_rn((float)rest / (float)sq * 0x1p64f);
-            }
-            __syncthreads();
-            minus = sh.minus;
-            delta = sh.delta;
+            // SP / SQ - 1 in units of 2^-64: to fp32, and then what that leaves
+            minus = sp < sq;
+            const mass_t gap = minus ? sq - sp : sp - sq;
+            const float inv = 0x1p64f / (float)sq;
+            delta = __float2ull_rz((float)gap * inv);
+            delta += (mass_t)__float2ll_rn((float)(long long)(gap - __umul64hi(delta, sq)) * inv);
             const mass_t x = __umul64hi(a.q_left, delta);
             left = minus ? left + x : left - x;
             // the entries that were undecided, a thread a segment; where there were too many, all
@@ -914,13 +933,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             if (n > kListed)
                 left = sh.more[tid];
         }
-        const mass_t R = cta_sum(left, sh.warps[0]);
+        mass_t R, none;
+        const mass_t before = cta_before(left, sh.warps[0], R);
         if (R > 0) {
             // The segment, and in it a thread's part.
-            if (tid == 0)
-                sh.goal = __umul64hi(R, __float2ull_rz(g.u_last[b] * 0x1p64f));  // (below R)
-            const mass_t before = cta_before(left, sh.warps[1]);  // (its barriers)
-            const mass_t goal = sh.goal;
+            const mass_t goal = __umul64hi(R, __float2ull_rz(u_last * 0x1p64f));  // (below R)
             if (before <= goal && goal < before + left) {
                 sh.seg = tid;
                 sh.rest = goal - before;
@@ -952,7 +969,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 }
             }
             atomicMax(&sh.end, end);
-            mass_t at = cta_before(own, sh.warps[0]);
+            mass_t at = cta_before(own, sh.warps[1], none);
             const unsigned hit = __ballot_sync(0xffffffffu, at <= rest && rest < at + own);
             if (hit) {  // the thread's entries, over its warp
                 const int src = __ffs(hit) - 1, e = __shfl_sync(0xffffffffu, a1, src);
@@ -1003,11 +1020,13 @@ int stretches_of(int64_t rows, int64_t V, int in_bytes)
     return c < 1 ? 1 : (int)c;
 }
 
-// The second kernel's CTAs a request: four an SM in all, 256 entries a segment at least, and no
-// more segments than a CTA has threads.
-int groups_of(int64_t B, int64_t V)
+// The second kernel's CTAs a request: four an SM in all, eight where entries are of two rows (the
+// first requests' tokens are drawn while others are added up: B=64, 4 drafts, V=151936: 80 us for 81;
+// B=128, V=32003 fp32: 70 for 73; without the draft's rows, B=96: 57 for 53), 256 entries a segment
+// at least, and no more segments than a CTA has threads.
+int groups_of(int64_t B, int64_t V, bool two)
 {
-    int64_t c = 608 / B;
+    int64_t c = (two ? 1216 : 608) / B;
     c = c < V / (256 * kWarps) ? c : V / (256 * kWarps);
     c = c < kVerifyThreads / kWarps ? c : kVerifyThreads / kWarps;
     return c < 1 ? 1 : (int)c;
@@ -1030,7 +1049,9 @@ VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D)
     VerifyLayout l;
     // (rows times their stretches: no more than the warps, or the rows)
     l.segs = ws_round_up((size_t)(B * (D + 1) + kRowWarps) * sizeof(Part));
-    const size_t n = (size_t)B * segments_of(V, groups_of(B, V));
+    const int one = segments_of(V, groups_of(B, V, false));
+    const int two = segments_of(V, groups_of(B, V, true));  // (may be fewer)
+    const size_t n = (size_t)B * (one > two ? one : two);
     l.undecided = l.segs + ws_round_up(n * sizeof(Segment));
     l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(int32_t));
     l.total = l.tickets + ws_round_up((size_t)B * sizeof(uint32_t));
@@ -1133,7 +1154,7 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     g.lps = lp_sampled_out;
     g.status = dev_status;
     g.stretches = stretches_of(N * (draft_logits ? 2 : 1) + B, V, dtype == CIS_BF16 ? 2 : 4);
-    g.groups = groups_of(B, V);
+    g.groups = groups_of(B, V, draft_logits != nullptr);
     g.segments = segments_of(V, g.groups);
     const VerifyLayout l = verify_layout(B, V, max_drafts);
     uint8_t *ws = static_cast<uint8_t *>(workspace);

@@ -358,6 +358,25 @@ def test_guard_bands_and_no_requests():
     assert none[0].shape == (0, D + 1) and none[1].shape == (0,)
 
 
+@pytest.mark.parametrize("B,D,V", [(1, 0, 3), (1, 4, 40001), (7, 64, 300), (64, 4, 20000),
+                                   (130, 3, 2500), (700, 2, 300), (33, 1, 151936)])
+@pytest.mark.parametrize("two", [True, False])
+def test_workspace_is_as_long_as_it_says(B, D, V, two):
+    z, zd, ids, cu, u, ul = _case(B, D, V, BF, B + V, ragged=False)
+    need = binding.cis_verify_workspace_size(B, V, D)
+    ws = torch.full((need + 65536,), 0x5A, dtype=torch.uint8, device=DEV)
+    L, p = binding.lib(), binding._ptr
+    tok = torch.empty(B, D + 1, dtype=torch.int32, device=DEV)
+    kept = torch.empty(B, dtype=torch.int32, device=DEV)
+    for n in (ids.numel(), 0):  # as many drafts as there may be, and none
+        c = cu if n else torch.zeros_like(cu)
+        assert L.cis_verify_tokens(p(z), 1, B, n, V, V, p(ids), p(c), D, p(zd) if two else None, V,
+                                   p(u), p(ul), None, None, None, p(tok), p(kept), None, None,
+                                   None, p(ws), need, binding._stream()) == 0
+        torch.cuda.synchronize()
+        assert (ws[need:] == 0x5A).all() and (kept >= 0).all()
+
+
 def test_two_graphs_with_a_workspace_each():
     """Captured on streams of their own and replayed at once, on new inputs."""
     B, D, V = 6, 4, 32000
