@@ -441,7 +441,8 @@ CIS_API cis_status_t cis_rmsnorm_bwd_workspace_size(int64_t T, int64_t H, size_t
  *   weight, eps, mask: as in the forward call; masked rows are not read, get dx 0 and have no
  *              part in dweight.
  *   dx         device, [T, H] of `dtype`;  dweight device float [H], both written.
- *   workspace  device, >= cis_rmsnorm_bwd_workspace_size(T, H) bytes, 256-byte aligned.
+ *   workspace  device, >= cis_rmsnorm_bwd_workspace_size(T, H) bytes, 256-byte aligned.  Calls whose
+ *              GPU work overlaps (streams, graphs) need one each.
  * Deterministic.  T == 0: dweight 0.  The outputs may not overlap each other or the inputs.
  * Errors: as cis_rmsnorm_fwd, and CIS_ERR_INVALID_ARG for a workspace that is too small or
  * misaligned.
@@ -593,7 +594,7 @@ CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, int32_t max
  * p_i = softmax(z_i / temperature) and q_i the distribution that draft x_i was drawn from, in order:
  *   x_i is kept where u_i q_i(x_i) < p_i(x_i);
  *   at the first i that is not, the last token is drawn from max(p_i - q_i, 0) (from p_i where
- *   that is 0 throughout);
+ *   that adds up to less than 2^-32);
  *   if all are kept, it is drawn from p_{n_b}.
  * It is the first entry, by index, whose running mass is above u_last times the mass.  At
  * temperature 0 p is 1 on the row's first largest entry.
@@ -620,11 +621,12 @@ CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, int32_t max
  *                   (0 at temperature 0).
  *   dev_status      device int32 [1] or NULL: device status bits are OR-ed in.
  *   workspace       device, >= cis_verify_workspace_size(B, V, max_drafts) bytes, 256-byte aligned.
+ *                   Calls whose GPU work overlaps (streams, graphs) need one each.
  * Rows are looked at in order up to the last token's.  Where one that is reached has NaN, +inf or
  * no finite logit, where a number that is reached or a request's setting or range of cu_drafts is
  * out of its range (CIS_ERR_BAD_INPUT), or a draft that is reached is not in [0, V)
  * (CIS_ERR_BAD_TOKEN_ID), the request's tokens and kept are -1 and its log-probabilities NaN.
- * Logits at -inf have probability 0, in either row.  The decisions are taken on masses that are
+ * Logits at -inf, and probabilities that fp64 cannot hold, are 0, in either row.  The decisions are taken on masses that are
  * right to 2^-35 of each and 2^-59 of the row's.  Deterministic.  The outputs may not overlap each
  * other or the inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, B < 0 or above
  * 2^20, N < 0 or above B max_drafts, V <= 0, a stride below V, max_drafts out of range, an unknown

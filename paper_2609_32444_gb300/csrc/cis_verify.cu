@@ -3,7 +3,8 @@
 //
 // Per request, with p_i = softmax(z_i / tau) of the target's rows, q_i the distribution that draft
 // x_i came from, in order:  x_i is kept where u_i q_i(x_i) < p_i(x_i).  After the first one that
-// is not, at i, the request's last token is drawn from max(p_i - q_i, 0); after the last draft,
+// is not, at i, the request's last token is drawn from max(p_i - q_i, 0) (from p_i where that adds
+// up to less than 2^-32: a draft from q_i is rejected that seldom); after the last draft,
 // from the target's next row.  At temperature 0 p is all on the row's first largest entry.
 //
 // Two kernels.  The first reads every row once, a row's stretches on CTAs of their own: maximum
@@ -392,6 +393,9 @@ __device__ inline void fill_table(mass_t *table, const mass_t *parts)
     for (int i = threadIdx.x; i < kSteps; i += kVerifyThreads)
         table[i] = __umul64hi(parts[64 + (i >> 6)], parts[i & 63]) << 2;
 }
+
+// What is left of p counts from 2^-32 on: below, it would be made of the masses' errors.
+constexpr mass_t kLeastLeft = 1ull << (kUnitBits - 32);
 
 // A segment's sums: of both rows' masses, of what is left of the first (P - Q, or P), and of Q
 // where something is left; and the number of entries that are not in the last two, as their sign
@@ -865,11 +869,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 Level &v = sh.level[k];
                 auto share = [](float z, float M, float tau, float unit, mass_t sum) {
                     return exp(((double)z - (double)M) / (double)tau -
-                               (double)unit * (0.693147180559945309417 / kSteps)) / (double)sum;
+                               (double)unit * (0.693147180559945309417 / kSteps)) *
+                           ((double)(1ull << kUnitBits) / (double)sum);
                 };
                 const double P = share(v.zx, v.m, r.tau, v.p.unit, sp);
-                const double Q = row.q ? share(v.dx, v.md, r.tau_d, v.q.unit, sq)
-                                       : 1.0 / (double)(1ull << kUnitBits);
+                const double Q = row.q ? share(v.dx, v.md, r.tau_d, v.q.unit, sq) : 1.0;
                 v.state = (double)v.u * Q < P ? kAccept : kReject;
             }
             __syncthreads();  // (of sh.level)
@@ -935,7 +939,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
         }
         mass_t R, none;
         const mass_t before = cta_before(left, sh.warps[0], R);
-        if (R > 0) {
+        if (R > (row.residual ? kLeastLeft : 0)) {
             // The segment, and in it a thread's part.
             const mass_t goal = __umul64hi(R, __float2ull_rz(u_last * 0x1p64f));  // (below R)
             if (before <= goal && goal < before + left) {
@@ -1000,7 +1004,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 return;
             }
         }
-        // p is q as far as can be told: the whole of p
+        // p is q: the whole of p
         row.residual = false;
         __syncthreads();
         sums(0, segs);

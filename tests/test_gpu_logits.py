@@ -80,6 +80,19 @@ def test_rows_of_a_wider_buffer(T, V, ld, off, dtype):
     assert (out[:, V:] == 7).all() and (flat[:off] == 7).all() and (flat[off + T * ld:] == 7).all()
 
 
+@pytest.mark.parametrize("T", [3, 70])
+def test_rows_far_apart(T):
+    """A row stride whose offsets pass 2^31 elements."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    x, xs = _rows(T, 128, g)
+    w, ws = _rows(300, 128, g)
+    ld = 2_500_000_001 // (T - 1) + 1
+    out = torch.empty(T * ld, dtype=BF, device=DEV).view(T, ld)
+    binding.cis_lmhead_logits(x, xs, w, ws, logits=out)
+    assert torch.equal(out[:, :300], binding.cis_lmhead_logits(x, xs, w, ws))
+
+
 def test_special_values():
     """A NaN spoils its row or column alone; zero scales give zeros; 448s add up exactly."""
     T, H, V = 20, 512, 300

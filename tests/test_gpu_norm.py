@@ -165,6 +165,20 @@ def test_strided_rows(dtype, pad):
     _check_bwd(binding.cis_rmsnorm_bwd(dy, x, w, dh=r), dy, x, w, r, None, 1e-6, dtype)
 
 
+def test_rows_far_apart():
+    """A row stride whose offsets pass 2^31 elements."""
+    T, H, ld = 3, 700, 1_300_000_001
+    g = _gen(4)
+    x = torch.empty(T * ld, dtype=BF, device=DEV).view(T, ld)[:, :H]
+    x.copy_(_rand(T, H, g, BF))
+    w = torch.randn(H, generator=g, device=DEV)
+    got, near = binding.cis_rmsnorm_fwd(x, w, residual=x), x.contiguous()
+    assert torch.equal(got["y"], binding.cis_rmsnorm_fwd(near, w, residual=near)["y"])
+    got = binding.cis_rmsnorm_bwd(x, x, w, dh=x)
+    want = binding.cis_rmsnorm_bwd(near, near, w, dh=near)
+    assert torch.equal(got["dx"], want["dx"]) and torch.equal(got["dweight"], want["dweight"])
+
+
 def test_unaligned_base():
     """A row tensor that starts off 16 bytes, and weights too."""
     T, H = 5, 512

@@ -1,8 +1,10 @@
 """cis_verify_tokens against its definition in 64 bits.
 
 Tokens and counts are equal: the reference says how near its decisions were to their borders,
-and the test asserts that none of its inputs is within 2^-36 of the row's mass (the kernel's masses
-are right to 2^-42 of each, and their units to 2^-60).  log-probabilities: the row's mass is summed to
+and the test asserts that none of its inputs is within 2^-33.  The kernel's masses are right to
+2^-35 of each: u q against p is off by twice that, relative to the larger (the sums of both rows
+and, in fp64, the two entries), and a running sum of p - q and its goal by twice that each, relative
+to the rows' masses of 1.  log-probabilities: the row's mass is summed to
 6 x 2^-20 (fp32 exponentials, each right to 2^-22, as the sampler's), and the difference from it is
 rounded to fp32 once or twice: 8 x 2^-20 + 2^-22 |lp|.
 """
@@ -61,12 +63,14 @@ def _reference(z, ids, cu, u, u_last, D, zd=None, tau=None, tau_d=None, mask=Non
                 else:
                     q = torch.softmax(zd[cu[b] + i].double() / td, 0)
                 if t > 0:
-                    near = min(near, abs(r * float(q[d]) - float(p[d])) or 1.0)
+                    a, c = r * float(q[d]), float(p[d])
+                    near = min(near, abs(a - c) / max(a, c) if max(a, c) > 0 else 1.0)
                 if (float(p[d]) > 0 if t == 0 else r * float(q[d]) < float(p[d])):
                     token = d
             if token is None:
                 m = p if q is None else (p - q).clamp(min=0)
-                m = m if float(m.sum()) > 0 else p
+                near = min(near, abs(float(m.sum()) * 2.0 ** 32 - 1))
+                m = m if float(m.sum()) * 2.0 ** 32 > 1 else p
                 c = m.cumsum(0)
                 goal = float(u_last[b].double()) * float(c[-1])
                 token = int((c <= goal).sum())
@@ -96,7 +100,7 @@ def _check(z, ids, cu, u, ul, D, zd=None, tau=None, tau_d=None, mask=None, V=Non
     cut = (lambda x: x) if V is None else (lambda x: None if x is None else x[:, :V])
     want = _reference(cut(z), ids.cpu(), cu.tolist(), u.cpu(), ul.cpu(), D, cut(zd), tau, tau_d,
                       mask)
-    assert want[4] > 2.0 ** -36
+    assert want[4] > 2.0 ** -33
     assert int(st) == 0
     assert got[0].cpu().tolist() == want[0].tolist() and got[1].cpu().tolist() == want[1].tolist()
     _close(got[2], want[2])
@@ -356,6 +360,34 @@ def test_guard_bands_and_no_requests():
         assert torch.equal(v[a], b.flatten())
     none = binding.cis_verify_tokens(z[:0], ids[:0], cu[:1], u[:0], ul[:0], D)
     assert none[0].shape == (0, D + 1) and none[1].shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [1e-3, 1.0, 300.0, 1e4, 1e7, 1e30])
+def test_extreme_logits_and_temperatures(size, dtype):
+    """Rows around +-size, temperatures at both ends of their range."""
+    B, D, V = 12, 2, 777
+    z, zd, ids, cu, u, ul = _case(B, D, V, dtype, 3)
+    z, zd = (z.float() * size).to(dtype), (zd.float() * size).to(dtype)
+    z[::2] -= 20 * size
+    for t in (1e-3, 1.0, 1e3):
+        tau = torch.full((B,), t, device=DEV)
+        _check(z, ids, cu, u, ul, D, zd=zd, tau=tau, tau_d=tau)
+        _check(z, ids, cu, u, ul, D, tau=tau)
+
+
+def test_rows_far_apart():
+    """Row strides whose offsets pass 2^31 elements."""
+    z, zd, ids, cu, u, ul = _case(2, 1, 4001, BF, 4, ragged=False)
+    ld = 1_300_000_001
+    far = torch.empty(5 * ld, dtype=BF, device=DEV)
+    z2, zd2 = far[:4 * ld].view(4, ld)[:, :4001], far[2 * ld + 7000:4 * ld + 7000]
+    zd2 = zd2.view(2, ld)[:, :4001]
+    z2.copy_(z)
+    zd2.copy_(zd)
+    got = binding.cis_verify_tokens(z2, ids, cu, u, ul, 1, draft_logits=zd2)
+    want = binding.cis_verify_tokens(z, ids, cu, u, ul, 1, draft_logits=zd)
+    assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
 
 
 @pytest.mark.parametrize("B,D,V", [(1, 0, 3), (1, 4, 40001), (7, 64, 300), (64, 4, 20000),
