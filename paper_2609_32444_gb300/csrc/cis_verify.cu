@@ -141,11 +141,15 @@ __device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, flo
     return fminf(u + (e + l - log_residual(mass, ls)), 0.0f);
 }
 
+// CTAs an SM: fp32 rows have more instructions a byte (B=128, up to 8 drafts, V=32003: 66 us a call
+// for 71 with three; bf16 rows, B=64, 4 drafts, V=151936: 82 for 80).
+template <typename InT> constexpr int kRowCtas = sizeof(InT) == 4 ? 4 : 3;
+
 // A stretch of one row, of the target's or (the items behind theirs) a draft's, by a warp of its
 // own: no barrier holds a warp whose loads have come.  Four vectors a lane at a time, with the next
 // four on their way.
 template <typename InT>
-__global__ void __launch_bounds__(kVerifyThreads, 3)
+__global__ void __launch_bounds__(kVerifyThreads, kRowCtas<InT>)
     cis_verify_rows_kernel(const __grid_constant__ VerifyArgs g)
 {
     constexpr int EV = Vec<InT>::kN, kB = 4;
@@ -1012,13 +1016,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     }
 }
 
-// A row's stretches: as many warps in all as the SMs hold at a time (24 each), 256 vectors each at
-// least.
-constexpr int64_t kRowWarps = 24 * 152;
-int stretches_of(int64_t rows, int64_t V, int in_bytes)
+// A row's stretches: as many warps in all as the SMs hold at a time, 256 vectors each at least.
+constexpr int64_t kSms = 152, kMostRowWarps = kRowCtas<float> * kWarps * kSms;
+template <typename InT> int stretches_of(int64_t rows, int64_t V)
 {
-    const int64_t nvec = V * in_bytes / 16;
-    int64_t c = kRowWarps / rows;
+    const int64_t nvec = V * (int64_t)sizeof(InT) / 16;
+    int64_t c = kRowCtas<InT> * kWarps * kSms / rows;
     c = c < nvec / 256 ? c : nvec / 256;
     c = c < kMaxStretches ? c : kMaxStretches;
     return c < 1 ? 1 : (int)c;
@@ -1052,7 +1055,7 @@ VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D)
 {
     VerifyLayout l;
     // (rows times their stretches: no more than the warps, or the rows)
-    l.segs = ws_round_up((size_t)(B * (D + 1) + kRowWarps) * sizeof(Part));
+    l.segs = ws_round_up((size_t)(B * (D + 1) + kMostRowWarps) * sizeof(Part));
     const int one = segments_of(V, groups_of(B, V, false));
     const int two = segments_of(V, groups_of(B, V, true));  // (may be fewer)
     const size_t n = (size_t)B * (one > two ? one : two);
@@ -1157,7 +1160,9 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     g.lp = lp_out;
     g.lps = lp_sampled_out;
     g.status = dev_status;
-    g.stretches = stretches_of(N * (draft_logits ? 2 : 1) + B, V, dtype == CIS_BF16 ? 2 : 4);
+    const int64_t rows = N * (draft_logits ? 2 : 1) + B;
+    g.stretches = dtype == CIS_BF16 ? stretches_of<__nv_bfloat16>(rows, V)
+                                    : stretches_of<float>(rows, V);
     g.groups = groups_of(B, V, draft_logits != nullptr);
     g.segments = segments_of(V, g.groups);
     const VerifyLayout l = verify_layout(B, V, max_drafts);
