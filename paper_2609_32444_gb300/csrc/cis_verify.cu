@@ -52,7 +52,7 @@ struct VerifyArgs {
     Part *parts;  // [N + B][stretches]
     int stretches;
     struct Segment *segs;  // [B][segments]
-    int32_t *undecided;    // [B][segments][kListed]
+    ulonglong2 *undecided;  // [B][segments][kListed]
     uint32_t *tickets;     // [B]: the second kernel's CTAs that have finished
     int groups, segments;  // of a request
 };
@@ -131,14 +131,22 @@ template <bool kScaled> __device__ __forceinline__ MaxSumU warp_exp(const ExpAcc
         all.lost = 0.0f;
     return all.result();
 }
+// The log of a row's mass, and what it is short of it.
+struct LogMass {
+    float log, rest;
+};
+__device__ __forceinline__ LogMass log_mass(float mass)
+{
+    const float ls = logf(mass);
+    return {ls, log_residual(mass, ls)};
+}
 // The log-probability of z: (z - M) / tau - log of the row's mass; at most 0, whatever the mass's
 // roundings.
-__device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, float mass)
+__device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, const LogMass &m)
 {
     float l, e;
-    const float x = scaled_diff(z, M, sc, l), ls = logf(mass);
-    const float u = two_sum(x, -ls, e);
-    return fminf(u + (e + l - log_residual(mass, ls)), 0.0f);
+    const float x = scaled_diff(z, M, sc, l), u = two_sum(x, -m.log, e);
+    return fminf(u + (e + l - m.rest), 0.0f);
 }
 
 // CTAs an SM: fp32 rows have more instructions a byte (B=128, up to 8 drafts, V=32003: 66 us a call
@@ -403,8 +411,8 @@ constexpr mass_t kLeastLeft = 1ull << (kUnitBits - 32);
 
 // A segment's sums: of both rows' masses, of what is left of the first (P - Q, or P), and of Q
 // where something is left; and the number of entries that are not in the last two, as their sign
-// is not settled.  kListed of them are listed; with more, all are looked at again.
-constexpr int kListed = 32;
+// is not settled.  The masses of kListed of them are listed; with more, all are looked at again.
+constexpr int kListed = 16;
 struct Segment {
     mass_t p, q, left, q_left;
     mass_t undecided;
@@ -412,8 +420,9 @@ struct Segment {
 
 // A row of the request, its draft and what they come to.
 struct Level {
-    float m, s, s1, md, sd;
-    float u, zx, dx;  // the draft's number and logits
+    float m, s, md, sd;
+    LogMass log, log1;  // of the target's mass at tau and at 1
+    float u, zx, dx;    // the draft's number and logits
     int arg, id, state;
     RowShare p, q;
 };
@@ -464,7 +473,7 @@ template <typename InT> struct DrawRow {
 template <typename InT, bool kPair>
 __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const RowShare &mp,
                                                const RowShare &mq, const mass_t *table, int s,
-                                               int *count, int32_t *list)
+                                               int *count, ulonglong2 *list)
 {
     constexpr int EV = Vec<InT>::kN;
     const int lane = threadIdx.x & 31, j0 = row.start(s), j1 = row.start(s + 1);
@@ -499,10 +508,12 @@ __device__ __forceinline__ Segment add_segment(const DrawRow<InT> &row, const Ro
     auto check = [&](int j) {  // lists entry j where its sign is not settled
         float2 t;
         const float2 f = two.split(make_float2(to_f32(row.p[j]), to_f32(row.q[j])), t);
-        if (fabsf((t.x - t.y) + (f.x - f.y)) <= 0.05f && mp(table, to_f32(row.p[j])) != 0) {
-            const int at = atomicAdd(count, 1);
+        if (fabsf((t.x - t.y) + (f.x - f.y)) <= 0.05f) {
+            mass_t P, Q;
+            TwoShares::masses(table, t, f, P, Q);
+            const int at = P != 0 ? atomicAdd(count, 1) : kListed;
             if (at < kListed)
-                list[at] = j;
+                list[at] = make_ulonglong2(P, Q);
         }
     };
     int from = j0, to = j0;  // the vectors' entries
@@ -722,11 +733,26 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             sq += __shfl_xor_sync(0xffffffffu, sq, o);
             arg = min(arg, __shfl_xor_sync(0xffffffffu, arg, o));
         }
+        // what follows of the sums, of the target's in lane 0 and of the draft's in lane 1
+        Level &v = sh.level[i];
+        const bool second = lane & 1;
+        const float mass = second ? sq : s, top = second ? Md : M;
+        RowShare share;
+        share.set(top, second ? r.tau_d : r.greedy ? 1.0f : r.tau, second ? sd : sc, mass,
+                  second ? RowShare::kDepth + 0.2f : RowShare::kDepth);
+        // (2^-21 more than the sums)
+        const float own = share_of(second ? v.dx : v.zx, top, second ? sd : sc) / mass;
+        const float other = __shfl_sync(0xffffffffu, own, 1);
+        const LogMass log = log_mass(second ? s1 : s);  // (lane 1: at temperature 1)
+        if (lane == 1) {
+            v.q = share;
+            v.log1 = log;
+        }
         if (lane == 0) {
-            Level &v = sh.level[i];
+            v.p = share;
+            v.log = log;
             v.m = M;
             v.s = s;
-            v.s1 = s1;
             v.md = Md;
             v.sd = sq;
             v.arg = arg;
@@ -737,23 +763,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 v.state = kBadRow;
             } else if (i < r.n && (v.id < 0 || v.id >= g.V)) {
                 v.state = kBadDraft;
-            } else if (r.greedy) {
-                if (i < r.n)
-                    v.state = v.id == arg ? kAccept : kReject;
-            } else {
-                v.p.set(M, r.tau, sc, s, RowShare::kDepth);
-                if (draft)
-                    v.q.set(Md, r.tau_d, sd, sq, RowShare::kDepth + 0.2f);
-                if (i < r.n) {
-                    // (2^-21 more than the sums; where fp32 has no such number the draft is left
-                    // open too)
-                    const float px = share_of(v.zx, M, sc) / s;
-                    const float uq = draft ? v.u * (share_of(v.dx, Md, sd) / sq) : v.u;
-                    const float most = fmaxf(px, uq);
-                    v.state = fabsf(px - uq) > 0x1p-16f * most && most > 1e-30f
-                                  ? (uq < px ? kAccept : kReject)
-                                  : kOpen;
-                }
+            } else if (i < r.n && r.greedy) {
+                v.state = v.id == arg ? kAccept : kReject;
+            } else if (i < r.n) {
+                // (where fp32 has no such number the draft is left open too)
+                const float px = own, uq = draft ? v.u * other : v.u, most = fmaxf(px, uq);
+                v.state = fabsf(px - uq) > 0x1p-16f * most && most > 1e-30f
+                              ? (uq < px ? kAccept : kReject)
+                              : kOpen;
             }
         }
     }
@@ -771,12 +788,17 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             refuse(state == kBadRow ? kStatusBadInput : kStatusBadId);
             return;
         }
-        for (int i = tid; i <= k; i += NT) {
+        static_assert(2 * CIS_MAX_DRAFTS < NT, "a thread a log-probability");
+        const int i = tid & (NT / 2 - 1);
+        if (i <= k) {
             const Level &v = sh.level[i];
             const float x = i < k ? v.zx : z;
-            g.tokens[out + i] = i < k ? v.id : token;
-            if (g.lp) g.lp[out + i] = log_prob(x, v.m, one, v.s1);
-            if (g.lps) g.lps[out + i] = r.greedy ? 0.0f : log_prob(x, v.m, sc, v.s);
+            if (tid == i) {
+                g.tokens[out + i] = i < k ? v.id : token;
+                if (g.lp) g.lp[out + i] = log_prob(x, v.m, one, v.log1);
+            } else if (g.lps) {
+                g.lps[out + i] = r.greedy ? 0.0f : log_prob(x, v.m, sc, v.log);
+            }
         }
         fill(k + 1, -1, 0.0f);
         if (tid == 0)
@@ -791,7 +813,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     // The row's masses, a warp a segment.
     const int segs = g.segments, own_segs = segs / g.groups;
     Segment *mine = g.segs + (int64_t)b * segs;
-    int32_t *undecided = g.undecided + (int64_t)b * segs * kListed;
+    ulonglong2 *undecided = g.undecided + (int64_t)b * segs * kListed;
     DrawRow<InT> row;
     auto enter = [&] {
         const Level &v = sh.level[k];
@@ -800,7 +822,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     auto sums = [&](int from, int to) {
         const RowShare mp = sh.level[k].p, mq = sh.level[k].q;
         for (int s = from + w; s < to; s += kWarps) {
-            int32_t *list = undecided + (int64_t)s * kListed;
+            ulonglong2 *list = undecided + (int64_t)s * kListed;
             int *count = &sh.undecided[w];
             const Segment a =
                 row.q && row.residual
@@ -831,14 +853,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
         const mass_t x = __umul64hi(Q, delta);
         return minus ? Q - x : Q + x;
     };
+    RowShare sp_of, sq_of;  // level k's
     auto mass_of = [&](int j, float z, float d) -> mass_t {
-        const Level &v = sh.level[k];
-        const mass_t P = v.p(sh.table, z);
+        const mass_t P = sp_of(sh.table, z);
         if (!row.residual)
             return P;
         if (!row.q)
             return j == row.id ? 0 : P;
-        const mass_t Q = off(v.q(sh.table, d));
+        const mass_t Q = off(sq_of(sh.table, d));
         return P > Q ? P - Q : 0;
     };
     auto mass = [&](int j) {
@@ -860,9 +882,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     };
     for (;;) {
         Segment a = {};
-        for (int s = tid; s < segs; s += NT)  // (segs <= NT)
-            a = Segment{__ldcg(&mine[s].p), __ldcg(&mine[s].q), __ldcg(&mine[s].left),
-                        __ldcg(&mine[s].q_left), __ldcg(&mine[s].undecided)};
+        ulonglong2 listed = make_ulonglong2(0, 0);  // the first of its list, if there is one
+        if (tid < segs) {
+            a = Segment{__ldcg(&mine[tid].p), __ldcg(&mine[tid].q), __ldcg(&mine[tid].left),
+                        __ldcg(&mine[tid].q_left), __ldcg(&mine[tid].undecided)};
+            listed = __ldcg(undecided + (int64_t)tid * kListed);
+        }
         mass_t sp = a.p, sq = a.q;
         cta_sums(sp, sq, sh.warps);
         if (!(row.q && row.residual))
@@ -894,6 +919,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 continue;
             }
         }
+        sp_of = sh.level[k].p;
+        sq_of = sh.level[k].q;
         left = a.left;
         if (row.q && row.residual) {
             // SP / SQ - 1 in units of 2^-64: to fp32, and then what that leaves
@@ -908,14 +935,20 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             // of them, a warp a segment
             const int n = (int)a.undecided;
             const unsigned many = __ballot_sync(0xffffffffu, n > kListed);
-            if (n <= kListed)
-                for (int i = 0; i < n; i += 4) {
-                    const int4 q = __ldcg(reinterpret_cast<const int4 *>(
-                        undecided + (int64_t)tid * kListed + i));
-                    const int j[4] = {q.x, i + 1 < n ? q.y : -1, i + 2 < n ? q.z : -1,
-                                      i + 3 < n ? q.w : -1};
-                    left += four(j);
+            auto settled = [&](const ulonglong2 &e) {
+                const mass_t Q = off(e.y);
+                return e.x > Q ? e.x - Q : 0;
+            };
+            if (n <= kListed) {
+                left += n > 0 ? settled(listed) : 0;
+                for (int i = 1; i < n; i += 3) {  // (kListed is 1 more than a multiple of 3)
+                    const ulonglong2 *at = undecided + (int64_t)tid * kListed + i;
+                    const ulonglong2 e0 = __ldcg(at), e1 = __ldcg(at + 1), e2 = __ldcg(at + 2);
+                    left += settled(e0);
+                    left += i + 1 < n ? settled(e1) : 0;
+                    left += i + 2 < n ? settled(e2) : 0;
                 }
+            }
             if (lane == 0)
                 sh.many[w] = many;
             __syncthreads();
@@ -959,9 +992,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             const int a0 = min(s1, s0 + tid * per), a1 = min(s1, a0 + per);
             mass_t own = 0;
             int end = -1;  // the last entry with a mass
+            mass_t m[4];  // of the last four
             for (int j = a0; j < a1; j += 4) {
                 float z[4], d[4];
-                mass_t m[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     z[i] = j + i < a1 ? to_f32(row.p[j + i]) : -INFINITY;
@@ -978,7 +1011,17 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             }
             atomicMax(&sh.end, end);
             mass_t at = cta_before(own, sh.warps[1], none);
-            const unsigned hit = __ballot_sync(0xffffffffu, at <= rest && rest < at + own);
+            const bool mine_it = at <= rest && rest < at + own;
+            if (mine_it && per <= 4) {
+                int i = 0;
+#pragma unroll
+                for (int e = 0; e < 3; ++e) {
+                    at += m[e];
+                    i += at <= rest;
+                }
+                sh.found = a0 + i;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, mine_it && per > 4);
             if (hit) {  // the thread's entries, over its warp
                 const int src = __ffs(hit) - 1, e = __shfl_sync(0xffffffffu, a1, src);
                 int j = __shfl_sync(0xffffffffu, a0, src);
@@ -1060,7 +1103,7 @@ VerifyLayout verify_layout(int64_t B, int64_t V, int32_t D)
     const int two = segments_of(V, groups_of(B, V, true));  // (may be fewer)
     const size_t n = (size_t)B * (one > two ? one : two);
     l.undecided = l.segs + ws_round_up(n * sizeof(Segment));
-    l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(int32_t));
+    l.tickets = l.undecided + ws_round_up(n * kListed * sizeof(ulonglong2));
     l.total = l.tickets + ws_round_up((size_t)B * sizeof(uint32_t));
     return l;
 }
@@ -1169,7 +1212,7 @@ extern "C" CIS_API cis_status_t cis_verify_tokens(
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     g.parts = reinterpret_cast<Part *>(ws);
     g.segs = reinterpret_cast<Segment *>(ws + l.segs);
-    g.undecided = reinterpret_cast<int32_t *>(ws + l.undecided);
+    g.undecided = reinterpret_cast<ulonglong2 *>(ws + l.undecided);
     g.tickets = reinterpret_cast<uint32_t *>(ws + l.tickets);
     const cudaError_t e = dtype == CIS_BF16 ? launch_verify<__nv_bfloat16>(g, (cudaStream_t)stream)
                                             : launch_verify<float>(g, (cudaStream_t)stream);
