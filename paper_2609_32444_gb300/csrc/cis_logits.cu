@@ -18,6 +18,10 @@
 // other.  (Two of 160 took 70 us where no logits were stored, T=320, H=2048, V=151936: as long as
 // 192 would.)
 //
+// Bound: HBM up to 256 tokens (H=2048, V=151936: T=1 51 us a call, 6.1 TB/s; T=256 66 us, 5.9), then
+// the tensor cores (T=320 75 to 85 us; T=2048, V=32000, bf16 logits 76 us, 3.5 PFLOP/s, and 69 with
+// nothing stored), and for fp32 logits the L2 that loads and stores share (T=2048, V=32003: 94 to 112).
+//
 // All waits are bounded: one that runs out sets CIS_ERR_DEVICE_TIMEOUT, and the CTA drains its own
 // loads and MMAs and runs to its end.
 #include <cuda.h>

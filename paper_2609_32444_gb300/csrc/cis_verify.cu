@@ -21,6 +21,10 @@
 // follows once delta is known; entries whose sign delta could turn are put in a list instead (a
 // few of a row; some hundreds where bf16 logits and drafts differ by the same step in many).
 // Sums of whole numbers depend on no order.
+//
+// Bound: the first kernel by HBM (B=64, 4 drafts, V=151936 bf16: 32 us, 5.4 TB/s), the second by
+// instruction issue (58 an entry of two rows, 43 to 50 us of the call's 79), or, with few requests, by
+// its dependent steps: stretches, drafts, sums, ticket, prefix, entry (B=1: 5 and 15 us, 21 a call).
 #include <math.h>
 
 #include "cis_nvtx.h"

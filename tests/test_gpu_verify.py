@@ -376,6 +376,19 @@ def test_extreme_logits_and_temperatures(size, dtype):
         _check(z, ids, cu, u, ul, D, tau=tau)
 
 
+def test_outputs_that_are_not_asked_for():
+    z, zd, ids, cu, u, ul = _case(5, 3, 4001, BF, 9)
+    tau = torch.full((5,), 0.6, device=DEV)
+    full = binding.cis_verify_tokens(z, ids, cu, u, ul, 3, draft_logits=zd, temperature=tau,
+                                     want_lp_sampled=True)
+    for lp in (False, True):
+        for lps in (False, True):
+            got = binding.cis_verify_tokens(z, ids, cu, u, ul, 3, draft_logits=zd, temperature=tau,
+                                            want_lp=lp, want_lp_sampled=lps)
+            assert (got[2] is not None) == lp and (got[3] is not None) == lps
+            assert all(a is None or torch.equal(a, b) for a, b in zip(got, full))
+
+
 def test_rows_far_apart():
     """Row strides whose offsets pass 2^31 elements."""
     z, zd, ids, cu, u, ul = _case(2, 1, 4001, BF, 4, ragged=False)
