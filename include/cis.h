@@ -626,9 +626,10 @@ CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, int32_t max
  * no finite logit, where a number that is reached or a request's setting or range of cu_drafts is
  * out of its range (CIS_ERR_BAD_INPUT), or a draft that is reached is not in [0, V)
  * (CIS_ERR_BAD_TOKEN_ID), the request's tokens and kept are -1 and its log-probabilities NaN.
- * Logits at -inf, and probabilities that fp64 cannot hold, are 0, in either row.  The decisions are taken on masses that are
- * right to 2^-35 of each and 2^-59 of the row's.  Deterministic.  The outputs may not overlap each
- * other or the inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, B < 0 or above
+ * (Where cu_drafts decreases, requests whose ranges overlap may get any tokens.)  Logits at -inf, and
+ * probabilities that fp64 cannot hold, are 0, in either row.  The decisions are taken on masses that
+ * are right to 2^-35 of each and 2^-59 of the row's.  Deterministic.  The outputs may not overlap
+ * each other or the inputs.  Errors: CIS_ERR_INVALID_ARG for NULL required pointers, B < 0 or above
  * 2^20, N < 0 or above B max_drafts, V <= 0, a stride below V, max_drafts out of range, an unknown
  * dtype, a pointer that is not aligned to its type, or a workspace that is too small or
  * misaligned; CIS_ERR_UNSUPPORTED for V above 2^20.

@@ -238,15 +238,27 @@ struct RowWalk {
     }
 };
 
+// Whether no thread has an element of its vector k, `step` elements behind the one before: the
+// same for all, so that what is not there is not issued either.  Looked at for every second vector
+// (T=3001, H=2531, rows not aligned: norm in fp32 36 to 33 us, bf16 to 8 bits 27 to 23, gradients in
+// bf16 29 to 27; for every vector its branches cost more: 35, 25, 31).
+template <int V> __device__ __forceinline__ bool past(int k, int step, int H)
+{
+    return k > 0 && k % 2 == 0 && k * step >= H;
+}
+
 // K tensors' rows on their way: a thread copies what it will use itself, V vectors of E elements of
 // each, into places of its own in shared memory, S - 1 rows ahead, and waits for nobody else.
-// Elements of 2 bytes by themselves cannot be copied so: they are loaded when they are used.
+// Elements of 2 bytes by themselves cannot be copied so: they are loaded when they are used.  (Rows
+// that start anywhere copied by 16 bytes and read by other threads, behind a barrier: 35 us for 27 at
+// T=3001, H=2531 fp32.)
 template <typename T, int E, int NT, int V, int K, int S> struct Rows {
     static constexpr bool kAsync = sizeof(Pack<T, E>) >= 4;
     static constexpr size_t kBytes = kAsync ? sizeof(Pack<T, E>) * NT * V * K * S : 0;
     const T *base[K];  // this thread's first element of row 0 (null: no such tensor)
     int64_t ld[K];
     int left, stride;  // elements from this thread's first on, and between its vectors
+    int H;
     uint32_t place;
     int stage = 0;
 
@@ -258,7 +270,9 @@ template <typename T, int E, int NT, int V, int K, int S> struct Rows {
                 if (base[i]) {
                     const T *row = base[i] + t * ld[i];
 #pragma unroll
-                    for (int k = 0; k < V; ++k)
+                    for (int k = 0; k < V; ++k) {
+                        if (past<V>(k, stride, H))
+                            break;
                         if (k * stride < left) {
                             const uint32_t to =
                                 place + (uint32_t)(((s * K + i) * V + k) * NT *
@@ -272,6 +286,7 @@ template <typename T, int E, int NT, int V, int K, int S> struct Rows {
                                              "l"(row + k * stride)
                                              : "memory");
                         }
+                    }
                 }
         }
     }
@@ -299,10 +314,13 @@ template <typename T, int E, int NT, int V, int K, int S> struct Rows {
                 for (int i = 0; i < K; ++i)
                     if (base[i])
 #pragma unroll
-                        for (int k = 0; k < V; ++k)
+                        for (int k = 0; k < V; ++k) {
+                            if (past<V>(k, stride, H))
+                                break;
                             if (k * stride < left)
                                 p[i][k].shared(place + (uint32_t)(((stage * K + i) * V + k) * NT *
                                                                   sizeof(Pack<T, E>)));
+                        }
             }
             stage = stage + 1 == S ? 0 : stage + 1;
         } else if (w.on(0)) {
@@ -310,9 +328,12 @@ template <typename T, int E, int NT, int V, int K, int S> struct Rows {
             for (int i = 0; i < K; ++i)
                 if (base[i])
 #pragma unroll
-                    for (int k = 0; k < V; ++k)
+                    for (int k = 0; k < V; ++k) {
+                        if (past<V>(k, stride, H))
+                            break;
                         if (k * stride < left)
                             p[i][k].load(base[i] + w.t * ld[i] + k * stride);
+                    }
         }
     }
 };
@@ -336,6 +357,8 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
             float z[E] = {};
             for (int k = 0; k < V; ++k) {
                 const int j = (at + k * TPR) * E;
+                if (past<V>(k, TPR * E, a.H))
+                    break;
                 if (j < a.H) {
                     if (h_out) put(h_out + j, z);
                     if (y_out) put(y_out + j, z);
@@ -352,6 +375,8 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int j = (at + k * TPR) * E;
+            if (past<V>(k, TPR * E, a.H))
+                break;
             if (j < a.H) {
                 px[k].load(x + j);
                 if (r)
@@ -362,6 +387,8 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int j = (at + k * TPR) * E;
+            if (past<V>(k, TPR * E, a.H))
+                break;
             if (j < a.H) {
                 weights_of(a, j, w[k]);
                 px[k].get(h[k]);
@@ -388,6 +415,8 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int j = (at + k * TPR) * E;
+                if (past<V>(k, TPR * E, a.H))
+                    break;
                 if (j < a.H) {
                     float y[E];
 #pragma unroll
@@ -403,6 +432,8 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int j = (at + k * TPR) * E;
+                if (past<V>(k, TPR * E, a.H))
+                    break;
                 if (j < a.H) {
                     float y[E];
 #pragma unroll
@@ -418,7 +449,9 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 }
 
 // The backward kernel's threads an SM, whose rows on their way have kRowBytes of its shared memory
-// (640 threads spill; 8 elements a thread and 768 took 49 us for 42 at T=16384, H=2048, 40% padding).
+// (640 threads spill; 8 elements a thread and 768 took 49 us for 42 at T=16384, H=2048, 40% padding;
+// rows read twice from shared memory allow 640 to 1024: 41.5 to 43, and 29 to 35 us for 27 at T=3001,
+// H=2531 fp32).
 constexpr int kBwdThreads = 512, kRowBytes = 200 * 1024;
 constexpr int kMaxSms = 256;
 // CTAs of TPR threads (128 at least) an SM.
@@ -444,7 +477,7 @@ __global__ void __launch_bounds__(kCta<TPR>, ctas_of(TPR, kBwdThreads))
     using In = Rows<T, E, kCta<TPR>, V, 3, S>;
     In in{{static_cast<const T *>(a.dy) + at, static_cast<const T *>(a.x) + at,
            a.residual ? static_cast<const T *>(a.residual) + at : nullptr},
-          {a.ld_dy, a.ld_x, a.ld_r}, a.H - at, kStep,
+          {a.ld_dy, a.ld_x, a.ld_r}, a.H - at, kStep, a.H,
           (uint32_t)__cvta_generic_to_shared(dyn_smem) +
               (uint32_t)(threadIdx.x * sizeof(Pack<T, E>))};
     in.start(row);
@@ -470,6 +503,8 @@ __global__ void __launch_bounds__(kCta<TPR>, ctas_of(TPR, kBwdThreads))
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int j = at + k * kStep;
+            if (past<V>(k, kStep, a.H))
+                break;
             if (j < a.H) {
                 float y[E], x[E];
                 now[0][k].get(y);
@@ -487,6 +522,8 @@ __global__ void __launch_bounds__(kCta<TPR>, ctas_of(TPR, kBwdThreads))
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int j = at + k * kStep;
+            if (past<V>(k, kStep, a.H))
+                break;
             if (j < a.H) {
                 float y[E], x[E], d[E] = {};
                 now[0][k].get(y);
@@ -560,7 +597,6 @@ cudaError_t sm_count(int *n)
     return e != cudaSuccess ? e : cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
 }
 
-// Backward CTAs: as many as the registers of an SM hold, whose sums the workspace keeps.
 // Backward CTAs: as many as run at a time, whose sums the workspace keeps.
 int64_t bwd_ctas(int64_t T, int tpr, int sms)
 {
