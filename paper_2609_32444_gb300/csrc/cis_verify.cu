@@ -884,8 +884,14 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             sum += mass_of(j[i], z[i], d[i]);
         return sum;
     };
+    // (where decreasing offsets make two requests share a row their sums may not be its own: then
+    // too every index stays in the row, and the loops end)
     for (;;) {
         Segment a = {};
+        if (tid == 0) {
+            sh.seg = 0;
+            sh.rest = 0;
+        }
         ulonglong2 listed = make_ulonglong2(0, 0);  // the first of its list, if there is one
         if (tid < segs) {
             a = Segment{__ldcg(&mine[tid].p), __ldcg(&mine[tid].q), __ldcg(&mine[tid].left),
@@ -1030,7 +1036,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 const int src = __ffs(hit) - 1, e = __shfl_sync(0xffffffffu, a1, src);
                 int j = __shfl_sync(0xffffffffu, a0, src);
                 mass_t passed = __shfl_sync(0xffffffffu, at, src);
-                for (;; j += 32) {
+                for (; j < e; j += 32) {
                     mass_t run = j + lane < e ? mass(j + lane) : 0;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
@@ -1054,6 +1060,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                 finish(j, to_f32(row.p[j]));
                 return;
             }
+        }
+        if (!row.residual) {
+            state = kBadRow;
+            finish(-1, 0.0f);
+            return;
         }
         // p is q: the whole of p
         row.residual = false;

@@ -318,6 +318,25 @@ def test_drafts_and_numbers_out_of_range():
     assert lp[0].isnan().all() and lp[1].isfinite().all()
 
 
+@pytest.mark.parametrize("tau", [1.0, 1e-3, 1e3])
+def test_offsets_that_decrease(tau):
+    """The request whose range is none is refused; those that come to share a row with another one
+    get some tokens of the vocabulary, and requests before them their own."""
+    B, D, V, N = 5, 6, 2051, 9
+    z, zd, ids, _, u, ul = _case(B, D, V, F32, 31, ragged=False)
+    z, zd, ids, u = z[:N + B], zd[:N], ids[:N], u[:N]
+    t = torch.tensor([1.0, 1.0, 1.0, tau, 1.0], device=DEV)
+    good = torch.tensor([0, 3, 6, 8, 8, N], dtype=torch.int32, device=DEV)
+    bad = torch.tensor([0, 3, 8, 5, 9, 9], dtype=torch.int32, device=DEV)
+    for q in (zd, None):
+        k = dict(draft_logits=q, temperature=t)
+        st, (tok, kept, _, _) = _status(z, ids, bad, u, ul, D, **k)
+        assert st & BAD_INPUT and kept[2] == -1 and (tok[2] == -1).all()
+        assert (tok >= -1).all() and (tok < V).all() and (kept >= -1).all() and (kept <= D).all()
+        want = _status(z, ids, good, u, ul, D, **k)[1]
+        assert torch.equal(tok[0], want[0][0]) and kept[0] == want[1][0]
+
+
 def test_refusals():
     z, zd, ids, cu, u, ul = _one()
     f = binding.cis_verify_tokens
