@@ -465,11 +465,14 @@ template <typename InT> struct DrawRow {
         same = q == nullptr ||
                ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) == 0;
     }
-    // Segment s has the entries [start(s), start(s + 1)).
+    // Segment s has the entries [start(s), start(s + 1)): a warp's whole turns, 32 vectors each, so
+    // that all lanes have some (B=96, V=151936 without draft rows: 51 us for 54).
     __device__ __forceinline__ int start(int s) const
     {
-        return s == 0 ? 0 : s >= segs ? V
-                                      : head + (int)((int64_t)nvec * s / segs) * Vec<InT>::kN;
+        if (s == 0 || s >= segs)
+            return s == 0 ? 0 : V;
+        const int turn = (int)((int64_t)((nvec + 31) / 32) * s / segs);
+        return head + min(nvec, 32 * turn) * Vec<InT>::kN;
     }
 };
 
@@ -1087,7 +1090,7 @@ template <typename InT> int stretches_of(int64_t rows, int64_t V)
 
 // The second kernel's CTAs a request: four an SM in all, eight where entries are of two rows (the
 // first requests' tokens are drawn while others are added up: B=64, 4 drafts, V=151936: 80 us for 81;
-// B=128, V=32003 fp32: 70 for 73; without the draft's rows, B=96: 57 for 53), 256 entries a segment
+// B=128, V=32003 fp32: 70 for 73; without the draft's rows, B=96: 55 for 51), 256 entries a segment
 // at least, and no more segments than a CTA has threads.
 int groups_of(int64_t B, int64_t V, bool two)
 {
