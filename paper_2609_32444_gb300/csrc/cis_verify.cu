@@ -382,32 +382,38 @@ struct TwoShares {
     }
 };
 
-// The table: T[32 .. 64 steps] from 2^{i / 32} and 2^{j / 2048}, j < 64.
-__device__ inline void fill_parts(mass_t *parts)
+// T, to 2^-58 of itself: every step is the product of the roots 2^{1/2}, 2^{1/4}, ... of its bits,
+// each the whole square root of the one before.
+struct alignas(16) Steps {
+    mass_t t[kSteps];
+};
+constexpr Steps exp2_steps()
 {
-    const int tid = threadIdx.x;
-    auto whole = [](float s, float lo) {  // s + lo in [1, 2), in units of 2^-62
-        return ((mass_t)__float2uint_rn(s * 0x1p24f) << 38) +
-               (mass_t)((long long)__float2int_rn(lo * 0x1p48f) << 14);
-    };
-    if (tid < 64) {
-        constexpr double step = 0.693147180559945309417 / kSteps;
-        constexpr float c = (float)step, cl = (float)(step - (double)c);
-        const float i = (float)tid, x = i * c;
-        float lo;
-        int n;
-        const float s = exp_parts(x, fmaf(i, c, -x) + i * cl, lo, n);
-        parts[tid] = whole(s, lo);
-    } else if (tid < 96) {
-        const float2 T = kExp2Table[tid - 64];
-        parts[tid] = whole(T.x, T.y);
+    using wide = unsigned __int128;
+    Steps s{};
+    s.t[0] = 1ull << 62;
+    mass_t root = 1ull << 63;
+    for (int bit = kSteps / 2; bit > 0; bit >>= 1) {
+        const wide square = (wide)root << 62;
+        root = 0;
+        for (int b = 62; b >= 0; --b) {
+            const mass_t r = root | 1ull << b;
+            root = (wide)r * r <= square ? r : root;
+        }
+        for (int i = bit; i < kSteps; i += 2 * bit) {
+            // (the bits above are in s.t[i - bit] already)
+            s.t[i] = (mass_t)((wide)s.t[i - bit] * root >> 62);
+        }
     }
+    return s;
 }
-__device__ inline void fill_table(mass_t *table, const mass_t *parts)
+__device__ const Steps kExp2Steps = exp2_steps();
+__device__ inline void fill_table(mass_t *table)
 {
+    const ulonglong2 *from = reinterpret_cast<const ulonglong2 *>(kExp2Steps.t);
 #pragma unroll
-    for (int i = threadIdx.x; i < kSteps; i += kVerifyThreads)
-        table[i] = __umul64hi(parts[64 + (i >> 6)], parts[i & 63]) << 2;
+    for (int i = threadIdx.x; i < kSteps / 2; i += kVerifyThreads)
+        reinterpret_cast<ulonglong2 *>(table)[i] = __ldg(from + i);
 }
 
 // What is left of p counts from 2^-32 on: below, it would be made of the masses' errors.
@@ -433,8 +439,7 @@ struct Level {
 
 struct RequestShared {
     Level level[CIS_MAX_DRAFTS + 1];
-    mass_t table[kSteps];
-    mass_t parts[96];
+    alignas(16) mass_t table[kSteps];
     mass_t warps[2][kWarps];
     mass_t rest;
     unsigned many[kWarps];        // segments with too many undecided entries, and
@@ -669,14 +674,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
     if (r.on && r.ok) {
         const int id = tid < r.n ? g.ids[r.a + tid] : -1;
         const float u = tid < r.n ? g.u[r.a + tid] : 0.0f;
-        if (!r.greedy)
-            fill_parts(sh.parts);
         const bool in = id >= 0 && id < g.V;
         const float zx = in ? to_f32(z0[tid * g.ld + id]) : 0.0f;
         const float dx = in && r.model ? to_f32(d0[tid * g.ldd + id]) : 0.0f;
-        __syncthreads();
         if (!r.greedy)
-            fill_table(sh.table, sh.parts);
+            fill_table(sh.table);
         if (tid <= r.n) {
             Level &v = sh.level[tid];
             v.id = id;
