@@ -421,7 +421,8 @@ constexpr mass_t kLeastLeft = 1ull << (kUnitBits - 32);
 
 // A segment's sums: of both rows' masses, of what is left of the first (P - Q, or P), and of Q
 // where something is left; and the number of entries that are not in the last two, as their sign
-// is not settled.  The masses of kListed of them are listed; with more, all are looked at again.
+// is not settled.  The masses of kListed of them are listed; with more, all entries are looked at
+// again.
 constexpr int kListed = 16;
 struct Segment {
     mass_t p, q, left, q_left;
@@ -442,7 +443,7 @@ struct RequestShared {
     alignas(16) mass_t table[kSteps];
     mass_t warps[2][kWarps];
     mass_t rest;
-    unsigned many[kWarps];        // segments with too many undecided entries, and
+    unsigned many[kWarps];        // segments whose entries are looked at again, and
     mass_t more[kVerifyThreads];  // what is left in them
     int undecided[kWarps];
     int seg, found, end, last;
@@ -947,14 +948,19 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
             const mass_t x = __umul64hi(a.q_left, delta);
             left = minus ? left + x : left - x;
             // the entries that were undecided, a thread a segment; where there were too many, all
-            // of them, a warp a segment
+            // of them, a warp a segment.  All of them too where the sum is less than the roundings of
+            // its entries, a unit each: x is rounded once and an entry's Q delta for itself, so that it
+            // can be below 0, or above it where no entry has a mass (flat rows that are nearly equal,
+            // some 10^4 units an entry).
             const int n = (int)a.undecided;
-            const unsigned many = __ballot_sync(0xffffffffu, n > kListed);
+            const bool again =
+                n > kListed || (x != 0 && (long long)left < g.V / segs + 66 * Vec<InT>::kN);
+            const unsigned many = __ballot_sync(0xffffffffu, again);
             auto settled = [&](const ulonglong2 &e) {
                 const mass_t Q = off(e.y);
                 return e.x > Q ? e.x - Q : 0;
             };
-            if (n <= kListed) {
+            if (!again) {
                 left += n > 0 ? settled(listed) : 0;
                 for (int i = 1; i < n; i += 3) {  // (kListed is 1 more than a multiple of 3)
                     const ulonglong2 *at = undecided + (int64_t)tid * kListed + i;
@@ -986,7 +992,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4)
                         sh.more[s] = own;
                 }
             __syncthreads();
-            if (n > kListed)
+            if (again)
                 left = sh.more[tid];
         }
         mass_t R, none;

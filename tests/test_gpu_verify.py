@@ -467,3 +467,53 @@ def test_two_graphs_with_a_workspace_each():
         for (z, zd, ids, cu, u, ul), got in zip(sets, outs):
             want = binding.cis_verify_tokens(z, ids, cu, u, ul, D, draft_logits=zd)
             assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
+
+
+def _nearly_equal_rows(B, V, dtype, seed):
+    """Requests of one draft, rejected.  Near the end are five likely tokens, of which the second is
+    a bf16 step (0.125) below the first in p and the draft; in the draft's row the two change places.
+    Token 0, of 1.7e-4 to 1.9e-4 of the mass, is a step higher there, so that p is above q in all the
+    others' equal logits by 2.2e-5 to 2.6e-5 of itself.  The other entries are 0 in both rows and have
+    e^-31.2 to e^-32.4 of the mass: 0.2 to 0.9 units of 2^-60 are left of each."""
+    g = torch.Generator().manual_seed(seed)
+    z = torch.zeros(2 * B, V)
+    x = 31.2 + 1.2 * torch.rand(B, 1, generator=g)
+    share = 0.2 + torch.rand(B, 5, generator=g)
+    top = (x + torch.log(share / share.sum(1, keepdim=True))).bfloat16().float()
+    top[:, 1] = top[:, 0] - 0.125
+    z[::2, V - 40:V - 15:5] = top
+    z[::2, 0] = (torch.logsumexp(top, 1) + math.log(1.8e-4)).bfloat16().float()
+    z[1::2] = z[::2]
+    assert (z >= 0).all() and (z[:, z[0] != 0] >= 16).all() and (z < 31.875).all()
+    zd = z[::2].clone()
+    zd[:, V - 40], zd[:, V - 35] = z[::2, V - 35], z[::2, V - 40]
+    zd[:, 0] += 0.125
+    cu = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+    ids = torch.full((B,), V - 35, dtype=torch.int32, device=DEV)
+    u = torch.full((B,), 1.0 - 2.0 ** -24, device=DEV)
+    return z.to(DEV, dtype), zd.to(DEV, dtype), ids, cu, u
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,V", [(300, 32000), (30, 151936)])
+def test_little_is_left_of_many_entries(B, V, dtype):
+    """What is left of such entries is lost in whole numbers, and must not come out below 0."""
+    z, zd, ids, cu, u = _nearly_equal_rows(B, V, dtype, V)
+    ul = 0.01 + 0.98 * torch.rand(B, generator=_gen(V), device=DEV)
+    _, kept, _, _ = _check(z, ids, cu, u, ul, 1, zd=zd)
+    assert (kept == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,V", [(300, 32000), (30, 151936)])
+def test_the_first_of_what_is_left(B, V, dtype):
+    """u_last = 0: the first entry of which something is left, wherever the sums say that it begins;
+    not one which p has no more of than q."""
+    z, zd, ids, cu, u = _nearly_equal_rows(B, V, dtype, V + 1)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    tok, kept, _, _ = binding.cis_verify_tokens(z, ids, cu, u, torch.zeros(B, device=DEV), 1,
+                                                draft_logits=zd, dev_status=st)
+    assert int(st) == 0 and (kept == 0).all()
+    j = tok[:, :1].long()
+    p, q = (torch.log_softmax(x.double(), 1).gather(1, j) for x in (z[::2], zd))
+    assert (p > q).all()
