@@ -63,6 +63,27 @@ def test_logits(T, H, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,H,V", [
+    (3, 128, 60001), (64, 272, 60000), (65, 144, 60001), (192, 128, 60003), (256, 384, 60000),
+    (257, 128, 60002), (320, 128, 60000), (320, 1040, 60001), (600, 128, 50003), (2048, 128, 20003)])
+def test_several_tiles_a_cta(T, H, V, dtype):
+    """3 tiles or more for each of up to 152 CTAs or 76 pairs: the accumulators and the ring come round, the
+    third accumulator too (257 to 320 tokens), with several token tiles for a vocabulary tile
+    (above 320)."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T + H + V)
+    x, xs = _rows(T, H, g)
+    w, ws = _rows(V, H, g)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    z = binding.cis_lmhead_logits(x, xs, w, ws, logits_dtype=dtype, dev_status=st)
+    _check(z, x, xs, w, ws)
+    for _ in range(4):
+        again = binding.cis_lmhead_logits(x, xs, w, ws, logits_dtype=dtype, dev_status=st)
+        assert torch.equal(z, again)
+    assert int(st) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T,V,ld,off", [(5, 300, 301, 1), (37, 254, 256, 0), (37, 255, 257, 3),
                                         (300, 512, 520, 8), (20, 128, 128, 1)])
 def test_rows_of_a_wider_buffer(T, V, ld, off, dtype):
