@@ -129,6 +129,48 @@ def test_backward(T, H, dtype):
             _check_bwd(out, dy, h, w, d, m, 1e-6, dtype)
 
 
+def _masks(T, g):
+    """Rows masked at random, with three quarters of them masked one after another, and none."""
+    mask = (torch.rand(T, generator=g, device=DEV) > 0.3).to(torch.uint8)
+    block = mask.clone()
+    block[T // 8:T // 8 + 3 * T // 4] = 0
+    return mask, block, None
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,H", [(110000, 128), (30000, 259), (30000, 520), (28000, 2048),
+                                 (14000, 2531), (14000, 4096), (7000, 8192), (7000, 16384),
+                                 (7000, 8207)])
+def test_forward_many_rows(T, H, dtype):
+    """Some 10 rows or more for each group of threads that is there at a time (152 SMs, 2048 threads each)."""
+    g = _gen(T + H)
+    x, r = _rand(T, H, g, dtype), _rand(T, H, g, dtype, 0.7)
+    w = 1 + 0.2 * torch.randn(H, generator=g, device=DEV)
+    for m in _masks(T, g):
+        out = binding.cis_rmsnorm_fwd(x, w, residual=r, mask=m, want_q=True)
+        _check_fwd(out, x, w, r, m, 1e-6, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,H", [(30000, 128), (30000, 512), (30000, 511), (8000, 777), (8000, 1024),
+                                 (8000, 2048), (4000, 4096), (4000, 2531), (2000, 8192),
+                                 (2000, 16384), (2000, 16383)])
+def test_backward_many_rows(T, H, dtype):
+    """Some 12 rows for each group of threads that is there at a time (152 SMs, 512 threads each): the
+    rows copied ahead come round, in each number of stages, and rows from the ninth on have their
+    mask read later; a block of masked rows is longer than what is known of the mask ahead."""
+    g = _gen(T + H)
+    h, dy, dh = (_rand(T, H, g, dtype, s) for s in (1.0, 1e-3, 1e-3))
+    w = 1 + 0.2 * torch.randn(H, generator=g, device=DEV)
+    for m in _masks(T, g):
+        for d in (dh, None):
+            out = binding.cis_rmsnorm_bwd(dy, h, w, dh=d, mask=m)
+            _check_bwd(out, dy, h, w, d, m, 1e-6, dtype)
+            again = binding.cis_rmsnorm_bwd(dy, h, w, dh=d, mask=m)
+            assert torch.equal(out["dx"], again["dx"])
+            assert torch.equal(out["dweight"], again["dweight"])
+
+
 def test_backward_against_differences():
     """Along random directions, of the forward call's formula in 64 bits."""
     g = _gen(5)
