@@ -540,8 +540,9 @@ __global__ void __launch_bounds__(kCta<TPR>, ctas_of(TPR, kBwdThreads))
         }
     }
     float *out = a.dw + (int64_t)blockIdx.x * a.H;
-    if constexpr (R > 1) {  // the CTA's warps together, in order
-        __shared__ float part[R][32 * E * V];
+    if constexpr (R > 1) {  // the CTA's warps together, in order (where their rows were copied to)
+        float(*part)[32 * E * V] = reinterpret_cast<float(*)[32 * E * V]>(dyn_smem);
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < V; ++k)
 #pragma unroll
@@ -631,7 +632,11 @@ cudaError_t launch(const NormArgs &a, bool bwd, void *workspace, cudaStream_t s)
         return cudaGetLastError();
     }
     constexpr int S = stages_of<T, E, NT, V, 3>(ctas_of(TPR, kBwdThreads));
-    constexpr size_t smem = Rows<T, E, NT, V, 3, S>::kBytes;
+    // (the sums have no place of their own: with 8 KB for them an SM held three CTAs, not four, for H
+    // from 257 to 512; T=65536, H=500 fp32: 91.4 us for 92.9, H=512 85.0 either way)
+    constexpr size_t rows = Rows<T, E, NT, V, 3, S>::kBytes;
+    constexpr size_t sums = R > 1 ? sizeof(float) * R * 32 * E * V : 0;
+    constexpr size_t smem = rows > sums ? rows : sums;
     auto kern = cis_rmsnorm_bwd_kernel<T, E, TPR, V, S>;
     if (smem > 32 * 1024 && (e = allow_smem(kern, smem)) != cudaSuccess)
         return e;
