@@ -114,6 +114,8 @@ __device__ __forceinline__ uint32_t elect_one()
                  : "=r"(p));
     return p;
 }
+// (every warp leaves its loop together: lanes that read the mark at different times would else wait for
+// one another in different places)
 __device__ __forceinline__ bool all(bool x) { return __all_sync(0xffffffffu, x); }
 
 // The leader's (rank 0) barrier at this offset, as a cluster address.
@@ -406,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         Ring acc;
         uint32_t turn = 0;
-        for (int u = first; u < units && !guard.on(); u += step) {
+        for (int u = first; u < units && !all(guard.on()); u += step) {
             const int v0 = (u / g.nN * kCtas + rank) * kM, at = quad * 32 + lane;
             const float ws = v0 + at < g.V ? __ldg(g.ws + v0 + at) : 0.0f;
             // the second accumulator first: the MMAs wait for it
