@@ -18,9 +18,12 @@
 // other.  (Two of 160 took 70 us where no logits were stored, T=320, H=2048, V=151936: as long as
 // 192 would.)
 //
-// Bound: HBM up to 256 tokens (H=2048, V=151936: T=1 51 us a call, 6.1 TB/s; T=256 66 us, 5.9), then
-// the tensor cores (T=320 75 to 85 us; T=2048, V=32000, bf16 logits 76 us, 3.5 PFLOP/s, and 69 with
-// nothing stored), and for fp32 logits the L2 that loads and stores share (T=2048, V=32003: 94 to 112).
+// Bound: HBM up to 256 tokens (H=2048, V=151936: T=1 51 us a call, 6.1 TB/s; T=256 67 us, 5.8; T=320
+// 77 us); with more, no unit by itself.  T=2048, a call and its kernel, and how busy the tensor cores
+// and L2 are: V=32000 84 and 79 us, 79% and 47% (bf16 logits), 94 and 93 us, 67% and 46% (fp32);
+// V=32003 4 to 5 us more.  What stores add is known by these times only.  All at 2070 MHz: after some
+// 50 ms of such calls the power cap takes the clock to 1440 to 1600 MHz, and T=320 takes 87 us, T=2048,
+// V=32000 98 and 109.
 //
 // All waits are bounded: one that runs out sets CIS_ERR_DEVICE_TIMEOUT, and the CTA drains its own
 // loads and MMAs and runs to its end.
@@ -105,7 +108,7 @@ struct Ring {
 // The loading and the MMA warp run as warps, so that the compiler keeps their addresses and
 // descriptors in uniform registers; `one` is true in the lane that issues.  (One lane by itself, its
 // operands moved to uniform registers each time, held the tensor cores up while the other warps were
-// busy: T=2048, H=2048, V=32000, fp32 logits took 101 us.)
+// busy: T=1, H=2048, V=151936 took 56 us for 51.)
 __device__ __forceinline__ uint32_t elect_one()
 {
     uint32_t p;

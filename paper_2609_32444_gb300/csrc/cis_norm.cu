@@ -16,8 +16,11 @@
 //
 // Bound: HBM for many rows (forward, T=16384, H=2048 bf16, 40% masked: 33 us of kernel, 38 a call,
 // for 32 of traffic); backward a row's own chain of copy, sums, reduction and store, some 2,500 cycles
-// with 16 warps an SM (the same batch: 35 us and 3 for dweight's second step, for 28 of traffic;
-// T=3001, H=2531 fp32: 24 for 14, an element at a time).  One row: 3 us of kernel, 7 a call.
+// with 16 warps an SM and 16 valid rows a CTA (the same batch: 35 us and 3 for dweight's second step, for
+// 28 of traffic; issue 56%, HBM 4.4 TB/s).  Rows go to CTAs by their number, whatever the mask: with
+// such a batch's masks the fullest CTA has 20 to 22 valid rows (as many valid rows without a mask: 36 us
+// a call for 42, 4 of them the zeros' traffic).  T=3001, H=2531 fp32: 24 for 14, an element at a time.
+// One row: 3 us of kernel, 7 a call.
 #include <cuda_fp8.h>
 #include <math.h>
 
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(kCta<TPR>) cis_rmsnorm_fwd_kernel(const NormAr
 // The backward kernel's threads an SM, whose rows on their way have kRowBytes of its shared memory
 // (640 threads spill; 8 elements a thread and 768 took 49 us for 42 at T=16384, H=2048, 40% padding;
 // rows read twice from shared memory allow 640 to 1024: 41.5 to 43, and 29 to 35 us for 27 at T=3001,
-// H=2531 fp32).
+// H=2531 fp32: what the warps gave, the second reading took).
 constexpr int kBwdThreads = 512, kRowBytes = 200 * 1024;
 constexpr int kMaxSms = 256;
 // CTAs of TPR threads (128 at least) an SM.

@@ -19,12 +19,16 @@
 // Q (1 + delta), delta = SP / SQ - 1, below 2^-16.  So that one pass does, a segment keeps SP, SQ
 // and, of the entries where P is above Q, the sums of P - Q and of Q, from which max(p - q, 0)
 // follows once delta is known; entries whose sign delta could turn are put in a list instead (a
-// few of a row; some hundreds where bf16 logits and drafts differ by the same step in many).
+// few of a row; some hundreds where bf16 logits and drafts differ by the same step in many).  Where
+// the roundings of these sums could matter, a segment's entries are looked at again.
 // Sums of whole numbers depend on no order.
 //
-// Bound: the first kernel by HBM (B=64, 4 drafts, V=151936 bf16: 32 us, 5.4 TB/s), the second by
-// instruction issue (58 an entry of two rows, 43 to 50 us of the call's 79), or, with few requests, by
-// its dependent steps: stretches, drafts, sums, ticket, prefix, entry (B=1: 5 and 15 us, 21 a call).
+// Bound: the first kernel by HBM (B=64, 4 drafts, V=151936 bf16: 32 us, 5.4 TB/s).  The second, 43 to
+// 50 us of the call's 75 to 80, by nothing that is full (46 to 62% of its issue slots): each CTA fills
+// the table (2 us), puts the stretches together and decides all drafts (2.4), as all of its request's
+// do, and adds up its masses (7: 58 instructions an entry of two rows), in two waves of CTAs, and a
+// request's last CTA draws (5 to 8).  With few requests the steps that depend on one another are all
+// there is: stretches, drafts, sums, ticket, prefix, entry (B=1: 5 and 15 us, 19 to 21 a call).
 #include <math.h>
 
 #include "cis_nvtx.h"
@@ -154,7 +158,7 @@ __device__ __forceinline__ float log_prob(float z, float M, const Scale &sc, con
 }
 
 // CTAs an SM: fp32 rows have more instructions a byte (B=128, up to 8 drafts, V=32003: 66 us a call
-// for 71 with three; bf16 rows, B=64, 4 drafts, V=151936: 82 for 80).
+// for 71 with three, on the same inputs; bf16 rows, B=64, 4 drafts, V=151936: 82 for 80).
 template <typename InT> constexpr int kRowCtas = sizeof(InT) == 4 ? 4 : 3;
 
 // A stretch of one row, of the target's or (the items behind theirs) a draft's, by a warp of its
@@ -290,7 +294,6 @@ __global__ void __launch_bounds__(kVerifyThreads, kRowCtas<InT>)
 
 // ------------------------------------------------------------------ the request
 enum : int { kAccept = 0, kReject = 1, kOpen = 2, kBadRow = 3, kBadDraft = 4 };
-struct Level;
 
 constexpr int kUnitBits = 60;
 constexpr int kSteps = 2048;  // the table's, from 1 to 2
