@@ -609,7 +609,7 @@ CIS_API cis_status_t cis_verify_workspace_size(int64_t B, int64_t V, int32_t max
  *   u_last          device float [B], each in [0, 1).
  *   temperature, draft_temperature
  *                   device float [B], each 0 or in [1e-3, 1e3]; NULL: 1.  A draft_temperature of 0
- *                   is a q that is 1 on the draft.
+ *                   is a q that is 1 on the draft; without draft_logits it is not looked at.
  *   mask            device uint8 [B] or NULL; requests with 0 are not read: tokens and kept -1,
  *                   log-probabilities 0.
  *   tokens_out      device int32 [B, max_drafts + 1]: the kept drafts, the last token, then -1.
